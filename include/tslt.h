@@ -69,6 +69,8 @@ enum {
   TSLT_ROW_TOKEN_NOT_IN_SET = 4, /* a draft token / candidate that is not in its sparse set: rejected */
   TSLT_ROW_BAD_SET = 8,          /* a received set with a value that is not finite or an index outside [0, V): the
                                     position counts as unusable (as for TSLT_ROW_NONFINITE) */
+  TSLT_ROW_BAD_PAGE = 16,        /* a page number that was needed lies outside the cache, or a length outside the page table */
+  TSLT_ROW_BAD_INDEX = 32,       /* an index or a count of new tokens outside those of the call */
   TSLT_ROW_EXACT_PATH = 256      /* informational: the row took the multi-pass selection path (the same row may take
                                     it in a large batch and not in a small one; its set is the same) */
 };
@@ -378,6 +380,106 @@ int tslt_verify_tree(const void* target_logits, tslt_dtype dt, int64_t B, int64_
                      int32_t without_replacement,
                      int32_t* out_node_token, int32_t* out_node_slot, int32_t* out_seq, int32_t* out_len,
                      float* out_ratio, float* out_beta, int32_t* status, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Keys and values in 8 bits --------------------------------------------------------------------------------
+ *
+ * The calls around verification that work on the tokens' keys and values.  The server's target model attends from a round's
+ * tokens (the chain that Algorithm 3 verifies, the tree of Algorithm 8) to all that came before (tslt_cache_attend, whose new
+ * tokens' own keys and values lie beside the cache, so that nothing has to be taken back when tokens are rejected), and what was
+ * accepted is then written into the cache (tslt_cache_append).  Where memory is short, as on the device, each cached token's attention
+ * weight is accumulated (tslt_cache_weigh) and the tokens of least weight are given up (tslt_cache_evict).
+ *
+ * A cache is an array of pages of TSLT_PAGE_TOKENS tokens.  Of every page and head, `codes` holds the keys, [64 tokens][D], and
+ * behind them the values, [4][D][16 tokens], as OCP e4m3 numbers, and `scales` one fp32 power of two for the keys and one for
+ * the values: a number is its code times its scale.  A sequence is a row of the page table, the page of its tokens 0..63,
+ * 64..127, and so on, and a length, both in device memory; no entry behind the length is read.  Keys carry their positions
+ * in themselves, so that where a token lies means nothing.
+ *   - Full pages may stand in the tables of several sequences.  A page that a sequence appends to is its own.
+ *   - D (head_dim) is 64, 128 or 256; heads_q is a multiple of the cache's heads, query head i reads head i / (heads_q / heads).
+ *   - New rows (tslt_rows) are [B][n][heads][D] with D dense and any strides that keep every row's first byte at a
+ *     multiple of 16.  Any of the three element types.
+ *   - A page number outside the cache sets TSLT_ROW_BAD_PAGE for the sequence; its tokens count as absent (attend, weigh), are not written
+ *     (append, evict) or come out as zeros (evict, the page they come from).  A length outside the table sets it too and counts as the nearest that fits. */
+#define TSLT_PAGE_TOKENS 64
+typedef struct {
+  uint8_t* codes;    /* [n_pages][heads][2 * 64 * head_dim], 16-byte aligned */
+  float* scales;     /* [n_pages][heads][2] */
+  int64_t n_pages;
+  int32_t heads;
+  int32_t head_dim;
+} tslt_cache;
+typedef struct {
+  const void* data;
+  int64_t seq_stride, token_stride, head_stride;   /* in elements */
+} tslt_rows;
+
+/* New tokens' keys and values to the end of their sequences.
+ *
+ *   pages [B][width], length [B]   the sequences, see above
+ *   k, v        [B][n][heads][D] of type dt
+ *   index       [B][n] int32: the new tokens to append, in order, the first count[b] of a row; NULL: tokens 0, 1, ...
+ *   count       [B] int32: how many (0..n); NULL: n.  With tslt_verify's accept_len + 1, or the nodes on tslt_verify_tree's
+ *               verified path, only what was accepted enters the cache
+ *   out_length  [B] int32 the sequences' new lengths; not `length` itself
+ *   status      [B] int32; may be NULL
+ * A page's scale is the least power of two, 2^-100 or more, that brings the largest finite magnitude of its head's keys (or
+ * values) to 448 or less, and never less than it was while the page holds older tokens; when it grows, their codes are brought to it.  Numbers
+ * are rounded to nearest-even; infinities become +-448 times the scale, NaN stays.  A page that the call begins is cleared behind its last token.  Tokens that the page table has no room for are not
+ * written, and an index outside 0..n-1 writes zeros (TSLT_ROW_BAD_PAGE, TSLT_ROW_BAD_INDEX).  No workspace. */
+int tslt_cache_append(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
+                      const tslt_rows* k, const tslt_rows* v, tslt_dtype dt, const int32_t* index, const int32_t* count,
+                      int32_t* out_length, int32_t* status, void* stream);
+
+/* Softmax attention of n new tokens a sequence over its cached tokens, all of which every one sees, and over each other:
+ * out_i = sum_j softmax_j(scale * q_i . k_j) v_j.
+ *
+ *   q           [B][n][heads_q][D] of type dt
+ *   k, v        [B][n][heads][D] the new tokens' own keys and values, not quantised; both NULL: the cached tokens alone
+ *   mask        [B][n][ceil(n / 32)] uint32, bit j % 32 of word j / 32 of row i: token i sees token j (for a tree: its
+ *               ancestors and itself).  mask_seq_stride words from a sequence's rows to the next's, 0 where all share one mask.
+ *               NULL: token i sees tokens 0..i
+ *   count       [B] int32: how many of the n tokens there are (0..n; the others' rows come out empty); NULL: n
+ *   scale       > 0
+ *   out         [B][n][heads_q][D] of type dt, dense, 16-byte aligned
+ *   out_lse     [B][n][heads_q] fp32: ln sum_j exp(scale * q_i . k_j)
+ *   status      [B] int32; may be NULL
+ * A row that sees nothing gives zeros and -inf.  What a row does not see has no part in it, whatever it holds, NaN and
+ * infinities too.  A seen value that is not finite goes into the sum as it is; a query, or a seen key, that is not finite makes
+ * NaN of its rows, or whatever fp32's rules give.  Sums, maxima and the softmax are fp32, weights are rounded to 16 bits or more
+ * before they meet the values (24 for fp32 rows).
+ * Workspace: tslt_cache_attend_workspace_bytes of the same arguments, 256-byte aligned; it need not be cleared.  0 where none is needed. */
+size_t tslt_cache_attend_workspace_bytes(int64_t B, int32_t n, int32_t heads_q, int32_t heads, int32_t head_dim, int64_t width);
+int tslt_cache_attend(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
+                      int32_t heads_q, const tslt_rows* q, const tslt_rows* k, const tslt_rows* v, tslt_dtype dt, const uint32_t* mask,
+                      int64_t mask_seq_stride, const int32_t* count, float scale, void* out, float* out_lse, int32_t* status, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/* The attention weight that each cached token got in a round, added to what it had:
+ * out_weight_j = decay * weight_j + sum over the n tokens and the query heads that share a head of exp(scale * q_i . k_j - lse_i).
+ *
+ *   q, count, scale   as tslt_cache_attend was given them, and lse its out_lse (a row with -inf adds nothing)
+ *   weight, out_weight  [B][heads][width * 64] fp32, may be the same array; 0 is written at and behind a sequence's length, so that tokens
+ *               appended later begin with 0
+ *   status      [B] int32; may be NULL
+ * No atomics: the same call gives the same bits.  No workspace. */
+int tslt_cache_weigh(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
+                     int32_t heads_q, const tslt_rows* q, tslt_dtype dt, const float* lse, const int32_t* count, float scale,
+                     const float* weight, float decay, float* out_weight, int32_t* status, void* stream);
+
+/* Keeps min(length, keep) tokens of every head of every sequence: the last min(recent, that many) ones, and of those before
+ * them the ones of most weight, of equal weights the first (NaN counts as the least).  They are copied, in their order, to new pages.
+ *
+ *   weight      [B][heads][width * 64] as tslt_cache_weigh writes it
+ *   new_pages   [B][new_width], new_width >= ceil(keep / 64): pages of the same cache that no table in use holds
+ *   out_length  [B] int32; not `length` itself
+ *   out_kept    [B][heads][keep] int32: where the kept tokens lay, ascending; -1 behind them
+ *   out_weight  [B][heads][new_width * 64] fp32: their weights, 0 behind them; not `weight` itself
+ *   status      [B] int32; may be NULL
+ * A new page's scales are the largest of the pages that its tokens come from; codes of others are brought to them, rounded to
+ * nearest-even.  The old pages are left as they are, for the caller to use again once the stream has got past the call.  No workspace. */
+int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, const float* weight,
+                     int32_t keep, int32_t recent, const int32_t* new_pages, int64_t new_width, int32_t* out_length, int32_t* out_kept,
+                     float* out_weight, int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

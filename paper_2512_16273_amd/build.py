@@ -7,20 +7,23 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libtslt.so")
 BINDING_PATH = os.path.join(HERE, "_binding.so")
 BINDING_SOURCE = os.path.join(HERE, "csrc", "binding.cpp")
-SOURCES = [os.path.join(HERE, "csrc", "tslt.hip")]
-HEADERS = [os.path.join(HERE, "csrc", n) for n in ("common.h", "bins.h", "handover.h", "pow_table.h", "truncate.h", "sample.h", "verify.h", "rowops.h", "rowsample.h", "exp64.h", "tree.h", "wire.h", "stats.h", "calib.h")] + \
+SOURCES = [os.path.join(HERE, "csrc", n) for n in ("tslt.hip", "cache.hip", "attend_f32.hip", "attend_bf16.hip", "attend_f16.hip")]
+HEADERS = [os.path.join(HERE, "csrc", n) for n in ("common.h", "bins.h", "handover.h", "pow_table.h", "truncate.h", "sample.h", "verify.h", "rowops.h", "rowsample.h", "exp64.h", "tree.h", "wire.h", "stats.h", "calib.h",
+                                                   "error.h", "cache.h", "append.h", "attend.h", "attend_launch.h", "weigh.h", "evict.h")] + \
           [os.path.join(ROOT, "include", "tslt.h")]
 
 
-def hipcc_command(out: str = LIB_PATH) -> list:
+def hipcc_command(out: str = LIB_PATH, sources: list = SOURCES, kind: str = "-shared") -> list:
+    """One command that makes `out` of `sources`; build_library compiles each source by one of its own, at the same time."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    return [hipcc, "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
+    return [hipcc, "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", kind,
             # packed-fp32 instructions are kept out of the generated code
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
             # loop-invariant code motion after instruction selection: it carries fp64 constants through the tree
@@ -29,7 +32,7 @@ def hipcc_command(out: str = LIB_PATH) -> list:
             "-mllvm", "-disable-machine-licm",
             "-Wall", "-Wno-unused-function",
             "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
-            "-o", out] + SOURCES
+            "-o", out] + list(sources)
 
 
 def built_for() -> str:
@@ -55,18 +58,31 @@ def binding_command(out: str = BINDING_PATH) -> list:
             "-o", out, BINDING_SOURCE, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
-def build_library(verbose: bool = True) -> str:
-    commands = [hipcc_command()]
-    if binding_possible():
-        commands.append(binding_command())
-    else:
-        print("no host compiler, or no headers of torch or Python: calls go through ctypes", flush=True)
-        if os.path.exists(BINDING_PATH):
-            os.remove(BINDING_PATH)                    # (of an earlier source, perhaps)
+def _run(commands: list, verbose: bool) -> None:
+    """All of them at the same time; raises if one fails."""
+    running = []
     for cmd in commands:
         if verbose:
             print(" ".join(cmd), flush=True)
-        subprocess.run(cmd, check=True)
+        running.append((cmd, subprocess.Popen(cmd)))
+    for cmd, process in running:
+        process.wait()
+    for cmd, process in running:
+        if process.returncode != 0:
+            raise subprocess.CalledProcessError(process.returncode, cmd)
+
+
+def build_library(verbose: bool = True) -> str:
+    bind = binding_possible()
+    if not bind:
+        print("no host compiler, or no headers of torch or Python: calls go through ctypes", flush=True)
+        if os.path.exists(BINDING_PATH):
+            os.remove(BINDING_PATH)                    # (of an earlier source, perhaps)
+    with tempfile.TemporaryDirectory() as made:
+        objects = [os.path.join(made, os.path.basename(s) + ".o") for s in SOURCES]
+        _run([hipcc_command(o, [s], "-c") for s, o in zip(SOURCES, objects)] + ([binding_command()] if bind else []), verbose)
+        hipcc = hipcc_command()[0]
+        _run([[hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", LIB_PATH] + objects], verbose)
     return LIB_PATH
 
 

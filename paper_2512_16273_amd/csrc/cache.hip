@@ -1,0 +1,221 @@
+// C ABI of the 8-bit key/value cache (see include/tslt.h): argument checks, launch plans, kernel launches.
+#include "tslt.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "append.h"
+#include "attend.h"
+#include "error.h"
+#include "evict.h"
+#include "weigh.h"
+
+namespace {
+
+using tslt::fail;
+
+int elem_bytes(tslt_dtype dt) { return dt == TSLT_F32 ? 4 : 2; }
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+// What every call says of its cache and its sequences; 0 if the kernels can take it.
+int check_cache(const char* who, const tslt_cache* c, const int32_t* pages, int64_t width, const int32_t* length, int64_t B) {
+  if (!c) return fail(TSLT_ERR_INVALID_ARG, "%s: null cache", who);
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)
+    return fail(TSLT_ERR_UNSUPPORTED, "%s: head_dim must be 64, 128 or 256 (got %d)", who, int(c->head_dim));
+  if (c->heads < 1 || c->n_pages < 1 || c->n_pages > 0x7FFFFFFF || B < 0 || width < 1)
+    return fail(TSLT_ERR_INVALID_ARG, "%s: bad shape heads=%d n_pages=%lld B=%lld width=%lld", who, int(c->heads), (long long)c->n_pages, (long long)B, (long long)width);
+  if (width > 0x7FFFFFFF / TSLT_PAGE_TOKENS) return fail(TSLT_ERR_UNSUPPORTED, "%s: a sequence's tokens must fit 31 bits", who);
+  if (B == 0) return TSLT_OK;
+  if (!c->codes || !c->scales || !pages || !length) return fail(TSLT_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (!aligned(c->codes, 16)) return fail(TSLT_ERR_INVALID_ARG, "%s: codes not aligned to 16 bytes", who);
+  return TSLT_OK;
+}
+// Rows of new tokens: 16 bytes at a time are read of each.
+int check_rows(const char* who, const char* what, const tslt_rows* r, tslt_dtype dt) {
+  if (!r || !r->data) return fail(TSLT_ERR_INVALID_ARG, "%s: null %s", who, what);
+  const int64_t unit = 16 / elem_bytes(dt);
+  if (!aligned(r->data, 16) || r->seq_stride % unit || r->token_stride % unit || r->head_stride % unit)
+    return fail(TSLT_ERR_INVALID_ARG, "%s: rows of %s must begin at multiples of 16 bytes", who, what);
+  return TSLT_OK;
+}
+bool valid_dtype(tslt_dtype dt) { return dt == TSLT_F32 || dt == TSLT_BF16 || dt == TSLT_F16; }
+tslt::CacheView view(const tslt_cache* c, const int32_t* pages, int64_t width, const int32_t* length) {
+  return tslt::CacheView{c->codes, c->scales, c->n_pages, int(c->heads), pages, width, length};
+}
+tslt::RowsView view(const tslt_rows* r) {
+  return r ? tslt::RowsView{r->data, r->seq_stride, r->token_stride, r->head_stride} : tslt::RowsView{nullptr, 0, 0, 0};
+}
+bool grid_fits(const char* who, int64_t blocks, int& code) {
+  code = blocks > 0x7FFFFFFF ? fail(TSLT_ERR_UNSUPPORTED, "%s: too many workgroups for one launch", who) : 0;
+  return code == 0;
+}
+int launched(const char* who) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TSLT_OK : tslt::hip_fail(e, who);
+}
+
+template <template <typename, int> class Launch, typename P> void by_type(tslt_dtype dt, int D, const P& p, unsigned blocks, hipStream_t s) {
+#define TSLT_BY_D(T) (D == 64 ? Launch<T, 64>::go(p, blocks, s) : D == 128 ? Launch<T, 128>::go(p, blocks, s) : Launch<T, 256>::go(p, blocks, s))
+  dt == TSLT_F32 ? TSLT_BY_D(float) : dt == TSLT_BF16 ? TSLT_BY_D(tslt::Bf16) : TSLT_BY_D(tslt::F16);
+#undef TSLT_BY_D
+}
+template <typename T, int D> struct Append {
+  static void go(const tslt::AppendParams& p, unsigned blocks, hipStream_t s) { hipLaunchKernelGGL((tslt::append_kernel<T, D>), dim3(blocks), dim3(256), 0, s, p); }
+};
+template <typename T, int D> struct Weigh {
+  static void go(const tslt::WeighParams& p, unsigned blocks, hipStream_t s) { hipLaunchKernelGGL((tslt::weigh_kernel<T, D>), dim3(blocks), dim3(256), 0, s, p); }
+};
+
+// How an attention call is cut: row groups, and chunks of a sequence's pages.
+void plan_attend(tslt::AttendParams& p) {
+  const int64_t rows = int64_t(p.n) * p.group, per = tslt::attend_rows(rows);
+  p.row_groups = int((rows + per - 1) / per);
+  const int64_t units = p.B * p.c.heads * p.row_groups, want = 8 * int64_t(tslt::compute_units());
+  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(want / units, (p.c.width + 3) / 4));
+  p.chunk = int((p.c.width + chunks - 1) / chunks);
+  p.chunks = int((p.c.width + p.chunk - 1) / p.chunk);
+}
+size_t attend_part_bytes(const tslt::AttendParams& p, int D) {
+  if (p.chunks == 1) return 0;
+  const size_t rows = size_t(p.B) * p.c.heads * p.chunks * p.n * p.group;
+  return (rows * (D * 4 + 8) + 255) / 256 * 256;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tslt_cache_append(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
+                      const tslt_rows* k, const tslt_rows* v, tslt_dtype dt, const int32_t* index, const int32_t* count,
+                      int32_t* out_length, int32_t* status, void* stream) {
+  const char* who = "tslt_cache_append";
+  if (int e = check_cache(who, cache, pages, width, length, B)) return e;
+  if (!valid_dtype(dt)) return fail(TSLT_ERR_INVALID_ARG, "%s: unknown dtype %d", who, int(dt));
+  if (n < 1) return fail(TSLT_ERR_INVALID_ARG, "%s: n must be at least 1", who);
+  if (B == 0) return TSLT_OK;
+  if (int e = check_rows(who, "k", k, dt)) return e;
+  if (int e = check_rows(who, "v", v, dt)) return e;
+  if (!out_length) return fail(TSLT_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (out_length == length) return fail(TSLT_ERR_INVALID_ARG, "%s: out_length must not be length", who);
+  tslt::AppendParams p{};
+  p.c = view(cache, pages, width, length);
+  p.k = view(k); p.v = view(v);
+  p.B = B; p.n = n; p.index = index; p.count = count; p.out_length = out_length; p.status = status;
+  p.most_pages = int((int64_t(n) + tslt::kPage - 2) / tslt::kPage + 1);
+  const int64_t blocks = B * cache->heads * p.most_pages;
+  int code;
+  if (!grid_fits(who, blocks, code)) return code;
+  by_type<Append>(dt, cache->head_dim, p, unsigned(blocks), reinterpret_cast<hipStream_t>(stream));
+  return launched("tslt_cache_append launch");
+}
+
+size_t tslt_cache_attend_workspace_bytes(int64_t B, int32_t n, int32_t heads_q, int32_t heads, int32_t head_dim, int64_t width) {
+  if (B < 1 || n < 1 || heads < 1 || heads_q < heads || heads_q % heads || width < 1 || width > 0x7FFFFFFF / TSLT_PAGE_TOKENS) return 0;
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256) return 0;
+  tslt::AttendParams p{};
+  p.B = B; p.n = n; p.group = heads_q / heads; p.c.heads = heads; p.c.width = width;
+  plan_attend(p);
+  return attend_part_bytes(p, head_dim);
+}
+
+int tslt_cache_attend(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
+                      int32_t heads_q, const tslt_rows* q, const tslt_rows* k, const tslt_rows* v, tslt_dtype dt, const uint32_t* mask,
+                      int64_t mask_seq_stride, const int32_t* count, float scale, void* out, float* out_lse, int32_t* status, void* ws,
+                      size_t ws_bytes, void* stream) {
+  const char* who = "tslt_cache_attend";
+  if (int e = check_cache(who, cache, pages, width, length, B)) return e;
+  if (!valid_dtype(dt)) return fail(TSLT_ERR_INVALID_ARG, "%s: unknown dtype %d", who, int(dt));
+  if (n < 1) return fail(TSLT_ERR_INVALID_ARG, "%s: n must be at least 1", who);
+  if (heads_q < cache->heads || heads_q % cache->heads) return fail(TSLT_ERR_INVALID_ARG, "%s: heads_q must be a multiple of the cache's heads", who);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(TSLT_ERR_INVALID_ARG, "%s: scale must be > 0", who);
+  if (int64_t(n) * (heads_q / cache->heads) > 0x3FFFFFFF) return fail(TSLT_ERR_UNSUPPORTED, "%s: too many rows", who);
+  if (B == 0) return TSLT_OK;
+  if (int e = check_rows(who, "q", q, dt)) return e;
+  if ((k == nullptr) != (v == nullptr)) return fail(TSLT_ERR_INVALID_ARG, "%s: k and v come together", who);
+  if (k) {
+    if (int e = check_rows(who, "k", k, dt)) return e;
+    if (int e = check_rows(who, "v", v, dt)) return e;
+  }
+  if (!out || !out_lse) return fail(TSLT_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (!aligned(out, 16)) return fail(TSLT_ERR_INVALID_ARG, "%s: out not aligned to 16 bytes", who);
+  if (mask && mask_seq_stride < 0) return fail(TSLT_ERR_INVALID_ARG, "%s: mask_seq_stride must not be negative", who);
+  tslt::AttendParams p{};
+  p.c = view(cache, pages, width, length);
+  p.q = view(q); p.k = view(k); p.v = view(v);
+  p.B = B; p.n = n; p.group = heads_q / cache->heads; p.heads_q = heads_q;
+  p.mask = mask; p.mask_seq = mask_seq_stride; p.mask_words = (n + 31) / 32; p.count = count;
+  p.scale2 = float(double(scale) * 1.4426950408889634074);
+  p.out = out; p.lse = out_lse; p.status = status;
+  plan_attend(p);
+  const size_t need = attend_part_bytes(p, cache->head_dim);
+  if (need > 0) {
+    if (!ws || !aligned(ws, 256) || ws_bytes < need)
+      return fail(TSLT_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu are needed, 256-byte aligned", who, ws ? ws_bytes : size_t(0), need);
+    const size_t rows = size_t(B) * cache->heads * p.chunks * n * p.group;
+    p.part_o = reinterpret_cast<float*>(ws);
+    p.part_ml = reinterpret_cast<float2*>(p.part_o + rows * cache->head_dim);
+  }
+  int code;
+  if (!grid_fits(who, (B * cache->heads * p.chunks + 8) * p.row_groups, code)) return code;
+  if (!grid_fits(who, B * cache->heads * ((int64_t(n) * p.group + tslt::kJoinRows - 1) / tslt::kJoinRows), code)) return code;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const hipError_t e = dt == TSLT_F32 ? tslt::launch_attend<float>(p, cache->head_dim, s)
+                       : dt == TSLT_BF16 ? tslt::launch_attend<tslt::Bf16>(p, cache->head_dim, s) : tslt::launch_attend<tslt::F16>(p, cache->head_dim, s);
+  if (e != hipSuccess) return tslt::hip_fail(e, "hipFuncSetAttribute");
+  return launched("tslt_cache_attend launch");
+}
+
+int tslt_cache_weigh(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
+                     int32_t heads_q, const tslt_rows* q, tslt_dtype dt, const float* lse, const int32_t* count, float scale,
+                     const float* weight, float decay, float* out_weight, int32_t* status, void* stream) {
+  const char* who = "tslt_cache_weigh";
+  if (int e = check_cache(who, cache, pages, width, length, B)) return e;
+  if (!valid_dtype(dt)) return fail(TSLT_ERR_INVALID_ARG, "%s: unknown dtype %d", who, int(dt));
+  if (n < 1) return fail(TSLT_ERR_INVALID_ARG, "%s: n must be at least 1", who);
+  if (heads_q < cache->heads || heads_q % cache->heads) return fail(TSLT_ERR_INVALID_ARG, "%s: heads_q must be a multiple of the cache's heads", who);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(TSLT_ERR_INVALID_ARG, "%s: scale must be > 0", who);
+  if (!std::isfinite(decay)) return fail(TSLT_ERR_INVALID_ARG, "%s: decay must be finite", who);
+  if (int64_t(n) * (heads_q / cache->heads) > 0x3FFFFFFF) return fail(TSLT_ERR_UNSUPPORTED, "%s: too many rows", who);
+  if (B == 0) return TSLT_OK;
+  if (int e = check_rows(who, "q", q, dt)) return e;
+  if (!lse || !weight || !out_weight) return fail(TSLT_ERR_INVALID_ARG, "%s: null pointer", who);
+  tslt::WeighParams p{};
+  p.c = view(cache, pages, width, length);
+  p.q = view(q);
+  p.B = B; p.n = n; p.group = heads_q / cache->heads; p.heads_q = heads_q; p.count = count; p.lse = lse;
+  p.scale2 = float(double(scale) * 1.4426950408889634074);
+  p.decay = decay; p.weight = weight; p.out_weight = out_weight; p.status = status;
+  const int64_t blocks = B * cache->heads * ((width + 3) / 4);
+  int code;
+  if (!grid_fits(who, blocks, code)) return code;
+  by_type<Weigh>(dt, cache->head_dim, p, unsigned(blocks), reinterpret_cast<hipStream_t>(stream));
+  return launched("tslt_cache_weigh launch");
+}
+
+int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, const float* weight,
+                     int32_t keep, int32_t recent, const int32_t* new_pages, int64_t new_width, int32_t* out_length, int32_t* out_kept,
+                     float* out_weight, int32_t* status, void* stream) {
+  const char* who = "tslt_cache_evict";
+  if (int e = check_cache(who, cache, pages, width, length, B)) return e;
+  if (keep < 1 || recent < 0) return fail(TSLT_ERR_INVALID_ARG, "%s: keep must be at least 1, recent at least 0", who);
+  if (new_width < (int64_t(keep) + tslt::kPage - 1) / tslt::kPage) return fail(TSLT_ERR_INVALID_ARG, "%s: %lld new pages a sequence do not hold %d tokens", who, (long long)new_width, int(keep));
+  if (new_width > 0x7FFFFFFF / TSLT_PAGE_TOKENS) return fail(TSLT_ERR_UNSUPPORTED, "%s: a sequence's tokens must fit 31 bits", who);
+  if (B == 0) return TSLT_OK;
+  if (!weight || !new_pages || !out_length || !out_kept || !out_weight) return fail(TSLT_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (out_length == length) return fail(TSLT_ERR_INVALID_ARG, "%s: out_length must not be length", who);
+  if (out_weight == weight) return fail(TSLT_ERR_INVALID_ARG, "%s: out_weight must not be weight", who);
+  tslt::EvictParams p{};
+  p.c = view(cache, pages, width, length);
+  p.B = B; p.weight = weight; p.keep = keep; p.recent = recent; p.new_pages = new_pages; p.new_width = new_width;
+  p.out_length = out_length; p.out_kept = out_kept; p.out_weight = out_weight; p.status = status;
+  const int64_t heads = B * cache->heads, moves = heads * ((keep + tslt::kPage - 1) / tslt::kPage);
+  int code;
+  if (!grid_fits(who, std::max(heads, moves), code)) return code;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(tslt::evict_select_kernel, dim3(unsigned(heads)), dim3(tslt::kEvictThreads), 0, s, p);
+  const auto move = cache->head_dim == 64 ? tslt::evict_move_kernel<64> : cache->head_dim == 128 ? tslt::evict_move_kernel<128> : tslt::evict_move_kernel<256>;
+  hipLaunchKernelGGL(move, dim3(unsigned(moves)), dim3(256), 0, s, p);
+  return launched("tslt_cache_evict launch");
+}
+
+}  // extern "C"

@@ -11,6 +11,7 @@
 #include <string>
 
 #include "common.h"
+#include "error.h"
 #include "sample.h"
 #include "truncate.h"
 #include "wire.h"
@@ -26,8 +27,10 @@
 static __device__ __align__(256) unsigned char scratch[TSLT_STATIC_SCRATCH_BYTES];
 
 namespace {
-
 thread_local std::string g_last_error;
+}
+
+namespace tslt {
 
 int fail(int code, const char* fmt, ...) {
   char buf[512];
@@ -42,6 +45,13 @@ int fail(int code, const char* fmt, ...) {
 int hip_fail(hipError_t e, const char* what) {
   return fail(TSLT_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace tslt
+
+namespace {
+
+using tslt::fail;
+using tslt::hip_fail;
 
 bool valid_dtype(tslt_dtype dt) { return dt == TSLT_F32 || dt == TSLT_BF16 || dt == TSLT_F16; }
 int elem_bytes(tslt_dtype dt) { return dt == TSLT_F32 ? 4 : 2; }

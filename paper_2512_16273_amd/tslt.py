@@ -27,13 +27,25 @@ LIB_PATH = os.path.join(_HERE, "libtslt.so")
 F32, BF16, F16 = 0, 1, 2
 OP_TRUNCATE, OP_SAMPLE, OP_VERIFY, OP_VERIFY_TREE, OP_VERIFY_TREE_PATH, OP_TRUNCATE_SHARED = 0, 1, 2, 3, 4, 5
 ROW_NONFINITE, ROW_EMPTY, ROW_TOKEN_NOT_IN_SET, ROW_BAD_SET, ROW_EXACT_PATH = 1, 2, 4, 8, 256
+ROW_BAD_PAGE, ROW_BAD_INDEX = 16, 32
+PAGE_TOKENS = 64
 MAX_K_CAP = 1024
 PAYLOAD = {"f32": 0, "bf16": 1, "f16": 2}       # tslt_dtype codes of the formats a payload can travel in
 
 EXPORTS = ("tslt_version", "tslt_last_error", "tslt_workspace_bytes", "tslt_truncate", "tslt_truncate_sample", "tslt_sample",
            "tslt_pack_bound_words", "tslt_pack", "tslt_pack_cleared", "tslt_unpack",
            "tslt_verify", "tslt_verify_accept", "tslt_verify_resample", "tslt_verify_staged", "tslt_verify_accept_staged",
-           "tslt_verify_static", "tslt_truncation_stats", "tslt_multicandidate_stats", "tslt_calibrate_read", "tslt_verify_tree")
+           "tslt_verify_static", "tslt_truncation_stats", "tslt_multicandidate_stats", "tslt_calibrate_read", "tslt_verify_tree",
+           "tslt_cache_append", "tslt_cache_attend", "tslt_cache_attend_workspace_bytes", "tslt_cache_weigh", "tslt_cache_evict")
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
 
 _lib = None
 _fast = None                                    # the module _binding, bound to the library that is loaded (None: there is none to use)
@@ -92,6 +104,17 @@ def load(path: Optional[str] = None):
     lib.tslt_verify_tree.restype = c.c_int
     lib.tslt_verify_tree.argtypes = [vp, c.c_int, i64, i64, i64, f32, i32, c.POINTER(i32), vp, vp, vp, i32, vp, vp,
                                      vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    cache, rows = c.POINTER(_Cache), c.POINTER(_Rows)
+    lib.tslt_cache_append.restype = c.c_int
+    lib.tslt_cache_append.argtypes = [cache, vp, i64, vp, i64, i32, rows, rows, c.c_int, vp, vp, vp, vp, vp]
+    lib.tslt_cache_attend_workspace_bytes.restype = sz
+    lib.tslt_cache_attend_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64]
+    lib.tslt_cache_attend.restype = c.c_int
+    lib.tslt_cache_attend.argtypes = [cache, vp, i64, vp, i64, i32, i32, rows, rows, rows, c.c_int, vp, i64, vp, f32, vp, vp, vp, vp, sz, vp]
+    lib.tslt_cache_weigh.restype = c.c_int
+    lib.tslt_cache_weigh.argtypes = [cache, vp, i64, vp, i64, i32, i32, rows, c.c_int, vp, vp, f32, vp, f32, vp, vp, vp]
+    lib.tslt_cache_evict.restype = c.c_int
+    lib.tslt_cache_evict.argtypes = [cache, vp, i64, vp, i64, vp, i32, i32, vp, i64, vp, vp, vp, vp, vp]
     _fast = _native_binding()
     if _fast is not None:
         _fast.bind(*[c.cast(getattr(lib, fn), vp).value for fn in (
@@ -463,4 +486,182 @@ def verify_tree(target: torch.Tensor, temperature: float, expansion: Sequence[in
                                 _ptr(out.get("node_token")),
                                 _ptr(out.get("node_slot")), _ptr(out["seq"]), _ptr(out["len"]), _ptr(out.get("ratio")),
                                 _ptr(out.get("beta")), _ptr(out.get("status")), _ptr(ws), ws.numel() if ws is not None else 0, _stream()))
+    return out
+
+
+# ---- keys and values in 8 bits -----------------------------------------------------------------------------------
+
+def cache_create(n_pages: int, heads: int, head_dim: int, device="cuda") -> dict:
+    """An empty cache: codes [n_pages, heads, 2, 64 * head_dim] uint8 and scale [n_pages, heads, 2] fp32 (see include/tslt.h for
+    their layout)."""
+    return {"codes": torch.zeros(n_pages, heads, 2, PAGE_TOKENS * head_dim, dtype=torch.uint8, device=device),
+            "scale": torch.ones(n_pages, heads, 2, dtype=torch.float32, device=device)}
+
+
+def tree_mask(expansion: Sequence[int], device="cuda") -> torch.Tensor:
+    """The mask of cache_attend for a token tree stored breadth-first, as verify_tree takes it: [1, N_nodes, ceil(N_nodes / 32)]
+    int32, of every node its ancestors and itself."""
+    rows, layer = [1], [0]
+    for k in expansion:
+        layer = [parent for parent in layer for _ in range(int(k))]
+        rows += [0] * len(layer)
+        first = len(rows) - len(layer)
+        for i, parent in enumerate(layer):
+            rows[first + i] = rows[parent] | 1 << (first + i)
+        layer = list(range(first, len(rows)))
+    words = (len(rows) + 31) // 32
+    bits = b"".join(r.to_bytes(4 * words, "little") for r in rows)
+    return torch.frombuffer(bytearray(bits), dtype=torch.int32).view(1, len(rows), words).to(device)
+
+
+def _cache_of(cache: dict):
+    codes, scale = cache["codes"], cache["scale"]
+    _dev(codes, torch.uint8, "codes"); _dev(scale, torch.float32, "scale")
+    if codes.dim() != 4 or codes.shape[2] != 2 or codes.shape[3] % PAGE_TOKENS or scale.shape != codes.shape[:3]:
+        raise TsltError("a cache is codes [n_pages, heads, 2, 64 * head_dim] and scale [n_pages, heads, 2]")
+    n_pages, heads, _, size = codes.shape
+    return _Cache(codes.data_ptr(), scale.data_ptr(), n_pages, heads, size // PAGE_TOKENS), heads, size // PAGE_TOKENS
+
+
+def _sequences(pages: torch.Tensor, length: torch.Tensor):
+    _dev(pages, torch.int32, "pages"); _dev(length, torch.int32, "length")
+    if pages.dim() != 2 or length.numel() != pages.shape[0]:
+        raise TsltError("pages must be [B, width], length [B]")
+    return pages.shape
+
+
+def _rows_of(t: torch.Tensor, name: str, shape, dtype) -> _Rows:
+    _dev(t, dtype, name, contiguous=False)
+    if tuple(t.shape) != tuple(shape):
+        raise TsltError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise TsltError(f"{name} must be dense along its last dimension")
+    seq, token, head = (s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape[:3]))      # (what no second row uses may be anything)
+    return _Rows(t.data_ptr(), seq, token, head)
+
+
+def _counted(t: Optional[torch.Tensor], name: str, numel: int) -> Optional[int]:
+    if t is None:
+        return None
+    _dev(t, torch.int32, name)
+    if t.numel() != numel:
+        raise TsltError(f"{name} has {t.numel()} entries, {numel} are needed")
+    return t.data_ptr()
+
+
+def _sized(out: dict, name: str, dtype, numel: int, optional=False) -> Optional[int]:
+    t = out.get(name)
+    if t is None and optional:
+        return None
+    if t is None:
+        raise TsltError(f"out holds no {name}")
+    _dev(t, dtype, name)
+    if t.numel() != numel:
+        raise TsltError(f"{name} has {t.numel()} entries, {numel} are needed")
+    return t.data_ptr()
+
+
+def cache_append(cache: dict, pages: torch.Tensor, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                 count: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None, out: Optional[dict] = None) -> dict:
+    """tslt_cache_append: k, v [B, n, heads, D] (any of the three types, any strides that keep rows 16-byte aligned) to the end of
+    the sequences pages [B, width], length [B] of the cache, which changes in place.  count [B]: how many of the n tokens; index [B, n]:
+    which ones.  Returns length, the new one, and status [B]."""
+    lib = load()
+    c, heads, D = _cache_of(cache)
+    B, width = _sequences(pages, length)
+    if k.dim() != 4:
+        raise TsltError("k must be [B, n, heads, D]")
+    n = k.shape[1]
+    kr, vr = _rows_of(k, "k", (B, n, heads, D), k.dtype), _rows_of(v, "v", (B, n, heads, D), k.dtype)
+    if out is None:
+        out = {"length": torch.empty(B, dtype=torch.int32, device=k.device), "status": torch.empty(B, dtype=torch.int32, device=k.device)}
+    _check(lib.tslt_cache_append(c, pages.data_ptr(), width, length.data_ptr(), B, n, kr, vr, _dtype_code(k),
+                                 _counted(index, "index", B * n), _counted(count, "count", B), _sized(out, "length", torch.int32, B),
+                                 _sized(out, "status", torch.int32, B, optional=True), _stream()))
+    return out
+
+
+def cache_attend_workspace_bytes(B: int, n: int, heads_q: int, heads: int, head_dim: int, width: int) -> int:
+    return int(load().tslt_cache_attend_workspace_bytes(B, n, heads_q, heads, head_dim, width))
+
+
+def cache_attend(q: torch.Tensor, cache: dict, pages: torch.Tensor, length: torch.Tensor, k: Optional[torch.Tensor] = None,
+                 v: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                 scale: Optional[float] = None, out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None) -> dict:
+    """tslt_cache_attend: q [B, n, heads_q, D] over the sequences' cached tokens and, where k, v [B, n, heads, D] are given, over the new
+    tokens that `mask` shows ([B or 1, n, ceil(n / 32)] int32, see tree_mask; None: a chain).  scale: 1 / sqrt(D).  Returns out
+    [B, n, heads_q, D], lse [B, n, heads_q] and status [B]."""
+    lib = load()
+    c, heads, D = _cache_of(cache)
+    B, width = _sequences(pages, length)
+    if q.dim() != 4:
+        raise TsltError("q must be [B, n, heads_q, D]")
+    _, n, heads_q, _ = q.shape
+    qr = _rows_of(q, "q", (B, n, heads_q, D), q.dtype)
+    if (k is None) != (v is None):
+        raise TsltError("k and v come together")
+    kr = None if k is None else _rows_of(k, "k", (B, n, heads, D), q.dtype)
+    vr = None if v is None else _rows_of(v, "v", (B, n, heads, D), q.dtype)
+    mask_ptr, mask_seq = None, 0
+    if mask is not None:
+        _dev(mask, torch.int32, "mask")
+        words = (n + 31) // 32
+        if mask.dim() != 3 or mask.shape[0] not in (1, B) or tuple(mask.shape[1:]) != (n, words):
+            raise TsltError(f"mask must be [B or 1, {n}, {words}], got {list(mask.shape)}")
+        mask_ptr, mask_seq = mask.data_ptr(), n * words if mask.shape[0] > 1 else 0
+    if out is None:
+        out = {"out": torch.empty(B, n, heads_q, D, dtype=q.dtype, device=q.device),
+               "lse": torch.empty(B, n, heads_q, dtype=torch.float32, device=q.device),
+               "status": torch.empty(B, dtype=torch.int32, device=q.device)}
+    ws = workspace if workspace is not None else _workspace(cache_attend_workspace_bytes(B, n, heads_q, heads, D, width), q.device)
+    _check(lib.tslt_cache_attend(c, pages.data_ptr(), width, length.data_ptr(), B, n, heads_q, qr, kr, vr, _dtype_code(q), mask_ptr, mask_seq,
+                                 _counted(count, "count", B), float(D ** -0.5 if scale is None else scale),
+                                 _sized(out, "out", q.dtype, B * n * heads_q * D), _sized(out, "lse", torch.float32, B * n * heads_q),
+                                 _sized(out, "status", torch.int32, B, optional=True), _ptr(ws), ws.numel() if ws is not None else 0, _stream()))
+    return out
+
+
+def cache_weigh(q: torch.Tensor, lse: torch.Tensor, cache: dict, pages: torch.Tensor, length: torch.Tensor, weight: torch.Tensor,
+                decay: float = 1.0, count: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[dict] = None) -> dict:
+    """tslt_cache_weigh: weight [B, heads, width * 64] times decay, and what cache_attend's rows q with its lse gave each cached token.
+    Returns weight (out may hold the same array) and status [B]."""
+    lib = load()
+    c, heads, D = _cache_of(cache)
+    B, width = _sequences(pages, length)
+    if q.dim() != 4:
+        raise TsltError("q must be [B, n, heads_q, D]")
+    _, n, heads_q, _ = q.shape
+    qr = _rows_of(q, "q", (B, n, heads_q, D), q.dtype)
+    _dev(lse, torch.float32, "lse"); _dev(weight, torch.float32, "weight")
+    if lse.numel() != B * n * heads_q or weight.numel() != B * heads * width * PAGE_TOKENS:
+        raise TsltError("cache_weigh: shapes do not agree")
+    if out is None:
+        out = {"weight": torch.empty_like(weight), "status": torch.empty(B, dtype=torch.int32, device=q.device)}
+    _check(lib.tslt_cache_weigh(c, pages.data_ptr(), width, length.data_ptr(), B, n, heads_q, qr, _dtype_code(q), lse.data_ptr(),
+                                _counted(count, "count", B), float(D ** -0.5 if scale is None else scale), weight.data_ptr(), float(decay),
+                                _sized(out, "weight", torch.float32, weight.numel()), _sized(out, "status", torch.int32, B, optional=True),
+                                _stream()))
+    return out
+
+
+def cache_evict(cache: dict, pages: torch.Tensor, length: torch.Tensor, weight: torch.Tensor, keep: int, recent: int,
+                new_pages: torch.Tensor, out: Optional[dict] = None) -> dict:
+    """tslt_cache_evict: of every head the `recent` last tokens and those of most weight, `keep` in all, copied to the pages
+    new_pages [B, new_width] of the same cache.  Returns length [B], kept [B, heads, keep], weight [B, heads, new_width * 64] and status [B]."""
+    lib = load()
+    c, heads, D = _cache_of(cache)
+    B, width = _sequences(pages, length)
+    _dev(weight, torch.float32, "weight"); _dev(new_pages, torch.int32, "new_pages")
+    if weight.numel() != B * heads * width * PAGE_TOKENS or new_pages.dim() != 2 or new_pages.shape[0] != B:
+        raise TsltError("cache_evict: shapes do not agree")
+    keep, new_width = int(keep), new_pages.shape[1]
+    if out is None:
+        out = {"length": torch.empty(B, dtype=torch.int32, device=weight.device),
+               "kept": torch.empty(B, heads, max(keep, 0), dtype=torch.int32, device=weight.device),
+               "weight": torch.empty(B, heads, new_width * PAGE_TOKENS, dtype=torch.float32, device=weight.device),
+               "status": torch.empty(B, dtype=torch.int32, device=weight.device)}
+    _check(lib.tslt_cache_evict(c, pages.data_ptr(), width, length.data_ptr(), B, weight.data_ptr(), keep, int(recent), new_pages.data_ptr(),
+                                new_width, _sized(out, "length", torch.int32, B), _sized(out, "kept", torch.int32, B * heads * max(keep, 0)),
+                                _sized(out, "weight", torch.float32, B * heads * new_width * PAGE_TOKENS),
+                                _sized(out, "status", torch.int32, B, optional=True), _stream()))
     return out
