@@ -444,7 +444,7 @@ int tslt_cache_append(const tslt_cache* cache, const int32_t* pages, int64_t wid
  *   out_lse     [B][n][heads_q] fp32: ln sum_j exp(scale * q_i . k_j)
  *   status      [B] int32; may be NULL
  * A row that sees nothing gives zeros and -inf.  What a row does not see has no part in it, whatever it holds, NaN and
- * infinities too.  A seen value that is not finite goes into the sum as it is; a query, or a seen key, that is not finite makes
+ * infinities too.  Seen values that are not finite make the sum what they add up to; a query, or a seen key, that is not finite makes
  * NaN of its rows, or whatever fp32's rules give.  Sums, maxima and the softmax are fp32, weights are rounded to 16 bits or more
  * before they meet the values (24 for fp32 rows).
  * Workspace: tslt_cache_attend_workspace_bytes of the same arguments, 256-byte aligned; it need not be cleared.  0 where none is needed. */

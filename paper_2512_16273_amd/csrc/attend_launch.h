@@ -4,24 +4,28 @@
 
 namespace tslt {
 
-template <typename T, int D, int RT, int KS> hipError_t launch_attend_shape(const AttendParams& p, hipStream_t s) {
-  constexpr auto fn = &attend_kernel<T, D, RT, KS>;
-  const int lds = attend_lds_bytes<T, D, RT, KS>(p.k.data != nullptr);
+template <auto Kernel> hipError_t launch_attend_kernel(const AttendParams& p, int threads, int lds, hipStream_t s) {
   if (lds > 48 * 1024) {
-    const hipError_t e = allow_dynamic_lds<fn>(160 * 1024 - 4096);
+    const hipError_t e = allow_dynamic_lds<Kernel>(160 * 1024 - 8192);
     if (e != hipSuccess) return e;
   }
   const int64_t units = p.B * p.c.heads * p.chunks;
-  hipLaunchKernelGGL(fn, dim3(unsigned((units + 7) / 8 * 8 * p.row_groups)), dim3(256), lds, s, p);
-  if (p.chunks > 1) {
-    const int64_t groups = (int64_t(p.n) * p.group + kJoinRows - 1) / kJoinRows;
-    hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3(unsigned(p.B * p.c.heads * groups)), dim3(256), 0, s, p);
-  }
+  hipLaunchKernelGGL(Kernel, dim3(unsigned((units + 7) / 8 * 8 * p.row_groups)), dim3(threads), lds, s, p);
   return hipSuccess;
 }
 template <typename T, int D> hipError_t launch_attend_rows(const AttendParams& p, hipStream_t s) {
-  if (attend_rows(int64_t(p.n) * p.group) == 16) return launch_attend_shape<T, D, 1, 4>(p, s);
-  return launch_attend_shape<T, D, 2, 1>(p, s);
+  constexpr int RT = AttendShapes<T, D>::kRT;
+  const bool fresh = p.k.data != nullptr;
+  switch (attend_choice(sizeof(T) == 4, D, int64_t(p.n) * p.group).kind) {
+    case kStreamOne: return launch_attend_kernel<&attend_stream_kernel<T, D, 1, 4>>(p, 256, stream_lds_bytes<T, D, 1, 4>(fresh), s);
+    case kStreamTall:
+      if constexpr (RT == 2) return launch_attend_kernel<&attend_stream_kernel<T, D, 2, 4>>(p, 256, stream_lds_bytes<T, D, 2, 4>(fresh), s);
+    case kStreamTwo: return launch_attend_kernel<&attend_stream_kernel<T, D, RT, 2>>(p, 256, stream_lds_bytes<T, D, RT, 2>(fresh), s);
+    case kRowsFour: return launch_attend_kernel<&attend_rows_kernel<T, D, RT, 4>>(p, 256, rows_lds_bytes<T, D>(fresh), s);
+    case kRowsEight:
+      if constexpr (RT == 1 && !(sizeof(T) == 4 && D == 256)) return launch_attend_kernel<&attend_rows_kernel<T, D, 1, 8>>(p, 512, rows_lds_bytes<T, D>(fresh), s);
+  }
+  return hipErrorInvalidValue;
 }
 template <typename T> hipError_t launch_attend(const AttendParams& p, int D, hipStream_t s) {
   return D == 64 ? launch_attend_rows<T, 64>(p, s) : D == 128 ? launch_attend_rows<T, 128>(p, s) : launch_attend_rows<T, 256>(p, s);

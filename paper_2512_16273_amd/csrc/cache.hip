@@ -67,18 +67,21 @@ template <typename T, int D> struct Weigh {
 };
 
 // How an attention call is cut: row groups, and chunks of a sequence's pages.
-void plan_attend(tslt::AttendParams& p) {
-  const int64_t rows = int64_t(p.n) * p.group, per = tslt::attend_rows(rows);
-  p.row_groups = int((rows + per - 1) / per);
-  const int64_t units = p.B * p.c.heads * p.row_groups, want = 8 * int64_t(tslt::compute_units());
-  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(want / units, (p.c.width + 3) / 4));
+void plan_attend(tslt::AttendParams& p, bool f32, int D) {
+  const int64_t rows = int64_t(p.n) * p.group;
+  const tslt::AttendChoice choice = tslt::attend_choice(f32, D, rows);
+  p.row_groups = int((rows + choice.rows - 1) / choice.rows);
+  const int64_t units = p.B * p.c.heads * p.row_groups, want = 4 * int64_t(tslt::compute_units());
+  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>({want / units, (p.c.width + 15) / 16, 256}));
   p.chunk = int((p.c.width + chunks - 1) / chunks);
   p.chunks = int((p.c.width + p.chunk - 1) / p.chunk);
 }
+// The workspace: a word for each chunk of each row group, then the chunks' parts.
+size_t attend_word_bytes(const tslt::AttendParams& p) { return (size_t(p.B) * p.c.heads * p.row_groups * p.chunks * 8 + 255) / 256 * 256; }
 size_t attend_part_bytes(const tslt::AttendParams& p, int D) {
   if (p.chunks == 1) return 0;
   const size_t rows = size_t(p.B) * p.c.heads * p.chunks * p.n * p.group;
-  return (rows * (D * 4 + 8) + 255) / 256 * 256;
+  return attend_word_bytes(p) + (rows * (D * 4 + 8) + 255) / 256 * 256;
 }
 
 }  // namespace
@@ -114,8 +117,12 @@ size_t tslt_cache_attend_workspace_bytes(int64_t B, int32_t n, int32_t heads_q, 
   if (head_dim != 64 && head_dim != 128 && head_dim != 256) return 0;
   tslt::AttendParams p{};
   p.B = B; p.n = n; p.group = heads_q / heads; p.c.heads = heads; p.c.width = width;
-  plan_attend(p);
-  return attend_part_bytes(p, head_dim);
+  size_t most = 0;
+  for (const bool f32 : {false, true}) {
+    plan_attend(p, f32, head_dim);
+    most = std::max(most, attend_part_bytes(p, head_dim));
+  }
+  return most;
 }
 
 int tslt_cache_attend(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
@@ -146,18 +153,18 @@ int tslt_cache_attend(const tslt_cache* cache, const int32_t* pages, int64_t wid
   p.mask = mask; p.mask_seq = mask_seq_stride; p.mask_words = (n + 31) / 32; p.count = count;
   p.scale2 = float(double(scale) * 1.4426950408889634074);
   p.out = out; p.lse = out_lse; p.status = status;
-  plan_attend(p);
+  plan_attend(p, dt == TSLT_F32, cache->head_dim);
   const size_t need = attend_part_bytes(p, cache->head_dim);
   if (need > 0) {
     if (!ws || !aligned(ws, 256) || ws_bytes < need)
       return fail(TSLT_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu are needed, 256-byte aligned", who, ws ? ws_bytes : size_t(0), need);
-    const size_t rows = size_t(B) * cache->heads * p.chunks * n * p.group;
-    p.part_o = reinterpret_cast<float*>(ws);
-    p.part_ml = reinterpret_cast<float2*>(p.part_o + rows * cache->head_dim);
+    p.words = reinterpret_cast<uint64_t*>(ws);
+    p.part_ml = p.words + attend_word_bytes(p) / 8;
+    p.part_o = p.part_ml + size_t(B) * cache->heads * p.chunks * n * p.group;
+    p.tag = tslt::next_tag();
   }
   int code;
   if (!grid_fits(who, (B * cache->heads * p.chunks + 8) * p.row_groups, code)) return code;
-  if (!grid_fits(who, B * cache->heads * ((int64_t(n) * p.group + tslt::kJoinRows - 1) / tslt::kJoinRows), code)) return code;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const hipError_t e = dt == TSLT_F32 ? tslt::launch_attend<float>(p, cache->head_dim, s)
                        : dt == TSLT_BF16 ? tslt::launch_attend<tslt::Bf16>(p, cache->head_dim, s) : tslt::launch_attend<tslt::F16>(p, cache->head_dim, s);

@@ -46,7 +46,7 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// All threads of a workgroup, one of `n` (64 at most) that share something: everything that any of its waves stored with
+// All threads of a workgroup, one of `n` that share something: everything that any of its waves stored with
 // store_through is at memory, it says so in words[i], and returns whether all the others have too.  `told` is a word of LDS.  What they
 // have left may be asked for then; which workgroup goes on with it claimed() says.
 __device__ __forceinline__ bool all_arrived(uint64_t* words, int i, int n, Tag tag, int& told) {
@@ -56,7 +56,8 @@ __device__ __forceinline__ bool all_arrived(uint64_t* words, int i, int n, Tag t
     const int lane = lane_id();
     if (lane == 0) store_through(&words[i], tag_word(tag));
     stores_arrived();
-    const bool missing = lane < n && load_through(&words[lane]) != tag_word(tag);
+    bool missing = false;
+    for (int k = lane; k < n; k += 64) missing |= load_through(&words[k]) != tag_word(tag);
     if (ballot(missing) != 0) { if (lane == 0) told = 0; }
     else if (lane == 0) told = 1;
   }
@@ -71,7 +72,9 @@ __device__ __forceinline__ bool claimed(uint64_t* words, int n, Tag tag) {
   bool mine = false;
   if (lane == 0) mine = __hip_atomic_compare_exchange_strong(&words[0], &word, 0ull, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   mine = ballot(mine) != 0;
-  if (mine && lane > 0 && lane < n) store_through(&words[lane], 0);
+  if (mine)
+    for (int k = lane; k < n; k += 64)
+      if (k > 0) store_through(&words[k], 0);
   return mine;
 }
 
