@@ -6,11 +6,9 @@
 // A row is one query head of one token; the rows of one sequence that share a key/value head, n * group of them, meet the same
 // keys, so the products are dense in tiles of 16 rows, and one pass keeps a running maximum m and sum l for each row.
 //
-// One wave takes 64 keys at a time against RT tiles of rows.  The scores come out with 16 keys of one row in each lane, which is how
-// the second product wants its weights, so nothing is exchanged between lanes on the way.  Two kernels:
+// One wave takes 64 keys at a time against tiles of 16 rows (see Tile), in two kernels:
 //   attend_stream_kernel, few rows: bound by memory.  Codes go from memory straight into the operand registers of the products (the
-//     order in which the cache holds them is made for that).  Of a workgroup's four waves KS take pages in turn and 4 / KS have
-//     rows of their own.
+//     order in which the cache holds them is made for that).  A workgroup's four waves have the same rows and take pages in turn.
 //   attend_rows_kernel, many rows: bound by the products and the exponentials.  A workgroup brings a page to LDS once, as operands, for
 //     all of its waves, each with rows of its own.
 // A sequence is cut into chunks of pages where its rows alone do not fill the GPU; whichever of its workgroups ends last joins them.
@@ -69,18 +67,14 @@ template <> __device__ __forceinline__ void store4<Bf16>(void* p, int64_t at, f3
   *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(p) + at) = bf16x4{__bf16(v[0]), __bf16(v[1]), __bf16(v[2]), __bf16(v[3])};
 }
 
-// New tokens' keys and values, a tile of 64 in LDS.  16 bytes of keys are kPer channels of one token: chunk of channels c, token
-// at place (token % 16) * 4 + token / 16 (the rows of one product next to each other), and that exclusive-or c % 16, so that neither
-// the lanes that write a token's channels nor those that read a channel of 16 tokens meet in a bank.  16 bytes of values are kPer
-// tokens of one channel.
-template <typename T, int D> struct Fresh {
+// 64 tokens in LDS.  16 bytes of keys are kPer channels of one token.  A chunk's tokens lie in the order in which the lanes of a product read them,
+// that exclusive-or a number of the chunk, so that of neither eight lanes that read a chunk of eight tokens nor eight that write eight chunks, or every
+// other of sixteen, of one token two meet in a bank.  16 bytes of values are kPer tokens of one channel.
+template <typename T, int D> struct Staged {
   static constexpr int kBytes = sizeof(T), kPer = 16 / kBytes;
   static constexpr int kKeyBytes = kPage * D * kBytes;
   static constexpr int kLds = 2 * kKeyBytes;
-  static __device__ __forceinline__ int key_at(int chunk, int token) {
-    const int place = (token & 15) * 4 + (token >> 4);
-    return (chunk * kPage + (place ^ (chunk & 15))) * 16;
-  }
+  static __device__ __forceinline__ int key_at(int chunk, int place) { return (chunk * kPage + (place ^ ((chunk & 7) ^ (chunk >> 3 & 1)))) * 16; }
   static __device__ __forceinline__ int value_at(int eight, int part, int d) { return kKeyBytes + ((eight * (8 / kPer) + part) * D + d) * 16; }
 };
 template <typename T> __device__ __forceinline__ bool not_finite(uint32_t bits);
@@ -102,7 +96,7 @@ struct FreshShared {
 // noted: a product would carry it to rows that do not see the token, as 0 times it (see add_odd_values).
 template <typename T, int D, int NT>
 __device__ __forceinline__ void stage_fresh(const AttendParams& p, int64_t b, int h, int j0, int there, uint8_t* lds, FreshShared& sh) {
-  typedef Fresh<T, D> F;
+  typedef Staged<T, D> F;
   const int tid = int(threadIdx.x);
   const T* kp = reinterpret_cast<const T*>(p.k.data) + b * p.k.seq + h * p.k.head;
   const T* vp = reinterpret_cast<const T*>(p.v.data) + b * p.v.seq + h * p.v.head;
@@ -112,7 +106,7 @@ __device__ __forceinline__ void stage_fresh(const AttendParams& p, int64_t b, in
     const int idx = it * NT + tid, chunk = idx % kChunks, token = idx / kChunks;
     u32x4 w = load16(kp + min(j0 + token, there - 1) * p.k.token + chunk * F::kPer);
     if (j0 + token >= there) w = u32x4{0, 0, 0, 0};
-    *reinterpret_cast<u32x4*>(lds + F::key_at(chunk, token)) = w;
+    *reinterpret_cast<u32x4*>(lds + F::key_at(chunk, Tile::place(token))) = w;
   }
   constexpr int kWide = F::kBytes == 4 ? 1 : 2;          // channels to a thread: a word
 #pragma unroll 2
@@ -149,13 +143,21 @@ __device__ __forceinline__ void stage_fresh(const AttendParams& p, int64_t b, in
   }
 }
 
-// What a wave keeps for its rows.  Lane l = 16 g + r: row r of each tile; of the sums, channels 16 t + 4 g .. + 3.
+// What a wave keeps for its rows: of row r of each tile the running maximum, the lane's part of the sum of weights, and of channels 16 d + 4 g .. + 3 the sums.
 template <int D, int RT> struct RowState {
   f32x4 o[RT][D / 16];
   float m[RT], l[RT];
 };
-
-// The running maximum follows where a row of the tile exceeds it by more than 2^kLag.
+template <int D, int RT> __device__ __forceinline__ void begin(RowState<D, RT>& st) {
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    st.m[rt] = kNoMax;
+    st.l[rt] = 0;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) st.o[rt][d] = f32x4{0, 0, 0, 0};
+  }
+}
+// The running maximum follows where a row of the tile exceeds it by more than kLag.
 template <int D, int RT> __device__ __forceinline__ void follow(RowState<D, RT>& st, int rt, float most) {
   if (ballot(most > st.m[rt] + kLag) == 0) return;
   const float m = over_groups_max(fmaxf(most, st.m[rt]));
@@ -165,6 +167,25 @@ template <int D, int RT> __device__ __forceinline__ void follow(RowState<D, RT>&
 #pragma unroll
   for (int d = 0; d < D / 16; ++d) st.o[rt][d] *= f;
 }
+__device__ __forceinline__ float most_of(const f32x4 (&s)[4]) {
+  float most = s[0][0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i >> 2][i & 3]);
+  return most;
+}
+// A page's scores without those of tokens from `there` on, which do not count, and the maximum.
+template <int D, int RT> __device__ __forceinline__ void page_maximum(f32x4 (&s)[RT][4], RowState<D, RT>& st, float c, int there, int g) {
+  if (there < kPage) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (g * 16 + i >= there) s[rt][i >> 2][i & 3] = -INFINITY;
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) follow(st, rt, most_of(s[rt]) * c);
+}
+
 // Of 16 bytes, one a token, those of the first `there` tokens: what lies behind them may be anything.
 __device__ __forceinline__ u32x4 tokens_below(int there) {
   u32x4 keep;
@@ -176,13 +197,13 @@ __device__ __forceinline__ u32x4 tokens_below(int there) {
   return keep;
 }
 
-// A wave's tile of values, 64 tokens: of each 16 channels lane 16 g + r has channel r of tokens 16 g .. + 15.
+// 64 tokens' values in a wave: of channel 16 d + r the lane's 16 tokens.
 template <int D> struct ValueTile {
   u32x4 w[D / 16];
   __device__ __forceinline__ void load(const uint8_t* values, int lane) {
     const uint8_t* p = values + (lane >> 4) * 16 * D + (lane & 15) * 16;
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) w[d] = load16(p + d * 256);
+    for (int d = 0; d < D / 16; ++d) w[d] = load16_once(p + d * 256);
   }
   __device__ __forceinline__ void cut(int there) {
     const u32x4 keep = tokens_below(there);
@@ -208,24 +229,63 @@ template <int N> __device__ __forceinline__ void split_weight(float x, int i, bf
   }
 }
 
-// Scores of a cached page into weights and their sum.  `there` of its 64 tokens count.
-template <typename T, int D, int RT>
-__device__ __forceinline__ void page_weights(f32x4 (&s)[RT][4], RowState<D, RT>& st, float c, int there, int g, bf16x8 (&w)[RT][2][Terms<T>::kW]) {
-  if (there < kPage) {
+// Vector instructions and matrix products stay in the order in which they are written down; memory's may move.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x3F4); }
+
+// A page's scores into weights, these and its values into the rows' sums, and beside that, the scores of the page after it, so that the products
+// run while the exponentials are made.  keys(t, i): operand of instruction t and step i of the next page; values(d, k): of this page's channels 16 d ..
+// and the k-th eight of the lane's 16 tokens; each is asked for kAhead operands before it is met.  The order is written out: a product, then a
+// weight or none.  (A product leaves room for two vector instructions beside it: measured, two waves to a SIMD, 18.2 cycles alone, 20.6 with
+// two, 23.9 with three, 30.6 with four.)
+template <int kAhead, typename T, int D, int RT, typename Keys, typename Values>
+__device__ __forceinline__ void page_round(const Queries<T, D, RT>& q, f32x4 (&s)[RT][4], RowState<D, RT>& st, float c, const Keys& keys, const Values& values) {
+  constexpr int kTerms = Operand<T>::kTerms, kW = Terms<T>::kW, kRing = kAhead + 1;
+  constexpr int kKeys = D / 32 * 4, kScores = kKeys * kTerms * RT;         // operands, and products with them
+  constexpr int kHalf = D / 16, kValues = kHalf * kW * RT;                 // the same of half a page's values
+  constexpr int kElements = 8 * RT;                                        // weights of half a page, a lane
+  static_assert(kElements <= kScores && kElements <= kValues, "a weight to a product at most");
+  f32x4 next[RT][4];
+  bf16x8 w[RT][2][kW];
+  const auto weight = [&](int k, int n) {
+    const int rt = n >> 3, e = n & 7;
+    const float x = exp2_fast(__builtin_fmaf(s[rt][2 * k + (e >> 2)][e & 3], c, -st.m[rt]));
+    st.l[rt] += x;
+    split_weight(x, e, w[rt][k]);
+  };
+  typename Operand<T>::Vec key[kRing];
+  bf16x8 value[kRing];
+  const auto ask = [&](int f) {
+    if (f < kKeys) key[f % kRing] = keys(f % 4, f / 4);
+    else if (f < kKeys + 2 * kHalf) value[(f - kKeys) % kRing] = values((f - kKeys) % kHalf, (f - kKeys) / kHalf);
+  };
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+  for (int f = 0; f < kAhead; ++f) ask(f);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (g * 16 + t * 4 + i >= there) s[rt][t][i] = -INFINITY;
+  for (int n = 0; n < kScores; ++n) {
+    const int rt = n % RT, e = n / RT % kTerms, f = n / (RT * kTerms), t = f % 4, i = f / 4;
+    if (n % (RT * kTerms) == 0) ask(f + kAhead);
+    next[rt][t] = mfma(key[f % kRing], q.v[rt][i][e], i == 0 && e == 0 ? f32x4{0, 0, 0, 0} : next[rt][t]);
+    if ((n + 1) * kElements / kScores > n * kElements / kScores) weight(0, n * kElements / kScores);
+    keep_order();
   }
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    float most = s[rt][0][0];
+  for (int n = 0; n < 2 * kValues; ++n) {
+    const int k = n / kValues, rt = n % RT, e = n / RT % kW, f = n / (RT * kW), d = f % kHalf;
+    if (n % (RT * kW) == 0) ask(kKeys + f + kAhead);
+    st.o[rt][d] = mfma(value[f % kRing], w[rt][k][e], st.o[rt][d]);
+    if (k == 0 && (n + 1) * kElements / kValues > n * kElements / kValues) weight(1, n * kElements / kValues);
+    keep_order();
+  }
 #pragma unroll
-    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[rt][i >> 2][i & 3]);
-    follow(st, rt, most * c);
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[rt][t] = next[rt][t];
+}
+// The same for the kernel whose waves read operands of their own: a page's weights, then its values.
+template <typename T, int D, int RT>
+__device__ __forceinline__ void page_weights(const f32x4 (&s)[RT][4], RowState<D, RT>& st, float c, bf16x8 (&w)[RT][2][Terms<T>::kW]) {
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
     float sum = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -236,9 +296,8 @@ __device__ __forceinline__ void page_weights(f32x4 (&s)[RT][4], RowState<D, RT>&
     st.l[rt] += sum;
   }
 }
-
-template <int D, int RT, int N>
-__device__ __forceinline__ void page_values(const ValueTile<D>& v, const bf16x8 (&w)[RT][2][N], RowState<D, RT>& st, float scale) {
+template <int D, int RT, int W>
+__device__ __forceinline__ void page_values(const ValueTile<D>& v, const bf16x8 (&w)[RT][2][W], RowState<D, RT>& st, float scale) {
 #pragma unroll
   for (int d = 0; d < D / 16; ++d)
 #pragma unroll
@@ -247,7 +306,7 @@ __device__ __forceinline__ void page_values(const ValueTile<D>& v, const bf16x8 
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int e = 0; e < N; ++e) st.o[rt][d] = mfma(a, w[rt][k][e], st.o[rt][d]);
+        for (int e = 0; e < W; ++e) st.o[rt][d] = mfma(a, w[rt][k][e], st.o[rt][d]);
     }
 }
 
@@ -269,43 +328,42 @@ __device__ __forceinline__ uint32_t seen_of(const AttendParams& p, const uint32_
   return there - at < 16 ? bits & ((1u << (there - at)) - 1) : bits;
 }
 
-// The call's own tokens, all of them that the wave's rows see, tile after tile; the waves of a workgroup that share rows take turns.
-template <typename T, int D, int RT, int KS, int NT>
-__device__ __forceinline__ void attend_fresh(const AttendParams& p, int64_t b, int h, int first_row, int last_row, int there, int wave_k,
+// The call's own tokens, all of them that the wave's rows see, tile after tile; `turns` waves that share rows take turns.
+template <typename T, int D, int RT, int NT>
+__device__ __forceinline__ void attend_fresh(const AttendParams& p, int64_t b, int h, int first_row, int last_row, int there, int turns, int my_turn,
                                              const Queries<T, D, RT>& q, RowState<D, RT>& st, uint8_t* lds, FreshShared& sh) {
-  typedef Fresh<T, D> F;
+  typedef Staged<T, D> F;
   typedef Terms<T> W;
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
   const uint32_t* mask = p.mask ? p.mask + b * p.mask_seq : nullptr;
   // (a token sees none behind itself where there is no mask: tiles behind the workgroup's last row's token are not looked at)
   const int reach = mask ? there : min(there, last_row / p.group + 1);
   for (int j0 = 0, turn = 0; j0 < reach; j0 += kPage, ++turn) {
-    uint32_t seen[RT];
-    bool any = false;
+    uint32_t seen[RT];                     // (a bit to each of the lane's scores)
+    bool mine = false;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       seen[rt] = seen_of(p, mask, (first_row + rt * 16 + r) / p.group, j0 + g * 16, there);
-      any |= seen[rt] != 0;
+      mine |= seen[rt] != 0;
     }
-    const bool wanted = ballot(any) != 0 && turn % KS == wave_k;
-    if (ballot(any) != 0 && lane == 0) sh.wanted[turn & 1] = turn + 1;
+    const bool any = ballot(mine) != 0;
+    if (any && lane == 0) sh.wanted[turn & 1] = turn + 1;
     __syncthreads();                       // (also: what was staged before has been read)
     if (sh.wanted[turn & 1] != turn + 1) continue;
     stage_fresh<T, D, NT>(p, b, h, j0, there, lds, sh);
     __syncthreads();
-    if (!wanted) continue;
+    if (!any || turn % turns != my_turn) continue;
     f32x4 s[RT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) s[rt][t] = f32x4{0, 0, 0, 0};
-      const int token = (r >> 2) * 16 + t * 4 + (r & 3);
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
-        const int chunk = step_channel(i, g) / F::kPer;
+        const int chunk = Tile::channel(i, g) / F::kPer, place = t * 16 + r;
         typename Operand<T>::Vec a[Operand<T>::kTerms];
-        const u32x4 x = *reinterpret_cast<const u32x4*>(lds + F::key_at(chunk, token));
-        if constexpr (sizeof(T) == 4) Operand<float>::split(x, *reinterpret_cast<const u32x4*>(lds + F::key_at(chunk + 1, token)), a);
+        const u32x4 x = *reinterpret_cast<const u32x4*>(lds + F::key_at(chunk, place));
+        if constexpr (sizeof(T) == 4) Operand<float>::split(x, *reinterpret_cast<const u32x4*>(lds + F::key_at(chunk + 1, place)), a);
         else a[0] = __builtin_bit_cast(typename Operand<T>::Vec, x);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -316,25 +374,14 @@ __device__ __forceinline__ void attend_fresh(const AttendParams& p, int64_t b, i
         if constexpr (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0);       // (the terms of one step in registers, not of several)
       }
     }
-    bf16x8 w[RT][2][W::kW];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float most = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[rt][i >> 2][i & 3] = (seen[rt] >> i & 1) ? s[rt][i >> 2][i & 3] * p.scale2 : -INFINITY;
-        most = fmaxf(most, s[rt][i >> 2][i & 3]);
-      }
-      follow(st, rt, most);
-      float sum = 0;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = exp2_fast(s[rt][i >> 2][i & 3] - st.m[rt]);
-        sum += x;
-        split_weight(x, i & 7, w[rt][i >> 3]);
-      }
-      st.l[rt] += sum;
+      for (int i = 0; i < 16; ++i) s[rt][i >> 2][i & 3] = (seen[rt] >> i & 1) ? s[rt][i >> 2][i & 3] * p.scale2 : -INFINITY;
+      follow(st, rt, most_of(s[rt]));
     }
+    bf16x8 w[RT][2][W::kW];
+    page_weights<T, D, RT>(s, st, 1.0f, w);
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
 #pragma unroll
@@ -362,40 +409,30 @@ struct Place {
   bool bad_length;
 };
 // False: there is nothing to do.  Workgroups go to the eight XCDs in turn; those that differ in their rows alone read the same pages: on one
-// XCD, one after the other.
+// XCD, one after the other, those of the last rows first, which see most of the new tokens.  A sequence's last chunk, which has the new tokens, comes first.
 __device__ __forceinline__ bool place_of(const AttendParams& p, Place& at) {
   const uint32_t block = blockIdx.x, slot = block >> 3;
-  const uint32_t unit = slot / uint32_t(p.row_groups) * 8 + (block & 7);
-  if (unit >= uint64_t(p.B) * p.c.heads * p.chunks) return false;
-  at.rg = int(slot % uint32_t(p.row_groups));
-  at.chunk = int(unit % uint32_t(p.chunks));
-  at.h = int(unit / uint32_t(p.chunks) % uint32_t(p.c.heads));
-  at.b = int64_t(unit / (uint32_t(p.chunks) * uint32_t(p.c.heads)));
+  const uint32_t unit = slot / uint32_t(p.row_groups) * 8 + (block & 7), heads = uint32_t(p.B * p.c.heads);
+  if (unit >= uint64_t(heads) * p.chunks) return false;
+  at.rg = p.row_groups - 1 - int(slot % uint32_t(p.row_groups));
+  at.h = int(unit % heads % uint32_t(p.c.heads));
+  at.b = int64_t(unit % heads / uint32_t(p.c.heads));
   at.len = cached_tokens(p.c, at.b, at.bad_length);
   at.n_pages = (at.len + kPage - 1) / kPage;
   at.active = max(1, (at.n_pages + p.chunk - 1) / p.chunk);
   at.there = p.count ? min(max(as_global(p.count)[at.b], 0), p.n) : p.n;
   at.rows = p.n * p.group;
-  return at.chunk < at.active;
+  at.chunk = at.active - 1 - int(unit / heads);
+  return at.chunk >= 0;
 }
-template <typename T, int D, int RT>
-__device__ __forceinline__ void load_queries(const AttendParams& p, const Place& at, int first_row, Queries<T, D, RT>& q) {
+template <typename T, int D, int RT> __device__ __forceinline__ void load_queries(const AttendParams& p, const Place& at, int first_row, Queries<T, D, RT>& q) {
   const int r = lane_id() & 15, g = lane_id() >> 4;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int row = min(first_row + rt * 16 + r, at.rows - 1);
     const int64_t from = at.b * p.q.seq + int64_t(row / p.group) * p.q.token + int64_t(at.h * p.group + row % p.group) * p.q.head;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) Operand<T>::load(p.q.data, from + step_channel(i, g), q.v[rt][i]);
-  }
-}
-template <int D, int RT> __device__ __forceinline__ void begin(RowState<D, RT>& st) {
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    st.m[rt] = kNoMax;
-    st.l[rt] = 0;
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) st.o[rt][d] = f32x4{0, 0, 0, 0};
+    for (int i = 0; i < D / 32; ++i) Operand<T>::load(p.q.data, from + Tile::channel(i, g), q.v[rt][i]);
   }
 }
 // Up to 64 entries of a sequence's table with the scales of their pages, one a lane: entries first, first + step, ...
@@ -531,30 +568,32 @@ __device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, boo
   }
 }
 
-template <typename T, int D, int RT, int KS> constexpr int stream_lds_bytes(bool fresh) {
-  const int join = KS == 1 ? 0 : KS * 16 * RT * (4 / KS) * (D + 4) * 4, staged = fresh ? Fresh<T, D>::kLds : 0;
+constexpr int kStreamTurns = 4;            // waves of a workgroup that take pages in turn
+// Most tiles of 16 rows that a wave has registers for with two waves to a SIMD (one for D = 256).
+template <typename T, int D> constexpr int stream_most_tiles() { return D == 64 || (D == 128 && sizeof(T) == 2) ? 2 : 1; }
+template <typename T, int D, int RT> constexpr int stream_lds_bytes(bool fresh) {
+  const int join = kStreamTurns * 16 * RT * (D + 4) * 4, staged = fresh ? Staged<T, D>::kLds : 0;
   return join > staged ? join : staged;
 }
 
-// Few rows.  KS of a workgroup's four waves share rows and take turns at the pages, 4 / KS have rows of their own.
-template <typename T, int D, int RT, int KS>
+// Few rows.
+template <typename T, int D, int RT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(const AttendParams p) {
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ FreshShared sh;
-  __shared__ float2 join_ml[KS][4 / KS * 16 * RT];
+  __shared__ float2 join_ml[kStreamTurns][16 * RT];
   __shared__ int told;
-  constexpr int RS = 4 / KS, kRows = RS * 16 * RT;
+  constexpr int KS = kStreamTurns, kRows = 16 * RT;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, g = lane >> 4, tid = int(threadIdx.x);
-  const int wave_k = wave % KS, wave_r = wave / KS;
   Place at;
   if (!place_of(p, at)) return;
-  const int first_row = at.rg * kRows + wave_r * 16 * RT;
+  const int first_row = at.rg * kRows;
   Queries<T, D, RT> q;
-  load_queries<T, D, RT>(p, at, first_row, q);
+  load_queries(p, at, first_row, q);
   RowState<D, RT> st;
   begin(st);
 
-  const int from = at.chunk * p.chunk + wave_k, to = min((at.chunk + 1) * p.chunk, at.n_pages);
+  const int from = at.chunk * p.chunk + wave, to = min((at.chunk + 1) * p.chunk, at.n_pages);
   const int turns = from < to ? (to - from + KS - 1) / KS : 0;
   bool bad = at.bad_length;
   for (int base = 0; base < turns; base += 64) {
@@ -569,11 +608,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(co
     for (int i = 0; i < some; ++i) {
       const int valid = list.page_at(i) < 0 ? 0 : min(kPage, at.len - (from + KS * (base + i)) * kPage);
       f32x4 s[RT][4];
-      key_products<T, D, RT>(kt, q, s);
+      key_products(kt, q, s);
       const uint8_t* next = page_codes(p.c, max(0, list.page_at(min(i + 1, some - 1))), at.h, D);
       if (i + 1 < some) kt.load(next, lane);
+      const float c = p.scale2 * list.k_at(i);
+      page_maximum(s, st, c, valid, g);
       bf16x8 w[RT][2][Terms<T>::kW];
-      page_weights<T, D, RT>(s, st, p.scale2 * list.k_at(i), valid, g, w);
+      page_weights<T, D, RT>(s, st, c, w);
       if (valid < kPage) vt.cut(valid - g * 16);
       page_values(vt, w, st, list.v_at(i));
       if (i + 1 < some) vt.load(next + kPage * D, lane);
@@ -583,70 +624,58 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(co
   if (fresh) {
     if (tid == 0) sh.wanted[0] = sh.wanted[1] = sh.odd = 0;
     __syncthreads();
-    attend_fresh<T, D, RT, KS, 256>(p, at.b, at.h, first_row, min(at.rows, (at.rg + 1) * kRows) - 1, at.there, wave_k, q, st, lds, sh);
+    attend_fresh<T, D, RT, 256>(p, at.b, at.h, first_row, min(at.rows, first_row + kRows) - 1, at.there, KS, wave, q, st, lds, sh);
   }
 
-  // Lane 16 g + r has its row's maximum, its group's part of the sum of weights, and its channels.
-  if constexpr (KS == 1) {
+  // The waves' parts meet in LDS.
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int row = first_row + rt * 16 + r;
-      const float l = over_groups_sum(st.l[rt]);
-      if (row >= at.rows) continue;
+  for (int rt = 0; rt < RT; ++rt) {
+    const float l = over_groups_sum(st.l[rt]);
+    if (g == 0) join_ml[wave][rt * 16 + r] = make_float2(st.m[rt], l);
+  }
+  __syncthreads();                         // (also: what was staged of new tokens has been read)
+  float* sums = reinterpret_cast<float*>(lds);
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) give<T, D>(p, at, row, d * 16 + g * 4, st.m[rt], l, st.o[rt][d]);
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = rt * 16 + r;
+    float m = st.m[rt];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) m = fmaxf(m, join_ml[k][row].x);
+    const float f = exp2_fast(st.m[rt] - m);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(sums + (wave * kRows + row) * (D + 4) + d * 16 + g * 4) = st.o[rt][d] * f;
+  }
+  __syncthreads();
+  for (int idx = tid; idx < kRows * (D / 4); idx += 256) {
+    const int local = idx / (D / 4), d = idx % (D / 4) * 4, row = first_row + local;
+    if (row >= at.rows) break;
+    float m = kNoMax, l = 0;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) m = fmaxf(m, join_ml[k][local].x);
+    f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      l += join_ml[k][local].y * exp2_fast(join_ml[k][local].x - m);
+      o += *reinterpret_cast<const f32x4*>(sums + (k * kRows + local) * (D + 4) + d);
     }
-  } else {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const float l = over_groups_sum(st.l[rt]);
-      if (g == 0) join_ml[wave_k][wave_r * 16 * RT + rt * 16 + r] = make_float2(st.m[rt], l);
-    }
-    __syncthreads();                       // (also: what was staged of new tokens has been read)
-    float* sums = reinterpret_cast<float*>(lds);
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int row = wave_r * 16 * RT + rt * 16 + r;
-      float m = st.m[rt];
-#pragma unroll
-      for (int k = 0; k < KS; ++k) m = fmaxf(m, join_ml[k][row].x);
-      const float f = exp2_fast(st.m[rt] - m);
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(sums + (wave_k * kRows + row) * (D + 4) + d * 16 + g * 4) = st.o[rt][d] * f;
-    }
-    __syncthreads();
-    for (int idx = tid; idx < kRows * (D / 4); idx += 256) {
-      const int local = idx / (D / 4), d = idx % (D / 4) * 4, row = at.rg * kRows + local;
-      if (row >= at.rows) break;
-      float m = kNoMax, l = 0;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) m = fmaxf(m, join_ml[k][local].x);
-      f32x4 o = {0, 0, 0, 0};
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        l += join_ml[k][local].y * exp2_fast(join_ml[k][local].x - m);
-        o += *reinterpret_cast<const f32x4*>(sums + (k * kRows + local) * (D + 4) + d);
-      }
-      give<T, D>(p, at, row, d, m, l, o);
-    }
+    give<T, D>(p, at, row, d, m, l, o);
   }
   if (fresh && sh.odd) add_odd_values<T, D, 256, kRows>(p, at);
   join_chunks<T, D, 256, kRows>(p, at, bad, told);
 }
 
-// A page as operands in LDS: 16 bits a number, in the order of Fresh.  Bytes of one of the two that take turns.
+// A page as operands in LDS: 16 bits a number.  Bytes of one of the two that take turns.
 template <int D> constexpr int page_lds_bytes() { return 2 * kPage * D * 2; }
 template <typename T, int D> constexpr int rows_lds_bytes(bool fresh) {
-  return 2 * page_lds_bytes<D>() > (fresh ? Fresh<T, D>::kLds : 0) ? 2 * page_lds_bytes<D>() : Fresh<T, D>::kLds;
+  return 2 * page_lds_bytes<D>() > (fresh ? Staged<T, D>::kLds : 0) ? 2 * page_lds_bytes<D>() : Staged<T, D>::kLds;
 }
-
-// Many rows: NW waves with RT tiles of rows each.
-template <typename T, int D, int RT, int NW>
+// Many rows: NW waves with RT tiles of rows each; kDeep pages on their way from memory, kAhead operands from LDS.
+template <typename T, int D, int RT, int NW, int kDeep, int kAhead>
 __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_rows_kernel(const AttendParams p) {
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ FreshShared sh;
   __shared__ int told;
-  typedef Fresh<Bf16, D> F;                // (places in a tile of 16 bits)
+  typedef Staged<Bf16, D> F;               // (places in a tile of 16 bits)
   constexpr int NT = NW * 64, kRows = NW * 16 * RT, kLoads = kPage * D / 16 / NT;
   static_assert(kPage * D / 16 % NT == 0, "every thread has as many pieces of a page");
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, g = lane >> 4, tid = int(threadIdx.x);
@@ -654,7 +683,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_r
   if (!place_of(p, at)) return;
   const int first_row = at.rg * kRows + wave * 16 * RT;
   Queries<T, D, RT> q;
-  load_queries<T, D, RT>(p, at, first_row, q);
+  load_queries(p, at, first_row, q);
   RowState<D, RT> st;
   begin(st);
 
@@ -665,73 +694,88 @@ __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_r
     const int some = min(64, turns - base);
     PageList list;
     bad |= list.load(p, at, from + base, 1, some);
-    u32x4 kw[kLoads], vw[kLoads];
-    const uint8_t* codes = page_codes(p.c, max(0, list.page_at(0)), at.h, D);
+    // While page i's weights are made and meet its values, the scores of page i + 1 are: the products run beside the exponentials.  So
+    // in LDS keys are a page ahead of values; in registers, on the way from memory, both are kDeep further.
+    u32x4 kw[kDeep][kLoads], vw[kDeep][kLoads];
+    const auto fetch = [&](u32x4 (&w)[kLoads], int i, int part) {
+      const uint8_t* codes = page_codes(p.c, max(0, list.page_at(min(i, some - 1))), at.h, D) + part * kPage * D;
 #pragma unroll
-    for (int it = 0; it < kLoads; ++it) {
-      kw[it] = load16(codes + (it * NT + tid) * 16);
-      vw[it] = load16(codes + kPage * D + (it * NT + tid) * 16);
-    }
-    for (int i = 0; i < some; ++i) {
-      const int valid = list.page_at(i) < 0 ? 0 : min(kPage, at.len - (from + base + i) * kPage);
+      for (int it = 0; it < kLoads; ++it) w[it] = load16(codes + (it * NT + tid) * 16);
+    };
+    const auto valid_of = [&](int i) { return list.page_at(i) < 0 ? 0 : min(kPage, at.len - (from + base + i) * kPage); };
+    const auto put_keys = [&](const u32x4 (&w)[kLoads], int i) {
       uint8_t* tile = lds + (i & 1) * page_lds_bytes<D>();
-      const float v_scale = list.v_at(i);
 #pragma unroll
       for (int it = 0; it < kLoads; ++it) {
-        const int idx = it * NT + tid, key = idx / (D / 16), chunk = idx % (D / 16) * 2;
-        *reinterpret_cast<u32x4*>(tile + F::key_at(chunk, key)) = __builtin_bit_cast(u32x4, Operand<T>::codes(kw[it][0], kw[it][1]));
-        *reinterpret_cast<u32x4*>(tile + F::key_at(chunk + 1, key)) = __builtin_bit_cast(u32x4, Operand<T>::codes(kw[it][2], kw[it][3]));
-        const int d = idx % D, eight = idx / D * 2;
-        if (valid < kPage) vw[it] &= tokens_below(valid - eight * 8);
-        *reinterpret_cast<u32x4*>(tile + F::value_at(eight, 0, d)) = __builtin_bit_cast(u32x4, codes_as_bf16(vw[it][0], vw[it][1], v_scale));
-        *reinterpret_cast<u32x4*>(tile + F::value_at(eight + 1, 0, d)) = __builtin_bit_cast(u32x4, codes_as_bf16(vw[it][2], vw[it][3], v_scale));
+        const int idx = it * NT + tid, place = Tile::place(idx / (D / 16)), chunk = idx % (D / 16) * 2;
+        *reinterpret_cast<u32x4*>(tile + F::key_at(chunk, place)) = __builtin_bit_cast(u32x4, Operand<T>::codes(w[it][0], w[it][1]));
+        *reinterpret_cast<u32x4*>(tile + F::key_at(chunk + 1, place)) = __builtin_bit_cast(u32x4, Operand<T>::codes(w[it][2], w[it][3]));
       }
-      if (i + 1 < some) {
-        const uint8_t* next = page_codes(p.c, max(0, list.page_at(i + 1)), at.h, D);
+    };
+    const auto put_values = [&](u32x4 (&w)[kLoads], int i) {
+      uint8_t* tile = lds + (i & 1) * page_lds_bytes<D>();
+      const float v_scale = list.v_at(i);
+      const int valid = valid_of(i);
 #pragma unroll
-        for (int it = 0; it < kLoads; ++it) {
-          kw[it] = load16(next + (it * NT + tid) * 16);
-          vw[it] = load16(next + kPage * D + (it * NT + tid) * 16);
-        }
+      for (int it = 0; it < kLoads; ++it) {
+        const int idx = it * NT + tid, d = idx % D, eight = idx / D * 2;
+        if (valid < kPage) w[it] &= tokens_below(valid - eight * 8);
+        *reinterpret_cast<u32x4*>(tile + F::value_at(eight, 0, d)) = __builtin_bit_cast(u32x4, codes_as_bf16(w[it][0], w[it][1], v_scale));
+        *reinterpret_cast<u32x4*>(tile + F::value_at(eight + 1, 0, d)) = __builtin_bit_cast(u32x4, codes_as_bf16(w[it][2], w[it][3], v_scale));
       }
-      // (one barrier a page: whoever writes a tile again has passed the barrier that all reach after reading it)
-      __syncthreads();
-      if (first_row >= at.rows) continue;
-      f32x4 s[RT][4];
+    };
+    const auto key_operand = [&](const uint8_t* tile, int t, int i) {
+      return __builtin_bit_cast(typename Operand<T>::Vec, *reinterpret_cast<const u32x4*>(tile + F::key_at(Tile::channel(i, g) / 8, t * 16 + r)));
+    };
+    f32x4 s[RT][4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][t] = f32x4{0, 0, 0, 0};
-        const int token = (r >> 2) * 16 + t * 4 + (r & 3);
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-          const auto a = __builtin_bit_cast(typename Operand<T>::Vec, *reinterpret_cast<const u32x4*>(tile + F::key_at(step_channel(j, g) / 8, token)));
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int e = 0; e < Operand<T>::kTerms; ++e) s[rt][t] = mfma(a, q.v[rt][j][e], s[rt][t]);
-        }
-      }
-      bf16x8 w[RT][2][Terms<T>::kW];
-      page_weights<T, D, RT>(s, st, p.scale2 * list.k_at(i), valid, g, w);
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const auto a = *reinterpret_cast<const bf16x8*>(tile + F::value_at(g * 2 + k, 0, d * 16 + r));
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int e = 0; e < Terms<T>::kW; ++e) st.o[rt][d] = mfma(a, w[rt][k][e], st.o[rt][d]);
-        }
+    for (int u = 0; u < kDeep; ++u) {
+      fetch(kw[u], u, 0);
+      fetch(vw[u], u, 1);
     }
-    __syncthreads();                       // (the next list's first page, or a tile of new tokens, goes where this one's last ones are)
+    put_keys(kw[0], 0);
+    put_values(vw[0], 0);
+    fetch(kw[0], kDeep, 0);
+    fetch(vw[0], kDeep, 1);
+    if (some > 1) put_keys(kw[1 % kDeep], 1);
+    fetch(kw[1 % kDeep], kDeep + 1, 0);
+    __syncthreads();
+    if (first_row < at.rows) {
+#pragma unroll
+      for (int f = 0; f < D / 32 * 4; ++f) {
+        const auto a = key_operand(lds, f % 4, f / 4);
+#pragma unroll
+        for (int e = 0; e < Operand<T>::kTerms; ++e)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) s[rt][f % 4] = mfma(a, q.v[rt][f / 4][e], f < 4 && e == 0 ? f32x4{0, 0, 0, 0} : s[rt][f % 4]);
+      }
+    }
+    __syncthreads();                       // (the first page's keys have been read: the third's go there)
+    for (int i0 = 0; i0 < some; i0 += kDeep)
+#pragma unroll
+      for (int u = 0; u < kDeep; ++u) {
+        const int i = i0 + u;
+        if (i >= some) break;
+        if (first_row < at.rows) {
+          const float c = p.scale2 * list.k_at(i);
+          page_maximum(s, st, c, valid_of(i), g);
+          const uint8_t *tile = lds + (i & 1) * page_lds_bytes<D>(), *next_tile = lds + ((i + 1) & 1) * page_lds_bytes<D>();
+          // (behind the last page: scores of what lies there, which are not used)
+          page_round<kAhead>(q, s, st, c, [&](int t, int i) { return key_operand(next_tile, t, i); },
+                             [&](int d, int k) { return *reinterpret_cast<const bf16x8*>(tile + F::value_at(g * 2 + k, 0, d * 16 + r)); });
+        }
+        if (i + 1 < some) put_values(vw[(u + 1) % kDeep], i + 1);
+        if (i + 2 < some) put_keys(kw[(u + 2) % kDeep], i + 2);
+        fetch(vw[(u + 1) % kDeep], i + 1 + kDeep, 1);
+        fetch(kw[(u + 2) % kDeep], i + 2 + kDeep, 0);
+        __syncthreads();                   // (of this page's tiles all is read, of the next one's all is written)
+      }
   }
   const bool fresh = at.chunk == at.active - 1 && p.k.data && at.there > 0;
   if (fresh) {
     if (tid == 0) sh.wanted[0] = sh.wanted[1] = sh.odd = 0;
     __syncthreads();
-    attend_fresh<T, D, RT, 1, NT>(p, at.b, at.h, first_row, min(at.rows, (at.rg + 1) * kRows) - 1, at.there, 0, q, st, lds, sh);
+    attend_fresh<T, D, RT, NT>(p, at.b, at.h, first_row, min(at.rows, (at.rg + 1) * kRows) - 1, at.there, 1, 0, q, st, lds, sh);
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -745,20 +789,20 @@ __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_r
   join_chunks<T, D, NT, kRows>(p, at, bad, told);
 }
 
-// The shapes of a type and head size: tiles of rows to a wave, so that nothing spills (two waves to a SIMD: 256 registers).
-template <typename T, int D> struct AttendShapes { static constexpr int kRT = D == 64 || (sizeof(T) == 2 && D == 128) ? 2 : 1; };
+// Tiles of rows to a wave of the kernel for many rows, so that two waves to a SIMD have registers enough (one for fp32 and D = 256).
+template <typename T, int D> constexpr int rows_tiles() { return D == 64 || (D == 128 && sizeof(T) == 2) ? 2 : 1; }
 // The launches, for each type of the call in a source file of its own (attend_launch.h, attend_*.hip).
 template <typename T> hipError_t launch_attend(const AttendParams& p, int D, hipStream_t s);
-// Which kernel `rows` that share a head go to, and the rows that one workgroup takes.
-enum AttendKind { kStreamOne, kStreamTall, kStreamTwo, kRowsFour, kRowsEight };
-struct AttendChoice { AttendKind kind; int rows; };
+
+// Which kernel `rows` that share a head go to (stream: the one for few), and the rows that one workgroup takes.
+struct AttendChoice { bool stream; int rows; };
+template <typename T, int D> constexpr AttendChoice attend_choice_of(int64_t rows) {
+  if (rows <= 16 * stream_most_tiles<T, D>()) return {true, rows <= 16 ? 16 : 32};
+  return {false, rows <= 64 || (sizeof(T) == 4 && D == 256) ? 64 : 128};
+}
 inline AttendChoice attend_choice(bool f32, int D, int64_t rows) {
-  const bool tall = D == 64 || (!f32 && D == 128);      // two tiles of rows to a wave
-  if (rows <= 16) return {kStreamOne, 16};
-  if (tall && rows <= 32) return {kStreamTall, 32};
-  if (rows <= (tall ? 64 : 32)) return {kStreamTwo, tall ? 64 : 32};
-  if (tall) return {kRowsFour, 128};
-  return rows <= 64 || (f32 && D == 256) ? AttendChoice{kRowsFour, 64} : AttendChoice{kRowsEight, 128};
+  if (f32) return D == 64 ? attend_choice_of<float, 64>(rows) : D == 128 ? attend_choice_of<float, 128>(rows) : attend_choice_of<float, 256>(rows);
+  return D == 64 ? attend_choice_of<F16, 64>(rows) : D == 128 ? attend_choice_of<F16, 128>(rows) : attend_choice_of<F16, 256>(rows);
 }
 
 }  // namespace tslt

@@ -1,7 +1,7 @@
 // The 8-bit key/value cache of include/tslt.h: its layout, and what the kernels that read it share.
 //
 // A page holds 64 tokens.  For each head its keys lie [64 tokens][D] and its values [4][D][16 tokens], both e4m3, one byte a
-// number, with one scale each.  Both orders are those in which the matrix instructions of attend.h take them, 16 bytes a lane
+// number, with one scale each.  Both orders are those in which the matrix instructions of the kernels take them, 16 bytes a lane
 // straight from memory into the registers of an operand, no transpose and no LDS between; 16 tokens of values together, not
 // 64, so that a token that is appended or moved touches 2 KB of a page's values (D = 128) and not all 8 KB.
 //
@@ -54,6 +54,9 @@ __device__ __forceinline__ const uint8_t* page_codes(const CacheView& c, int64_t
 }
 
 __device__ __forceinline__ u32x4 load16(const void* p) { return *as_global(reinterpret_cast<const u32x4*>(p)); }
+
+// The same of what no other workgroup reads: it need not stay in a cache (4 x 131000 tokens 167 us so, 185 without).
+__device__ __forceinline__ u32x4 load16_once(const void* p) { return __builtin_nontemporal_load(as_global(reinterpret_cast<const u32x4*>(p))); }
 
 // Eight codes (two words) as an operand of a 16-bit matrix product: exact, as e4m3 has four significant bits and reaches from
 // 2^-9 to 448; times a power of two in bfloat16, which reaches as far as fp32.
@@ -117,38 +120,49 @@ template <> struct Operand<float> {
   }
 };
 
-// A wave's tile of one head's keys, 64 tokens.  Lane l = 16 g + r holds, of the four products of 16 tokens that make the
-// tile, row r: token 16 (r / 4) + 4 t + r % 4 in product t, and of its channels the 16 from 64 j + 16 g on, for each j.  With the
-// tokens dealt out so, what a lane gets of a product's result, rows 4 g .. 4 g + 3, are tokens 16 g + 4 t .. + 3: over the four
-// products 16 tokens in a row, those whose values it reads as 16 bytes of the other operand.
+// How the lanes of a wave share 64 tokens of one head and tiles of 16 of its rows (queries).  Lane l = 16 g + r has row r of each tile.  The
+// first product is four matrix instructions of 16 tokens by 16 rows for each 32 channels, the second one of 16 channels by 16 rows for each 32 tokens.
+// Tokens are dealt out to the first one's lines so that what a lane gets of its results, lines 4 g .. 4 g + 3 of each of the four, are tokens 16 g ..
+// 16 g + 15: those whose values it reads as 16 bytes for the second, in the order in which it has their weights.  So nothing is exchanged between lanes.
+// (Instructions of 32 by 32, half as many, leave more room for others beside them, and the same work takes a tenth fewer cycles; but the clock falls by
+// more, and so few sums at a time leave each waiting for the one before it: 2048 tokens on 16000 875 us, 826 so, 32 rows on 4050 tokens 129 and 103.)
+struct Tile {
+  // Token of line `line` of instruction t, and the place of a token when tokens are put in the order instruction by instruction, line by line.
+  static __device__ __forceinline__ int token(int t, int line) { return (line >> 2) * 16 + t * 4 + (line & 3); }
+  static __device__ __forceinline__ int place(int token) { return (token >> 2 & 3) * 16 + (token >> 4) * 4 + (token & 3); }
+  // The first of a lane's eight channels of step i, 32 channels.
+  static __device__ __forceinline__ int channel(int i, int g) { return (i >> 1) * 64 + g * 16 + (i & 1) * 8; }
+};
+
+// 64 tokens' keys in a wave: the lane's 16 bytes j are channels 64 j + 16 g .. of its line's token.
 template <int D> struct KeyTile {
   u32x4 w[4][D / 64];
   __device__ __forceinline__ void load(const uint8_t* keys, int lane) {
-    const int r = lane & 15, g = lane >> 4;
-    const uint8_t* p = keys + ((r >> 2) * 16 + (r & 3)) * D + g * 16;
+    const uint8_t* from = keys + Tile::token(0, lane & 15) * D + (lane >> 4) * 16;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int j = 0; j < D / 64; ++j) w[t][j] = load16(p + t * 4 * D + j * 64);
+      for (int j = 0; j < D / 64; ++j) w[t][j] = load16_once(from + t * 4 * D + j * 64);
+  }
+  // Operand of instruction t and step i.
+  template <typename T> __device__ __forceinline__ typename Operand<T>::Vec operand(int t, int i) const {
+    const u32x4 x = w[t][i >> 1];
+    return (i & 1) ? Operand<T>::codes(x[2], x[3]) : Operand<T>::codes(x[0], x[1]);
   }
 };
-// Channel of the first of the eight numbers that lane group g brings to step i of a product over the channels.
-__device__ __forceinline__ int step_channel(int i, int g) { return (i >> 1) * 64 + g * 16 + (i & 1) * 8; }
-
-// A wave's queries: RT tiles of 16 rows, each the other operand of the products above.
+// A wave's rows, RT tiles of 16, as the other operand.
 template <typename T, int D, int RT> struct Queries {
   typename Operand<T>::Vec v[RT][D / 32][Operand<T>::kTerms];
 };
-template <typename T, int D, int RT>
-__device__ __forceinline__ void key_products(const KeyTile<D>& k, const Queries<T, D, RT>& q, f32x4 (&s)[RT][4]) {
+// Their scores: s[rt][t][i] is of row r of tile rt and token 16 g + 4 t + i.
+template <typename T, int D, int RT> __device__ __forceinline__ void key_products(const KeyTile<D>& k, const Queries<T, D, RT>& q, f32x4 (&s)[RT][4]) {
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) s[rt][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      const u32x4 w = k.w[t][i >> 1];
-      const auto a = (i & 1) ? Operand<T>::codes(w[2], w[3]) : Operand<T>::codes(w[0], w[1]);
+      const auto a = k.template operand<T>(t, i);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll

@@ -66,12 +66,12 @@ template <typename T, int D> __global__ __launch_bounds__(256) void weigh_kernel
     const int row = min(row0 + r, rows - 1), token = row / p.group, head = h * p.group + row % p.group;
     Queries<T, D, 1> q;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) Operand<T>::load(p.q.data, b * p.q.seq + token * p.q.token + head * p.q.head + step_channel(i, g), q.v[0][i]);
+    for (int i = 0; i < D / 32; ++i) Operand<T>::load(p.q.data, b * p.q.seq + token * p.q.token + head * p.q.head + Tile::channel(i, g), q.v[0][i]);
     const float lse = as_global(p.lse)[(b * p.n + token) * p.heads_q + head];
     // (a row that saw nothing gives nothing, and neither does one that is not there)
     const float off = row0 + r < rows && lse != -INFINITY ? lse * -1.4426950408889634f : -INFINITY;
     f32x4 s[1][4];
-    key_products<T, D, 1>(kt, q, s);
+    key_products(kt, q, s);
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][i >> 2][i & 3], c, off));
   }
