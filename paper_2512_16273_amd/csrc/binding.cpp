@@ -7,6 +7,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <cmath>
+
 #include <ATen/ATen.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -22,11 +24,16 @@ struct Library {
   decltype(&tslt_pack_bound_words) pack_bound_words;
   decltype(&tslt_pack_cleared) pack_cleared;
   decltype(&tslt_unpack) unpack;
+  decltype(&tslt_cache_append) cache_append;
+  decltype(&tslt_cache_attend) cache_attend;
+  decltype(&tslt_cache_weigh) cache_weigh;
+  decltype(&tslt_cache_evict) cache_evict;
 } lib;
 bool bound = false;
 
 PyObject *k_idx, *k_logit, *k_prob, *k_count, *k_mass, *k_status, *k_token, *k_slot, *k_accept_len, *k_tokens, *k_ratio, *k_beta, *k_seq,
-    *k_len, *k_node_token, *k_node_slot, *k_words, *k_row_offset;
+    *k_len, *k_node_token, *k_node_slot, *k_words, *k_row_offset, *k_codes,
+    *k_scale, *k_length, *k_out, *k_lse, *k_weight, *k_kept;
 
 // A strided tensor on a GPU that no transform has wrapped, else null.
 const at::Tensor* plain(PyObject* o) {
@@ -70,8 +77,14 @@ bool unread() {
 PyObject* result(int code) { return PyLong_FromLong(code); }
 
 PyObject* py_bind(PyObject*, PyObject* args) {
-  unsigned long long a[9];
-  if (!PyArg_ParseTuple(args, "KKKKKKKKK", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8])) return nullptr;
+  constexpr Py_ssize_t kFunctions = 13;
+  if (PyTuple_GET_SIZE(args) != kFunctions) {
+    PyErr_SetString(PyExc_TypeError, "bind takes the addresses of 13 functions");
+    return nullptr;
+  }
+  unsigned long long a[kFunctions];
+  for (Py_ssize_t i = 0; i < kFunctions; ++i) a[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(args, i));
+  if (PyErr_Occurred()) return nullptr;
   lib.workspace_bytes = reinterpret_cast<decltype(lib.workspace_bytes)>(a[0]);
   lib.truncate_sample = reinterpret_cast<decltype(lib.truncate_sample)>(a[1]);
   lib.verify = reinterpret_cast<decltype(lib.verify)>(a[2]);
@@ -81,6 +94,10 @@ PyObject* py_bind(PyObject*, PyObject* args) {
   lib.pack_bound_words = reinterpret_cast<decltype(lib.pack_bound_words)>(a[6]);
   lib.pack_cleared = reinterpret_cast<decltype(lib.pack_cleared)>(a[7]);
   lib.unpack = reinterpret_cast<decltype(lib.unpack)>(a[8]);
+  lib.cache_append = reinterpret_cast<decltype(lib.cache_append)>(a[9]);
+  lib.cache_attend = reinterpret_cast<decltype(lib.cache_attend)>(a[10]);
+  lib.cache_weigh = reinterpret_cast<decltype(lib.cache_weigh)>(a[11]);
+  lib.cache_evict = reinterpret_cast<decltype(lib.cache_evict)>(a[12]);
   bound = true;
   Py_RETURN_NONE;
 }
@@ -256,6 +273,182 @@ PyObject* py_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return with_code(code, {{k_idx, idx}, {k_logit, logit}, {k_count, count}});
 }
 
+// What the calls of the 8-bit cache share: the cache, its sequences and rows of new tokens.
+struct Sequences {
+  tslt_cache cache;
+  const int32_t *pages, *length;
+  int64_t B, width;
+  int64_t heads() const { return cache.heads; }
+  int64_t D() const { return cache.head_dim; }
+};
+bool read_sequences(PyObject* dict, PyObject* pages, PyObject* length, Sequences& s) {
+  if (!PyDict_CheckExact(dict)) return false;
+  const at::Tensor *codes = dense(PyDict_GetItem(dict, k_codes), at::kByte), *scale = dense(PyDict_GetItem(dict, k_scale), at::kFloat);
+  const at::Tensor *table = dense(pages, at::kInt), *len = dense(length, at::kInt);
+  if (!codes || !scale || !table || !len || codes->dim() != 4 || codes->size(2) != 2 || codes->size(3) % TSLT_PAGE_TOKENS != 0) return false;
+  if (scale->dim() != 3 || scale->size(0) != codes->size(0) || scale->size(1) != codes->size(1) || scale->size(2) != 2) return false;
+  if (table->dim() != 2 || len->numel() != table->size(0)) return false;
+  s.cache = {ptr<uint8_t>(codes), ptr<float>(scale), codes->size(0), int32_t(codes->size(1)), int32_t(codes->size(3) / TSLT_PAGE_TOKENS)};
+  s.pages = ptr<int32_t>(table);
+  s.length = ptr<int32_t>(len);
+  s.B = table->size(0);
+  s.width = table->size(1);
+  return true;
+}
+// [B][n][heads][D], dense along D; n < 0 takes the tensor's and writes it there, dt < 0 likewise.
+bool read_rows(PyObject* o, const Sequences& s, int64_t& n, int64_t heads, int& dt, tslt_rows& rows) {
+  const at::Tensor* t = plain(o);
+  if (t == nullptr || t->dim() != 4) return false;
+  const int type = dtype_code(*t);
+  if (n < 0) n = t->size(1);
+  if (dt < 0) dt = type;
+  if (type < 0 || type != dt || t->size(0) != s.B || t->size(1) != n || t->size(2) != heads || t->size(3) != s.D() || t->stride(3) != 1) return false;
+  const auto stride = [&](int i) { return t->size(i) > 1 ? t->stride(i) : 0; };
+  rows = {t->data_ptr(), stride(0), stride(1), stride(2)};
+  return true;
+}
+bool read_ints(PyObject* o, int64_t numel, const int32_t*& p) {
+  p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = dense(o, at::kInt);
+  if (t == nullptr || t->numel() != numel) return false;
+  p = ptr<int32_t>(t);
+  return true;
+}
+template <typename T> T* sized(PyObject* dict, PyObject* key, at::ScalarType type, int64_t numel, bool optional, bool& there) {
+  PyObject* o = PyDict_GetItem(dict, key);
+  if (o == nullptr || o == Py_None) {
+    there = there && optional;
+    return nullptr;
+  }
+  const at::Tensor* t = dense(o, type);
+  if (t == nullptr || t->numel() != numel) { there = false; return nullptr; }
+  return ptr<T>(t);
+}
+at::ScalarType scalar_type(int dt) { return dt == TSLT_F32 ? at::kFloat : dt == TSLT_BF16 ? at::kBFloat16 : at::kHalf; }
+
+// cache_append(cache, pages, length, k, v, count, index, out, stream)
+PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 9 || !bound) Py_RETURN_NONE;
+  void* stream = PyLong_AsVoidPtr(a[8]);
+  if (unread()) Py_RETURN_NONE;
+  Sequences s;
+  tslt_rows k, v;
+  const int32_t *count, *index;
+  int64_t n = -1;
+  int dt = -1;
+  if (!read_sequences(a[0], a[1], a[2], s) || !read_rows(a[3], s, n, s.heads(), dt, k) || !read_rows(a[4], s, n, s.heads(), dt, v)) Py_RETURN_NONE;
+  if (!read_ints(a[5], s.B, count) || !read_ints(a[6], s.B * n, index) || !PyDict_CheckExact(a[7])) Py_RETURN_NONE;
+  bool there = true;
+  int32_t* length = sized<int32_t>(a[7], k_length, at::kInt, s.B, false, there);
+  int32_t* status = sized<int32_t>(a[7], k_status, at::kInt, s.B, true, there);
+  if (!there) Py_RETURN_NONE;
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.cache_append(&s.cache, s.pages, s.width, s.length, s.B, int32_t(n), &k, &v, tslt_dtype(dt), index, count, length, status, stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
+// cache_attend(q, cache, pages, length, k, v, mask, count, scale or None, out, workspace, stream)
+PyObject* py_cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 12 || !bound) Py_RETURN_NONE;
+  void* stream = PyLong_AsVoidPtr(a[11]);
+  const bool has_scale = a[8] != Py_None;
+  const double given = has_scale ? PyFloat_AsDouble(a[8]) : 0;
+  if (unread()) Py_RETURN_NONE;
+  Sequences s;
+  tslt_rows q, k, v;
+  const int32_t* count;
+  int64_t n = -1;
+  int dt = -1;
+  const at::Tensor* qt = plain(a[0]);
+  if (qt == nullptr || qt->dim() != 4 || !read_sequences(a[1], a[2], a[3], s)) Py_RETURN_NONE;
+  const int64_t heads_q = qt->size(2);
+  if (!read_rows(a[0], s, n, heads_q, dt, q)) Py_RETURN_NONE;
+  const bool fresh = a[4] != Py_None;
+  if (fresh != (a[5] != Py_None)) Py_RETURN_NONE;
+  if (fresh && (!read_rows(a[4], s, n, s.heads(), dt, k) || !read_rows(a[5], s, n, s.heads(), dt, v))) Py_RETURN_NONE;
+  const uint32_t* mask = nullptr;
+  int64_t mask_seq = 0;
+  if (a[6] != Py_None) {
+    const at::Tensor* m = dense(a[6], at::kInt);
+    const int64_t words = (n + 31) / 32;
+    if (m == nullptr || m->dim() != 3 || (m->size(0) != 1 && m->size(0) != s.B) || m->size(1) != n || m->size(2) != words) Py_RETURN_NONE;
+    mask = reinterpret_cast<const uint32_t*>(m->data_ptr());
+    mask_seq = m->size(0) > 1 ? n * words : 0;
+  }
+  const at::Tensor* ws = plain(a[10]);
+  if (!read_ints(a[7], s.B, count) || !PyDict_CheckExact(a[9]) || ws == nullptr || ws->scalar_type() != at::kByte || !ws->is_contiguous()) Py_RETURN_NONE;
+  bool there = true;
+  void* out = sized<void>(a[9], k_out, scalar_type(dt), s.B * n * heads_q * s.D(), false, there);
+  float* lse = sized<float>(a[9], k_lse, at::kFloat, s.B * n * heads_q, false, there);
+  int32_t* status = sized<int32_t>(a[9], k_status, at::kInt, s.B, true, there);
+  if (!there) Py_RETURN_NONE;
+  const float scale = float(has_scale ? given : 1.0 / std::sqrt(double(s.D())));
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.cache_attend(&s.cache, s.pages, s.width, s.length, s.B, int32_t(n), int32_t(heads_q), &q, fresh ? &k : nullptr, fresh ? &v : nullptr,
+                          tslt_dtype(dt), mask, mask_seq, count, scale, out, lse, status, ws->data_ptr(), size_t(ws->numel()), stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
+// cache_weigh(q, lse, cache, pages, length, weight, decay, count, scale or None, out, stream)
+PyObject* py_cache_weigh(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 11 || !bound) Py_RETURN_NONE;
+  void* stream = PyLong_AsVoidPtr(a[10]);
+  const double decay = PyFloat_AsDouble(a[6]);
+  const bool has_scale = a[8] != Py_None;
+  const double given = has_scale ? PyFloat_AsDouble(a[8]) : 0;
+  if (unread()) Py_RETURN_NONE;
+  Sequences s;
+  tslt_rows q;
+  const int32_t* count;
+  int64_t n = -1;
+  int dt = -1;
+  const at::Tensor *qt = plain(a[0]), *lse = dense(a[1], at::kFloat), *weight = dense(a[5], at::kFloat);
+  if (qt == nullptr || qt->dim() != 4 || !lse || !weight || !read_sequences(a[2], a[3], a[4], s)) Py_RETURN_NONE;
+  const int64_t heads_q = qt->size(2), all = s.B * s.heads() * s.width * TSLT_PAGE_TOKENS;
+  if (!read_rows(a[0], s, n, heads_q, dt, q) || lse->numel() != s.B * n * heads_q || weight->numel() != all) Py_RETURN_NONE;
+  if (!read_ints(a[7], s.B, count) || !PyDict_CheckExact(a[9])) Py_RETURN_NONE;
+  bool there = true;
+  float* out = sized<float>(a[9], k_weight, at::kFloat, all, false, there);
+  int32_t* status = sized<int32_t>(a[9], k_status, at::kInt, s.B, true, there);
+  if (!there) Py_RETURN_NONE;
+  const float scale = float(has_scale ? given : 1.0 / std::sqrt(double(s.D())));
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.cache_weigh(&s.cache, s.pages, s.width, s.length, s.B, int32_t(n), int32_t(heads_q), &q, tslt_dtype(dt), ptr<float>(lse), count, scale,
+                         ptr<float>(weight), float(decay), out, status, stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
+// cache_evict(cache, pages, length, weight, keep, recent, new_pages, out, stream)
+PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 9 || !bound) Py_RETURN_NONE;
+  void* stream = PyLong_AsVoidPtr(a[8]);
+  const long long keep = PyLong_AsLongLong(a[4]), recent = PyLong_AsLongLong(a[5]);
+  if (unread()) Py_RETURN_NONE;
+  Sequences s;
+  const at::Tensor *weight = dense(a[3], at::kFloat), *fresh = dense(a[6], at::kInt);
+  if (keep < 1 || keep > 0x7FFFFFFF || recent < 0 || recent > 0x7FFFFFFF || !read_sequences(a[0], a[1], a[2], s) || !weight || !fresh) Py_RETURN_NONE;
+  if (weight->numel() != s.B * s.heads() * s.width * TSLT_PAGE_TOKENS || fresh->dim() != 2 || fresh->size(0) != s.B || !PyDict_CheckExact(a[7])) Py_RETURN_NONE;
+  bool there = true;
+  int32_t* length = sized<int32_t>(a[7], k_length, at::kInt, s.B, false, there);
+  int32_t* kept = sized<int32_t>(a[7], k_kept, at::kInt, s.B * s.heads() * keep, false, there);
+  float* out = sized<float>(a[7], k_weight, at::kFloat, s.B * s.heads() * fresh->size(1) * TSLT_PAGE_TOKENS, false, there);
+  int32_t* status = sized<int32_t>(a[7], k_status, at::kInt, s.B, true, there);
+  if (!there) Py_RETURN_NONE;
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.cache_evict(&s.cache, s.pages, s.width, s.length, s.B, ptr<float>(weight), int32_t(keep), int32_t(recent), ptr<int32_t>(fresh), fresh->size(1),
+                         length, kept, out, status, stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
 // What a call into torch throws (no memory left, say) becomes a Python exception, as from torch itself.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -267,7 +460,8 @@ template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyMethodDef f
 }
 PyMethodDef methods[] = {
     {"bind", py_bind, METH_VARARGS, nullptr}, fast<py_truncate>("truncate"), fast<py_verify>("verify"), fast<py_verify_tree>("verify_tree"),
-    fast<py_pack>("pack"), fast<py_unpack>("unpack"), {nullptr, nullptr, 0, nullptr}};
+    fast<py_pack>("pack"), fast<py_unpack>("unpack"), fast<py_cache_append>("cache_append"), fast<py_cache_attend>("cache_attend"),
+    fast<py_cache_weigh>("cache_weigh"), fast<py_cache_evict>("cache_evict"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -276,7 +470,8 @@ PyMODINIT_FUNC PyInit__binding() {
   const std::pair<PyObject**, const char*> keys[] = {
       {&k_idx, "idx"}, {&k_logit, "logit"}, {&k_prob, "prob"}, {&k_count, "count"}, {&k_mass, "mass"}, {&k_status, "status"},
       {&k_token, "token"}, {&k_slot, "slot"}, {&k_accept_len, "accept_len"}, {&k_tokens, "tokens"}, {&k_ratio, "ratio"}, {&k_beta, "beta"},
-      {&k_seq, "seq"}, {&k_len, "len"}, {&k_node_token, "node_token"}, {&k_node_slot, "node_slot"}, {&k_words, "words"}, {&k_row_offset, "row_offset"}};
+      {&k_seq, "seq"}, {&k_len, "len"}, {&k_node_token, "node_token"}, {&k_node_slot, "node_slot"}, {&k_words, "words"}, {&k_row_offset, "row_offset"},
+      {&k_codes, "codes"}, {&k_scale, "scale"}, {&k_length, "length"}, {&k_out, "out"}, {&k_lse, "lse"}, {&k_weight, "weight"}, {&k_kept, "kept"}};
   for (const auto& k : keys)
     if ((*k.first = PyUnicode_InternFromString(k.second)) == nullptr) return nullptr;
   PyObject* m = PyModule_Create(&module);

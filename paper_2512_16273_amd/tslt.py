@@ -119,7 +119,8 @@ def load(path: Optional[str] = None):
     if _fast is not None:
         _fast.bind(*[c.cast(getattr(lib, fn), vp).value for fn in (
             "tslt_workspace_bytes", "tslt_truncate_sample", "tslt_verify", "tslt_verify_accept", "tslt_verify_resample", "tslt_verify_tree",
-            "tslt_pack_bound_words", "tslt_pack_cleared", "tslt_unpack")])
+            "tslt_pack_bound_words", "tslt_pack_cleared", "tslt_unpack",
+            "tslt_cache_append", "tslt_cache_attend", "tslt_cache_weigh", "tslt_cache_evict")])
     _lib = lib
     return lib
 
@@ -567,6 +568,12 @@ def cache_append(cache: dict, pages: torch.Tensor, length: torch.Tensor, k: torc
     the sequences pages [B, width], length [B] of the cache, which changes in place.  count [B]: how many of the n tokens; index [B, n]:
     which ones.  Returns length, the new one, and status [B]."""
     lib = load()
+    if _fast is not None and out is not None and k.is_cuda:
+        code = _fast.cache_append(cache, pages, length, k, v, count, index, out, _stream())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     c, heads, D = _cache_of(cache)
     B, width = _sequences(pages, length)
     if k.dim() != 4:
@@ -592,6 +599,12 @@ def cache_attend(q: torch.Tensor, cache: dict, pages: torch.Tensor, length: torc
     tokens that `mask` shows ([B or 1, n, ceil(n / 32)] int32, see tree_mask; None: a chain).  scale: 1 / sqrt(D).  Returns out
     [B, n, heads_q, D], lse [B, n, heads_q] and status [B]."""
     lib = load()
+    if _fast is not None and out is not None and workspace is not None and q.is_cuda:
+        code = _fast.cache_attend(q, cache, pages, length, k, v, mask, count, scale, out, workspace, _stream())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     c, heads, D = _cache_of(cache)
     B, width = _sequences(pages, length)
     if q.dim() != 4:
@@ -626,6 +639,12 @@ def cache_weigh(q: torch.Tensor, lse: torch.Tensor, cache: dict, pages: torch.Te
     """tslt_cache_weigh: weight [B, heads, width * 64] times decay, and what cache_attend's rows q with its lse gave each cached token.
     Returns weight (out may hold the same array) and status [B]."""
     lib = load()
+    if _fast is not None and out is not None and q.is_cuda:
+        code = _fast.cache_weigh(q, lse, cache, pages, length, weight, float(decay), count, scale, out, _stream())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     c, heads, D = _cache_of(cache)
     B, width = _sequences(pages, length)
     if q.dim() != 4:
@@ -649,6 +668,12 @@ def cache_evict(cache: dict, pages: torch.Tensor, length: torch.Tensor, weight: 
     """tslt_cache_evict: of every head the `recent` last tokens and those of most weight, `keep` in all, copied to the pages
     new_pages [B, new_width] of the same cache.  Returns length [B], kept [B, heads, keep], weight [B, heads, new_width * 64] and status [B]."""
     lib = load()
+    if _fast is not None and out is not None and weight.is_cuda:
+        code = _fast.cache_evict(cache, pages, length, weight, int(keep), int(recent), new_pages, out, _stream())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     c, heads, D = _cache_of(cache)
     B, width = _sequences(pages, length)
     _dev(weight, torch.float32, "weight"); _dev(new_pages, torch.int32, "new_pages")

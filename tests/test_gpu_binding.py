@@ -134,3 +134,68 @@ def test_trees_by_either_path(tslt, monkeypatch):
         for bad in ((2, 99), [], (0, 2)):
             assert call(bad)[0] is tslt.TsltError
         assert call(expansion, ws=ws[:64])[0] is tslt.TsltError and call(expansion, t["target"][0], taken=False)[0] is tslt.TsltError
+
+
+def test_calls_of_the_cache(tslt, monkeypatch):
+    torch.manual_seed(3)
+    B, n, H, G, D, keep = 3, 5, 2, 3, 64, 70
+    pages = torch.arange(3 * B, dtype=torch.int32, device=DEV).view(B, 3)
+    start = tslt.cache_create(5 * B, H, D, DEV)
+    x = torch.randn(B, 128, H * (G + 2), D, device=DEV, dtype=torch.bfloat16)
+    length = tslt.cache_append(start, pages, torch.zeros(B, dtype=torch.int32, device=DEV), x[:, :, :H], x[:, :, H:2 * H],
+                               count=torch.tensor([100, 0, 128], dtype=torch.int32, device=DEV))["length"]
+    q, k, v = x[:, :n, 2 * H:], x[:, 20:20 + n, :H], x[:, 20:20 + n, H:2 * H]
+    index = torch.stack([torch.randperm(n, device=DEV) for _ in range(B)]).to(torch.int32)
+    count = torch.tensor([n, 2, 0], dtype=torch.int32, device=DEV)
+    mask = tslt.tree_mask((2, 1), DEV)
+    i32, f32 = torch.int32, torch.float32
+
+    def outs(**shapes):
+        return {name: torch.full(shape, 77, dtype=dt, device=DEV) for name, (shape, dt) in shapes.items()}
+
+    def fresh():
+        return {name: t.clone() for name, t in start.items()}
+
+    def append(cache, **kw):
+        out = outs(length=((B,), i32), status=((B,), i32))
+        got = tslt.cache_append(cache, pages, length, **{"k": k, "v": v, "count": count, "index": index, "out": out, **kw})
+        return {**got, **cache}
+
+    appended = both(tslt, monkeypatch, lambda: append(fresh()))
+    assert appended["length"].tolist() == [105, 2, 128]
+    both(tslt, monkeypatch, lambda: append(fresh(), count=None, index=None))
+    assert "entries" in both(tslt, monkeypatch, lambda: append(fresh(), count=count[:2]), taken=False)[1]
+    assert "16 bytes" in both(tslt, monkeypatch, lambda: append(fresh(), k=torch.zeros(B, n, H, D + 2, device=DEV)[..., :D], v=k.float()))[1]
+    assert "must be" in both(tslt, monkeypatch, lambda: append(fresh(), v=v.float()), taken=False)[1]
+
+    ws = torch.empty(max(256, tslt.cache_attend_workspace_bytes(B, n, H * G, H, D, 3)), dtype=torch.uint8, device=DEV)
+    def attend(**kw):
+        out = outs(out=((B, n, H * G, D), torch.bfloat16), lse=((B, n, H * G), f32), status=((B,), i32))
+        return tslt.cache_attend(q, start, pages, length, **{"out": out, "workspace": ws, **kw})
+
+    for kw in ({}, {"k": k, "v": v}, {"k": k, "v": v, "count": count, "scale": 0.5}, {"k": k, "v": v, "mask": mask}):
+        both(tslt, monkeypatch, lambda: attend(**kw))
+    assert "together" in both(tslt, monkeypatch, lambda: attend(k=k), taken=False)[1]
+    assert "scale" in both(tslt, monkeypatch, lambda: attend(scale=-1.0))[1]
+    assert "mask must be" in both(tslt, monkeypatch, lambda: attend(k=k, v=v, mask=mask[:, 1:]), taken=False)[1]
+    lse = attend(k=k, v=v)["lse"]
+
+    weight = torch.rand(B, H, 192, device=DEV)
+    def weigh(**kw):
+        out = outs(weight=((B, H, 192), f32), status=((B,), i32))
+        return tslt.cache_weigh(q, lse, start, pages, length, **{"weight": weight, "decay": 0.5, "out": out, **kw})
+
+    both(tslt, monkeypatch, lambda: weigh())
+    both(tslt, monkeypatch, lambda: weigh(count=count, scale=0.2, decay=1))
+    assert "shapes" in both(tslt, monkeypatch, lambda: weigh(weight=weight[:, :1].contiguous()), taken=False)[1]
+
+    new_pages = torch.arange(3 * B, 5 * B, dtype=torch.int32, device=DEV).view(B, 2)
+    def evict(**kw):
+        out = outs(length=((B,), i32), kept=((B, H, keep), i32), weight=((B, H, 128), f32), status=((B,), i32))
+        cache = fresh()
+        got = tslt.cache_evict(cache, pages, length, **{"weight": weight, "keep": keep, "recent": 8, "new_pages": new_pages, "out": out, **kw})
+        return {**got, **cache}
+
+    assert both(tslt, monkeypatch, lambda: evict())["length"].tolist() == [70, 0, 70]
+    assert "do not hold" in both(tslt, monkeypatch, lambda: evict(new_pages=new_pages[:, :1].contiguous(), out=outs(
+        length=((B,), i32), kept=((B, H, keep), i32), weight=((B, H, 64), f32), status=((B,), i32))))[1]
