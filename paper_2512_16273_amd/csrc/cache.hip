@@ -237,7 +237,9 @@ int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t widt
   int code;
   if (!grid_fits(who, std::max(heads, moves), code)) return code;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(tslt::evict_select_kernel, dim3(unsigned(heads)), dim3(tslt::kEvictThreads), 0, s, p);
+  // (weights in registers where the longest sequence's fit: 16 waves of 64 lanes)
+  const auto select = width <= 64 ? tslt::evict_select_kernel<4> : width <= 512 ? tslt::evict_select_kernel<32> : tslt::evict_select_kernel<0>;
+  hipLaunchKernelGGL(select, dim3(unsigned(heads)), dim3(tslt::kEvictThreads), 0, s, p);
   const auto move = cache->head_dim == 64 ? tslt::evict_move_kernel<64> : cache->head_dim == 128 ? tslt::evict_move_kernel<128> : tslt::evict_move_kernel<256>;
   hipLaunchKernelGGL(move, dim3(unsigned(moves)), dim3(256), 0, s, p);
   return launched("tslt_cache_evict launch");
