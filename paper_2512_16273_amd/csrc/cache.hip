@@ -224,14 +224,8 @@ int tslt_cache_weigh(const tslt_cache* cache, const int32_t* pages, int64_t widt
   p.B = B; p.n = n; p.group = heads_q / cache->heads; p.heads_q = heads_q; p.count = count; p.lse = lse;
   p.scale2 = float(double(scale) * 1.4426950408889634074);
   p.decay = decay; p.weight = weight; p.out_weight = out_weight; p.status = status;
-  // Strips of a sequence's pages, a multiple of the waves: as many as make one round of workgroups (32 sequences of 1000 to 16000 tokens, 8 heads, in
-  // one strip / two / four / eight: 97 / 98 / 104 / 117 us; one sequence of 1500, 12 heads: 8.0 / 6.5 / 6.6 / 6.5).
-  const int64_t strips = std::max<int64_t>(1, std::min<int64_t>(2 * int64_t(tslt::compute_units()) / (B * cache->heads), (width + 3) / 4));
-  p.strip = int(((width + strips - 1) / strips + 3) / 4 * 4);
-  p.strips = int((width + p.strip - 1) / p.strip);
-  const int64_t blocks = B * cache->heads * p.strips;
-  int code;
-  if (!grid_fits(who, blocks, code)) return code;
+  // One round of workgroups, two to a compute unit, or a page to each wave.
+  const int64_t blocks = std::min<int64_t>(2 * int64_t(tslt::compute_units()), (std::min<int64_t>(B * cache->heads, 1 << 20) * width + 3) / 4);
   by_type<Weigh>(dt, cache->head_dim, p, unsigned(blocks), reinterpret_cast<hipStream_t>(stream));
   return launched("tslt_cache_weigh launch");
 }
