@@ -417,8 +417,8 @@ typedef struct {
  *
  *   pages [B][width], length [B]   the sequences, see above
  *   k, v        [B][n][heads][D] of type dt
- *   index       [B][n] int32: the new tokens to append, in order, the first count[b] of a row; NULL: tokens 0, 1, ...
- *   count       [B] int32: how many (0..n); NULL: n.  With tslt_verify's accept_len + 1, or the nodes on tslt_verify_tree's
+ *   index       [B][index_width] int32: the new tokens to append, in order, the first count[b] of a row; NULL: tokens 0, 1, ..., n - 1
+ *   count       [B] int32: how many (0..index_width, or 0..n without index); NULL: all.  With tslt_verify's accept_len + 1, or the nodes on tslt_verify_tree's
  *               verified path, only what was accepted enters the cache
  *   out_length  [B] int32 the sequences' new lengths; not `length` itself
  *   status      [B] int32; may be NULL
@@ -427,7 +427,7 @@ typedef struct {
  * are rounded to nearest-even; infinities become +-448 times the scale, NaN stays.  A page that the call begins is cleared behind its last token.  Tokens that the page table has no room for are not
  * written, and an index outside 0..n-1 writes zeros (TSLT_ROW_BAD_PAGE, TSLT_ROW_BAD_INDEX).  No workspace. */
 int tslt_cache_append(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
-                      const tslt_rows* k, const tslt_rows* v, tslt_dtype dt, const int32_t* index, const int32_t* count,
+                      const tslt_rows* k, const tslt_rows* v, tslt_dtype dt, const int32_t* index, int32_t index_width, const int32_t* count,
                       int32_t* out_length, int32_t* status, void* stream);
 
 /* Softmax attention of n new tokens a sequence over its cached tokens, all of which every one sees, and over each other:

@@ -80,7 +80,7 @@ def append(codes, scale, tables, lengths, k, v, index=None, count=None):
     B, n, H, D = k.shape
     out = []
     for b in range(B):
-        m = n if count is None else int(count[b])
+        m = (n if index is None else len(index[b])) if count is None else int(count[b])
         rows = list(range(m)) if index is None else [int(i) for i in index[b][:m]]
         start = int(lengths[b])
         end = min(start + m, len(tables[b]) * PAGE)

@@ -16,11 +16,12 @@ struct AppendParams {
   RowsView k, v;
   int64_t B;
   int n;
-  const int32_t* index;                    // [B][n], null: 0 .. n - 1
-  const int32_t* count;                    // null: n
+  const int32_t* index;                    // [B][most], null: 0 .. most - 1
+  const int32_t* count;                    // null: most
+  int most;                                // tokens that a sequence appends at most
   int32_t* out_length;
   int32_t* status;
-  int most_pages;                          // pages that n tokens can touch
+  int most_pages;                          // pages that `most` tokens can touch
 };
 
 // Two numbers as codes (the low or the high half of a word).  Infinite ones saturate, as the format has none; NaN stays.
@@ -76,13 +77,13 @@ template <typename T, int D, int kTeam, int kMost> __global__ __launch_bounds__(
   const int64_t b = blockIdx.x / (groups * uint32_t(p.most_pages));
   bool bad_length;
   const int start = cached_tokens(p.c, b, bad_length);
-  const int asked = p.count ? as_global(p.count)[b] : p.n;
-  const int more = min(max(asked, 0), p.n);
+  const int asked = p.count ? as_global(p.count)[b] : p.most;
+  const int more = min(max(asked, 0), p.most);
   const int64_t end64 = min(int64_t(start) + more, p.c.width * kPage);
   const int end = int(end64);
   const int first = start / kPage;
   const int32_t* table = p.c.pages + b * p.c.width;
-  const int32_t* index = p.index ? p.index + b * p.n : nullptr;
+  const int32_t* index = p.index ? p.index + b * p.most : nullptr;
 
   if (h0 == 0 && w == 0) {
     int bits = bad_length || end64 < int64_t(start) + more ? kBadPage : 0;

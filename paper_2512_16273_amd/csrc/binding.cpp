@@ -338,14 +338,17 @@ PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   int64_t n = -1;
   int dt = -1;
   if (!read_sequences(a[0], a[1], a[2], s) || !read_rows(a[3], s, n, s.heads(), dt, k) || !read_rows(a[4], s, n, s.heads(), dt, v)) Py_RETURN_NONE;
-  if (!read_ints(a[5], s.B, count) || !read_ints(a[6], s.B * n, index) || !PyDict_CheckExact(a[7])) Py_RETURN_NONE;
+  const at::Tensor* chosen = plain(a[6]);
+  if (a[6] != Py_None && (chosen == nullptr || chosen->dim() != 2)) Py_RETURN_NONE;
+  const int64_t most = chosen == nullptr ? 0 : chosen->size(1);
+  if (!read_ints(a[5], s.B, count) || !read_ints(a[6], s.B * most, index) || !PyDict_CheckExact(a[7])) Py_RETURN_NONE;
   bool there = true;
   int32_t* length = sized<int32_t>(a[7], k_length, at::kInt, s.B, false, there);
   int32_t* status = sized<int32_t>(a[7], k_status, at::kInt, s.B, true, there);
   if (!there) Py_RETURN_NONE;
   int code;
   Py_BEGIN_ALLOW_THREADS
-  code = lib.cache_append(&s.cache, s.pages, s.width, s.length, s.B, int32_t(n), &k, &v, tslt_dtype(dt), index, count, length, status, stream);
+  code = lib.cache_append(&s.cache, s.pages, s.width, s.length, s.B, int32_t(n), &k, &v, tslt_dtype(dt), index, int32_t(most), count, length, status, stream);
   Py_END_ALLOW_THREADS
   return result(code);
 }

@@ -63,7 +63,7 @@ template <template <typename, int> class Launch, typename P> void by_type(tslt_d
 constexpr int kFewTokens = 16;
 template <typename T, int D> struct Append {
   static void go(const tslt::AppendParams& p, unsigned blocks, hipStream_t s) {
-    if (p.n <= kFewTokens) hipLaunchKernelGGL((tslt::append_kernel<T, D, 64, kFewTokens>), dim3(blocks), dim3(256), 0, s, p);
+    if (p.most <= kFewTokens) hipLaunchKernelGGL((tslt::append_kernel<T, D, 64, kFewTokens>), dim3(blocks), dim3(256), 0, s, p);
     else hipLaunchKernelGGL((tslt::append_kernel<T, D, 256, tslt::kPage>), dim3(blocks), dim3(256), 0, s, p);
   }
 };
@@ -121,12 +121,13 @@ size_t attend_part_bytes(const tslt::AttendParams& p, int D) {
 extern "C" {
 
 int tslt_cache_append(const tslt_cache* cache, const int32_t* pages, int64_t width, const int32_t* length, int64_t B, int32_t n,
-                      const tslt_rows* k, const tslt_rows* v, tslt_dtype dt, const int32_t* index, const int32_t* count,
+                      const tslt_rows* k, const tslt_rows* v, tslt_dtype dt, const int32_t* index, int32_t index_width, const int32_t* count,
                       int32_t* out_length, int32_t* status, void* stream) {
   const char* who = "tslt_cache_append";
   if (int e = check_cache(who, cache, pages, width, length, B)) return e;
   if (!valid_dtype(dt)) return fail(TSLT_ERR_INVALID_ARG, "%s: unknown dtype %d", who, int(dt));
   if (n < 1) return fail(TSLT_ERR_INVALID_ARG, "%s: n must be at least 1", who);
+  if (index && index_width < 1) return fail(TSLT_ERR_INVALID_ARG, "%s: index_width must be at least 1", who);
   if (B == 0) return TSLT_OK;
   if (int e = check_rows(who, "k", k, dt)) return e;
   if (int e = check_rows(who, "v", v, dt)) return e;
@@ -136,8 +137,9 @@ int tslt_cache_append(const tslt_cache* cache, const int32_t* pages, int64_t wid
   p.c = view(cache, pages, width, length);
   p.k = view(k); p.v = view(v);
   p.B = B; p.n = n; p.index = index; p.count = count; p.out_length = out_length; p.status = status;
-  p.most_pages = int((int64_t(n) + tslt::kPage - 2) / tslt::kPage + 1);
-  const int64_t heads_each = n <= kFewTokens ? 4 : 1, blocks = B * ((cache->heads + heads_each - 1) / heads_each) * p.most_pages;
+  p.most = index ? index_width : n;
+  p.most_pages = int((int64_t(p.most) + tslt::kPage - 2) / tslt::kPage + 1);
+  const int64_t heads_each = p.most <= kFewTokens ? 4 : 1, blocks = B * ((cache->heads + heads_each - 1) / heads_each) * p.most_pages;
   int code;
   if (!grid_fits(who, blocks, code)) return code;
   by_type<Append>(dt, cache->head_dim, p, unsigned(blocks), reinterpret_cast<hipStream_t>(stream));

@@ -106,7 +106,7 @@ def load(path: Optional[str] = None):
                                      vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     cache, rows = c.POINTER(_Cache), c.POINTER(_Rows)
     lib.tslt_cache_append.restype = c.c_int
-    lib.tslt_cache_append.argtypes = [cache, vp, i64, vp, i64, i32, rows, rows, c.c_int, vp, vp, vp, vp, vp]
+    lib.tslt_cache_append.argtypes = [cache, vp, i64, vp, i64, i32, rows, rows, c.c_int, vp, i32, vp, vp, vp, vp]
     lib.tslt_cache_attend_workspace_bytes.restype = sz
     lib.tslt_cache_attend_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64]
     lib.tslt_cache_attend.restype = c.c_int
@@ -565,8 +565,8 @@ def _sized(out: dict, name: str, dtype, numel: int, optional=False) -> Optional[
 def cache_append(cache: dict, pages: torch.Tensor, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                  count: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None, out: Optional[dict] = None) -> dict:
     """tslt_cache_append: k, v [B, n, heads, D] (any of the three types, any strides that keep rows 16-byte aligned) to the end of
-    the sequences pages [B, width], length [B] of the cache, which changes in place.  count [B]: how many of the n tokens; index [B, n]:
-    which ones.  Returns length, the new one, and status [B]."""
+    the sequences pages [B, width], length [B] of the cache, which changes in place.  index [B, m]: which of
+    the n tokens, in order; count [B]: how many of them.  Returns length, the new one, and status [B]."""
     lib = load()
     if _fast is not None and out is not None and k.is_cuda:
         code = _fast.cache_append(cache, pages, length, k, v, count, index, out, _stream())
@@ -580,10 +580,13 @@ def cache_append(cache: dict, pages: torch.Tensor, length: torch.Tensor, k: torc
         raise TsltError("k must be [B, n, heads, D]")
     n = k.shape[1]
     kr, vr = _rows_of(k, "k", (B, n, heads, D), k.dtype), _rows_of(v, "v", (B, n, heads, D), k.dtype)
+    if index is not None and index.dim() != 2:
+        raise TsltError("index must be [B, m]")
+    most = 0 if index is None else index.shape[1]
     if out is None:
         out = {"length": torch.empty(B, dtype=torch.int32, device=k.device), "status": torch.empty(B, dtype=torch.int32, device=k.device)}
     _check(lib.tslt_cache_append(c, pages.data_ptr(), width, length.data_ptr(), B, n, kr, vr, _dtype_code(k),
-                                 _counted(index, "index", B * n), _counted(count, "count", B), _sized(out, "length", torch.int32, B),
+                                 _counted(index, "index", B * most), most, _counted(count, "count", B), _sized(out, "length", torch.int32, B),
                                  _sized(out, "status", torch.int32, B, optional=True), _stream()))
     return out
 

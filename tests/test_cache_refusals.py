@@ -40,10 +40,10 @@ def common(lib, call, dt_arg=True):
 
 
 def test_append(lib):
-    def call(c=cache(), pages=FAKE, width=4, length=FAKE, B=3, n=2, k=rows(), v=rows(), dt=1, out=FAKE + 64):
-        return lib.tslt_cache_append(c, pages, width, length, B, n, k, v, dt, None, None, out, None, None)
+    def call(c=cache(), pages=FAKE, width=4, length=FAKE, B=3, n=2, k=rows(), v=rows(), dt=1, index=None, most=0, out=FAKE + 64):
+        return lib.tslt_cache_append(c, pages, width, length, B, n, k, v, dt, index, most, None, out, None, None)
     common(lib, call)
-    assert call(n=0) == -1 and call(dt=5) == -1
+    assert call(n=0) == -1 and call(dt=5) == -1 and call(index=FAKE, most=0) == -1
     assert call(k=None) == -1 and call(v=rows(data=None)) == -1
     assert call(k=rows(data=FAKE + 2)) == -1 and call(v=rows(token=100)) == -1 and "16 bytes" in message(lib)
     assert call(out=None) == -1 and call(out=FAKE) == -1 and "out_length" in message(lib)

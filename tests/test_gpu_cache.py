@@ -295,6 +295,24 @@ def test_append_is_exact(tslt, dtype, D, H, n, lengths, chosen):
     same_values((cache["codes"].cpu().numpy(), cache["scale"].cpu().numpy()), want[:2], host[2], want[2], H)
 
 
+def test_append_of_a_few_of_many_tokens(tslt):
+    """Index rows of their own width, narrower and wider than the call's tokens."""
+    rng = np.random.default_rng(22)
+    D, H, B, lengths = 128, 5, 3, [60, 0, 64]
+    for n, m, counts in ((40, 4, [4, 0, 2]), (3, 70, [70, 1, 33]), (100, 17, None)):
+        host = make_cache(rng, H, D, lengths, spare=3)
+        cache, pages, length = on_gpu(*host)
+        _, k, v = projection(rng, B, n, 1, H, D, torch.bfloat16)[0]
+        index = rng.integers(0, n, (B, m)).astype(np.int32)
+        count = None if counts is None else np.array(counts, np.int32)
+        want = O.append(*host, *(t.double().cpu().numpy() for t in (k, v)), index, count)
+        got = tslt.cache_append(cache, pages, length, k, v, index=torch.from_numpy(index).to(DEV),
+                                count=None if count is None else torch.from_numpy(count).to(DEV))
+        torch.cuda.synchronize()
+        assert got["length"].tolist() == want[2].tolist() and got["status"].tolist() == [0] * B
+        same_values((cache["codes"].cpu().numpy(), cache["scale"].cpu().numpy()), want[:2], host[2], want[2], H)
+
+
 def test_a_page_that_is_begun_is_cleared_behind_its_last_token(tslt):
     for D, n, tokens in ((64, 5, 5), (128, 130, 2), (256, 65, 1)):
         cache = tslt.cache_create(4, 2, D, DEV)
