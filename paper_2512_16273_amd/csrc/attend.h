@@ -246,10 +246,11 @@ __device__ __forceinline__ void page_round(const Queries<T, D, RT>& q, f32x4 (&s
   static_assert(kElements <= kScores && kElements <= kValues, "a weight to a product at most");
   f32x4 next[RT][4];
   bf16x8 w[RT][2][kW];
+  float sum[RT] = {};                      // (a page's weights by themselves: a long sequence's sum takes an addition a page, not sixteen)
   const auto weight = [&](int k, int n) {
     const int rt = n >> 3, e = n & 7;
     const float x = exp2_fast(__builtin_fmaf(s[rt][2 * k + (e >> 2)][e & 3], c, -st.m[rt]));
-    st.l[rt] += x;
+    sum[rt] += x;
     split_weight(x, e, w[rt][k]);
   };
   typename Operand<T>::Vec key[kRing];
@@ -277,9 +278,11 @@ __device__ __forceinline__ void page_round(const Queries<T, D, RT>& q, f32x4 (&s
     keep_order();
   }
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
+  for (int rt = 0; rt < RT; ++rt) {
+    st.l[rt] += sum[rt];
 #pragma unroll
     for (int t = 0; t < 4; ++t) s[rt][t] = next[rt][t];
+  }
 }
 // The same for the kernel whose waves read operands of their own: a page's weights, then its values.
 template <typename T, int D, int RT>
@@ -511,7 +514,7 @@ template <typename T, int D, int NT, int kRows> __device__ __forceinline__ void 
 
 // All threads of a workgroup that has given its rows: the last one of a sequence's chunks joins them, and says how the sequence's pages were.
 template <typename T, int D, int NT, int kRows>
-__device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, bool bad, int& told) {
+__device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, bool bad, int (&told)[2]) {
   const int tid = int(threadIdx.x);
   const bool speaks = p.status && at.h == 0 && at.rg == 0;
   if (at.active == 1) {
@@ -521,13 +524,13 @@ __device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, boo
     return;
   }
   uint64_t* words = p.words + ((at.b * p.c.heads + at.h) * p.row_groups + at.rg) * int64_t(p.chunks);
-  if (!all_arrived(words, at.chunk, at.active, p.tag, told)) return;
+  if (!all_arrived(words, at.chunk, at.active, p.tag, told[0])) return;
   if (wave_id() == 0) {
     const bool mine = claimed(words, at.active, p.tag);
-    if (lane_id() == 0) told = mine ? 1 : 0;
+    if (lane_id() == 0) told[1] = mine ? 1 : 0;
   }
   __syncthreads();
-  if (__builtin_amdgcn_readfirstlane(told) == 0) return;
+  if (__builtin_amdgcn_readfirstlane(told[1]) == 0) return;
   const int64_t part = (at.b * p.c.heads + at.h) * int64_t(p.chunks) * at.rows;
   const int chunks = at.active;
   at.active = 1;
@@ -582,7 +585,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(co
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ FreshShared sh;
   __shared__ float2 join_ml[kStreamTurns][16 * RT];
-  __shared__ int told;
+  __shared__ int told[2];
   constexpr int KS = kStreamTurns, kRows = 16 * RT;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, g = lane >> 4, tid = int(threadIdx.x);
   Place at;
@@ -674,7 +677,7 @@ template <typename T, int D, int RT, int NW, int kDeep, int kAhead>
 __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_rows_kernel(const AttendParams p) {
   extern __shared__ __align__(16) uint8_t lds[];
   __shared__ FreshShared sh;
-  __shared__ int told;
+  __shared__ int told[2];
   typedef Staged<Bf16, D> F;               // (places in a tile of 16 bits)
   constexpr int NT = NW * 64, kRows = NW * 16 * RT, kLoads = kPage * D / 16 / NT;
   static_assert(kPage * D / 16 % NT == 0, "every thread has as many pieces of a page");

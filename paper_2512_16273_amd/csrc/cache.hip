@@ -85,7 +85,8 @@ template <typename T, int D> struct Weigh {
 //   more, once with 32, whose parts cost more to join.  us by one round of workgroups / two: 4 sequences of 131000 tokens 167 / 172.  Where there are
 //   enough without, 16 rows are still cut in four, as sequences differ in length: 64 sequences of 100 to 8000 tokens, 8 heads, in one / four: 4 rows
 //   112.6 / 106.0, 32 rows 123 / 134; all of 4050 tokens 93.9 / 96.1, 106 / 124.
-//   Up to 64 rows, the same in one / two / four: 36 rows 205 / 188 / 179, of 4050 tokens 150 / 155 / 168: three.
+//   Up to 64 rows, the same in one / two / four: 36 rows 205 / 188 / 179, of 4050 tokens 150 / 155 / 168: three.  (Of neither more than eight rounds
+//   in all: sequences even out by their number then.)
 //   More rows: what takes least, in pages, of rounds of workgroups and what a chunk costs beside its pages (2048 tokens on 16000, 512 workgroups
 //   in one / two / four chunks: 818 / 915 / 903).
 void plan_attend(tslt::AttendParams& p, bool f32, int D) {
@@ -95,15 +96,15 @@ void plan_attend(tslt::AttendParams& p, bool f32, int D) {
   const int64_t units = p.B * p.c.heads * p.row_groups, slots = 2 * int64_t(tslt::compute_units());
   int64_t chunks = 1;
   if (choice.stream) {
-    chunks = choice.rows == 32 ? slots / units : 2 * units > slots ? 4 : 2 * slots / units;
+    chunks = choice.rows == 32 ? slots / units : 2 * units > slots ? std::min<int64_t>(4, 8 * slots / units) : 2 * slots / units;
     chunks = std::max<int64_t>(1, std::min<int64_t>({chunks, (p.c.width + 15) / 16, 256}));
   } else {
     int64_t least = 0;
-    for (int64_t n = 1; n <= std::min<int64_t>(256, (p.c.width + 7) / 8); ++n) {
+    for (int64_t n = 1; n <= std::max<int64_t>(1, std::min<int64_t>({256, (p.c.width + 7) / 8, 2 * slots / units})); ++n) {
       const int64_t cost = (units * n + slots - 1) / slots * ((p.c.width + n - 1) / n + (n > 1 ? 20 : 8));
       if (n == 1 || cost < least) { least = cost; chunks = n; }
     }
-    if (choice.rows == 64 && 2 * units > slots) chunks = std::max(chunks, std::min<int64_t>(3, (p.c.width + 15) / 16));
+    if (choice.rows == 64 && 2 * units > slots) chunks = std::max(chunks, std::min<int64_t>({3, 6 * slots / units, (p.c.width + 15) / 16}));
   }
   p.chunk = int((p.c.width + chunks - 1) / chunks);
   p.chunks = int((p.c.width + p.chunk - 1) / p.chunk);

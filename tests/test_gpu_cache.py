@@ -497,3 +497,42 @@ def test_captured_round_replays_like_eager(tslt):
                 torch.cuda.synchronize()
                 results.append([x.clone() for x in (att["out"], att["lse"], wgh["weight"], app["length"], cache["codes"], cache["scale"])])
             assert all(torch.equal(x, y) for x, y in zip(*results)), (rep, i)
+
+
+@pytest.mark.parametrize("dtype,n,G", [("bf16", 3, 4), ("f16", 9, 4), ("f32", 40, 4)])          # the kernel for few rows, and the one for many
+def test_captured_chunks_replay_like_eager(tslt, dtype, n, G):
+    """A sequence cut into chunks that its workgroups join: every replay finds the words that the one before left, and none of its own."""
+    rng = np.random.default_rng(n)
+    D, H, lengths = 128, 1, [6000, 300, 4096]
+    host = make_cache(rng, H, D, lengths)
+    cache, pages, length = on_gpu(*host)
+    need = tslt.cache_attend_workspace_bytes(3, n, H * G, H, D, pages.shape[1])
+    assert need > 256                                             # more than one chunk
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV).fill_(1)
+    sets = [projection(np.random.default_rng(80 + i), 3, n, H * G, H, D, DTYPES[dtype]) for i in range(2)]
+    q, k, v = (x.clone() for x in sets[0][0])
+    out = {"out": torch.empty_like(q), "lse": torch.empty(3, n, H * G, device=DEV), "status": torch.empty(3, dtype=torch.int32, device=DEV)}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        tslt.cache_attend(q, cache, pages, length, k=k, v=v, out=out, workspace=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tslt.cache_attend(q, cache, pages, length, k=k, v=v, out=out, workspace=ws)
+    want = [O.attend(qh, *host, kh, vh) for _, (qh, kh, vh) in sets]
+    for rep in range(3):
+        for i in (0, 1):
+            for x, y in zip((q, k, v), sets[i][0]):
+                x.copy_(y)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            check_attend(out, want[i], DTYPES[dtype])
+            assert out["status"].tolist() == [0, 0, 0]
+            replayed = {name: x.clone() for name, x in out.items()}
+            tslt.cache_attend(q, cache, pages, length, k=k, v=v, out=out, workspace=ws)
+            torch.cuda.synchronize()
+            check_attend(out, want[i], DTYPES[dtype])
+            assert all(torch.equal(out[name], replayed[name]) for name in out)
