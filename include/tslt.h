@@ -392,7 +392,7 @@ int tslt_verify_tree(const void* target_logits, tslt_dtype dt, int64_t B, int64_
  * A cache is an array of pages of TSLT_PAGE_TOKENS tokens.  Of every page and head, `codes` holds the keys, [64 tokens][D], and
  * behind them the values, [4][D][16 tokens], as OCP e4m3 numbers, and `scales` one fp32 power of two for the keys and one for
  * the values: a number is its code times its scale.  A sequence is a row of the page table, the page of its tokens 0..63,
- * 64..127, and so on, and a length, both in device memory; no entry behind the length is read.  Keys carry their positions
+ * 64..127, and so on, and a length, both in device memory; what entries behind the length hold does not matter.  Keys carry their positions
  * in themselves, so that where a token lies means nothing.
  *   - Full pages may stand in the tables of several sequences.  A page that a sequence appends to is its own.
  *   - D (head_dim) is 64, 128 or 256; heads_q is a multiple of the cache's heads, query head i reads head i / (heads_q / heads).

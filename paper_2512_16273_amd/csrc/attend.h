@@ -409,23 +409,29 @@ struct Place {
   int64_t b;
   int h, rg, chunk, active;                // head, row group, chunk, and chunks of this sequence that hold anything
   int len, n_pages, there, rows;           // cached tokens and their pages, new tokens, rows of the head
-  bool bad_length;
+  bool bad_length, none;                   // none: there is nothing to do
 };
-// False: there is nothing to do.  Workgroups go to the eight XCDs in turn; those that differ in their rows alone read the same pages: on one
+// What its number alone says.  Workgroups go to the eight XCDs in turn; those that differ in their rows alone read the same pages: on one
 // XCD, one after the other, those of the last rows first, which see most of the new tokens.  A sequence's last chunk, which has the new tokens, comes first.
-__device__ __forceinline__ bool place_of(const AttendParams& p, Place& at) {
+__device__ __forceinline__ Place place_of(const AttendParams& p) {
+  Place at{};
   const uint32_t block = blockIdx.x, slot = block >> 3;
   const uint32_t unit = slot / uint32_t(p.row_groups) * 8 + (block & 7), heads = uint32_t(p.B * p.c.heads);
-  if (unit >= uint64_t(heads) * p.chunks) return false;
+  at.none = unit >= uint64_t(heads) * p.chunks;
   at.rg = p.row_groups - 1 - int(slot % uint32_t(p.row_groups));
   at.h = int(unit % heads % uint32_t(p.c.heads));
   at.b = int64_t(unit % heads / uint32_t(p.c.heads));
+  at.rows = p.n * p.group;
+  at.chunk = int(unit / heads);            // (from the last one on, until the length is known)
+  return at;
+}
+// The rest; false: the sequence has no such chunk.  What does not depend on lengths is asked for before this.
+__device__ __forceinline__ bool place_in_sequence(const AttendParams& p, Place& at) {
   at.len = cached_tokens(p.c, at.b, at.bad_length);
   at.n_pages = (at.len + kPage - 1) / kPage;
   at.active = max(1, (at.n_pages + p.chunk - 1) / p.chunk);
   at.there = p.count ? min(max(as_global(p.count)[at.b], 0), p.n) : p.n;
-  at.rows = p.n * p.group;
-  at.chunk = at.active - 1 - int(unit / heads);
+  at.chunk = at.active - 1 - at.chunk;
   return at.chunk >= 0;
 }
 template <typename T, int D, int RT> __device__ __forceinline__ void load_queries(const AttendParams& p, const Place& at, int first_row, Queries<T, D, RT>& q) {
@@ -442,11 +448,16 @@ template <typename T, int D, int RT> __device__ __forceinline__ void load_querie
 struct PageList {
   int page;                                // -1: outside the cache
   float k_scale, v_scale;
-  __device__ __forceinline__ bool load(const AttendParams& p, const Place& at, int first, int step, int some) {
-    const int lane = lane_id();
+  __device__ __forceinline__ void ask(const AttendParams& p, const Place& at, int first, int step, int some) {
     page = -1;
+    if (lane_id() < some) page = as_global(p.c.pages + at.b * p.c.width)[first + step * lane_id()];
+  }
+  // Returns whether any is outside the cache; `asked`: ask() has been called, for these entries and perhaps ones behind them.
+  __device__ __forceinline__ bool load(const AttendParams& p, const Place& at, int first, int step, int some, bool asked) {
+    const int lane = lane_id();
+    if (!asked) ask(p, at, first, step, some);
+    if (lane >= some) page = -1;
     k_scale = v_scale = 1.0f;
-    if (lane < some) page = as_global(p.c.pages + at.b * p.c.width)[first + step * lane];
     const bool in = page >= 0 && page < p.c.n_pages;
     const bool bad = lane < some && !in;
     if (!in) page = -1;
@@ -588,11 +599,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(co
   __shared__ int told[2];
   constexpr int KS = kStreamTurns, kRows = 16 * RT;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, g = lane >> 4, tid = int(threadIdx.x);
-  Place at;
-  if (!place_of(p, at)) return;
+  Place at = place_of(p);
+  if (at.none) return;
   const int first_row = at.rg * kRows;
   Queries<T, D, RT> q;
   load_queries(p, at, first_row, q);
+  // (a sequence in one chunk: the wave's first pages, as far as the table goes)
+  const bool early = p.chunks == 1;
+  PageList list;
+  if (early) list.ask(p, at, wave, KS, int(min<int64_t>(64, (p.c.width - wave + KS - 1) / KS)));
+  if (!place_in_sequence(p, at)) return;
   RowState<D, RT> st;
   begin(st);
 
@@ -601,8 +617,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(co
   bool bad = at.bad_length;
   for (int base = 0; base < turns; base += 64) {
     const int some = min(64, turns - base);
-    PageList list;
-    bad |= list.load(p, at, from + KS * base, KS, some);
+    bad |= list.load(p, at, from + KS * base, KS, some, early && base == 0);
     KeyTile<D> kt;
     ValueTile<D> vt;
     const uint8_t* codes = page_codes(p.c, max(0, list.page_at(0)), at.h, D);
@@ -682,10 +697,11 @@ __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_r
   constexpr int NT = NW * 64, kRows = NW * 16 * RT, kLoads = kPage * D / 16 / NT;
   static_assert(kPage * D / 16 % NT == 0, "every thread has as many pieces of a page");
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, g = lane >> 4, tid = int(threadIdx.x);
-  Place at;
-  if (!place_of(p, at)) return;
+  Place at = place_of(p);
+  if (at.none) return;
   const int first_row = at.rg * kRows + wave * 16 * RT;
   Queries<T, D, RT> q;
+  if (!place_in_sequence(p, at)) return;
   load_queries(p, at, first_row, q);
   RowState<D, RT> st;
   begin(st);
@@ -696,7 +712,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_r
   for (int base = 0; base < turns; base += 64) {
     const int some = min(64, turns - base);
     PageList list;
-    bad |= list.load(p, at, from + base, 1, some);
+    bad |= list.load(p, at, from + base, 1, some, false);
     // While page i's weights are made and meet its values, the scores of page i + 1 are: the products run beside the exponentials.  So
     // in LDS keys are a page ahead of values; in registers, on the way from memory, both are kDeep further.
     u32x4 kw[kDeep][kLoads], vw[kDeep][kLoads];
