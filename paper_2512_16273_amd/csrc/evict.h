@@ -4,7 +4,8 @@
 // rounds of counting (11, 11 and 10 bits of a key that orders as the weights do), then the tokens above it and as many equal to it
 // as are missing, the first ones, in ascending order.  The second, a workgroup to a new page, gathers their codes (moved by the first one's
 // workgroups too, a head's 1024 tokens take 42 us in all, 16 so).  Bound
-// by the latency of the counting where a cache is short, by the bytes moved where it is long.
+// by the latency of the counting where a cache is short (4096 tokens: 8 us of 16), by the bytes moved where it is long: 16 sequences of 9000 to 32768
+// tokens, 8 heads of 128, to 16001, 280 us, 30 of them the counting; the move reads and writes 1.0 GB in 250, 4 TB/s, a copy 4.9.
 #pragma once
 #include "append.h"
 

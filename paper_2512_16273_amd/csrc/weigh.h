@@ -6,7 +6,8 @@
 // registers where they are no more, and else pass by every page, RT tiles at a time.  A token's weight is added to by one wave alone, so that
 // nothing is exchanged between waves.  Bound by the bytes of the keys where the rows are few, by the products and the exponentials where they are many.
 // All pages of all sequences and heads are dealt out to one round of waves in equal shares, as sequences differ in length and the host does not know
-// how (32 sequences of 1000 to 16000 tokens, 8 heads, 36 rows: 97 us with as many workgroups to each head of each sequence, 78 so).
+// how (32 sequences of 1000 to 16000 tokens, 8 heads, 36 rows: 97 us with as many workgroups to each head of each sequence, 78 so:
+// 315 MB at 4.0 TB/s, 32 GFLOP).
 #pragma once
 #include "cache.h"
 
