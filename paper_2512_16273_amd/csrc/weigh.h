@@ -4,7 +4,8 @@
 //
 // A wave takes pages of a head one after the other, the next two's keys on their way while this one's meet the rows; the rows, RT tiles of 16, stay in
 // registers where they are no more, and else pass by every page, RT tiles at a time.  A token's weight is added to by one wave alone, so that
-// nothing is exchanged between waves.  Bound by the bytes of the keys where the rows are few, by the products and the exponentials where they are many.
+// nothing is exchanged between waves (but for the sums of four that share a page, in an order that does not change).  Bound by the bytes of the keys where the rows are few, by the products and the exponentials where they are many.
+// Where there are fewer pages than workgroups fit the GPU and many rows, a workgroup's four waves share a page and its rows.
 // All pages of all sequences and heads are dealt out to one round of waves in equal shares, as sequences differ in length and the host does not know
 // how (32 sequences of 1000 to 16000 tokens, 8 heads, 36 rows: 97 us with as many workgroups to each head of each sequence, 78 so:
 // 315 MB at 4.0 TB/s, 32 GFLOP).
@@ -46,6 +47,9 @@ template <int kHalf> __device__ __forceinline__ void fold(float (&sum)[16], int 
   }
 }
 
+// Most tiles of rows that there are registers for.
+template <typename T, int D> constexpr int weigh_tiles() { return sizeof(T) == 2 ? (D == 256 ? 2 : 4) : D == 64 ? 2 : 1; }
+
 // Pages of a sequence.
 __device__ __forceinline__ int sequence_pages(const CacheView& c, int64_t b) {
   bool bad;
@@ -55,8 +59,11 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
   return int64_t(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(x >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(x))));
 }
 
-// Pages first .. first + count - 1 of one head.
-template <typename T, int D, int RT> __device__ __forceinline__ void weigh_pages(const WeighParams& p, int64_t b, int h, int first, int count) {
+// Pages first .. first + count - 1 of one head.  kWaves = 4: for a whole workgroup, whose waves have every fourth RT tiles of rows each, the next ones on their
+// way, and hand each other their sums; turn: pages that the workgroup has done.
+template <typename T, int D, int RT, int kWaves> __device__ __forceinline__ void weigh_pages(const WeighParams& p, int64_t b, int h, int first, int count, int wave, uint32_t& turn) {
+  constexpr bool kTwo = kWaves > 1 && weigh_tiles<T, D>() >= 2 * RT;      // room for the next rows
+  __shared__ float parts[kWaves > 1 ? 2 : 1][kWaves][kPage];
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
   bool bad;
   const int len = cached_tokens(p.c, b, bad);
@@ -65,9 +72,9 @@ template <typename T, int D, int RT> __device__ __forceinline__ void weigh_pages
   const int rows = there * p.group, blocks = (rows + 16 * RT - 1) / (16 * RT);
   const int64_t weights = (b * p.c.heads + h) * p.c.width * kPage;
 
-  Queries<T, D, RT> q;
-  float off[RT];
-  const auto load_rows = [&](int from) {
+  Queries<T, D, RT> qs[kTwo ? 2 : 1];
+  float offs[kTwo ? 2 : 1][RT];
+  const auto load_rows = [&](int from, Queries<T, D, RT>& q, float (&off)[RT]) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int row = min(from + rt * 16 + r, rows - 1), token = row / p.group, head = h * p.group + row % p.group;
@@ -96,7 +103,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void weigh_pages
     load_keys(kt[1], 1);
     before[1] = load_weights(1);
     // (the rows are asked for behind the first pages: what their sums of weights are is looked at only when all are on their way)
-    if (blocks == 1 && base == 0) load_rows(0);
+    if (kWaves == 1 && blocks == 1 && base == 0) load_rows(0, qs[0], offs[0]);
     for (int i0 = 0; i0 < some; i0 += 2)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -109,8 +116,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void weigh_pages
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum[e] = 0;
         const float c = p.scale2 * as_f32(__builtin_amdgcn_readlane(as_u32(scale), i));
-        for (int block = 0; block < blocks; ++block) {
-          if (blocks > 1) load_rows(block * 16 * RT);
+        const auto meet = [&](const Queries<T, D, RT>& q, const float (&off)[RT], bool last) {
           // (half of the tokens at a time, the scores of one tile: in registers, not those of all)
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
@@ -119,7 +125,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void weigh_pages
             for (int t = 0; t < 2; ++t)
 #pragma unroll
               for (int j = 0; j < D / 32; ++j) keys[t][j] = kt[u].template operand<T>(2 * half + t, j);
-            if (half == 1 && block == blocks - 1) load_keys(kt[u], i + 2);
+            if (half == 1 && last) load_keys(kt[u], i + 2);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
               __builtin_amdgcn_sched_barrier(0);
@@ -134,23 +140,50 @@ template <typename T, int D, int RT> __device__ __forceinline__ void weigh_pages
               for (int e = 0; e < 8; ++e) sum[8 * half + e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][e & 3], c, off[rt]));
             }
           }
+        };
+        const int last = (blocks - 1 - wave) / kWaves * kWaves + wave;       // the wave's last rows (below `wave`: it has none)
+        if constexpr (kTwo) {
+          if (wave < blocks) load_rows(wave * 16 * RT, qs[0], offs[0]);
+          for (int two = wave; two < blocks; two += 2 * kWaves)
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              const int block = two + v * kWaves;
+              if (block >= blocks) break;
+              load_rows((block + kWaves) * 16 * RT, qs[v ^ 1], offs[v ^ 1]);
+              meet(qs[v], offs[v], block == last);
+            }
+        } else {
+          for (int block = wave; block < blocks; block += kWaves) {
+            if (kWaves > 1 || blocks > 1) load_rows(block * 16 * RT, qs[0], offs[0]);
+            meet(qs[0], offs[0], block == last);
+          }
         }
-        if (blocks == 0) load_keys(kt[u], i + 2);
+        if (wave >= blocks) load_keys(kt[u], i + 2);
         before[u] = load_weights(i + 2);
         __builtin_amdgcn_sched_barrier(0);
         fold<8>(sum, r);
         fold<4>(sum, r);
         fold<2>(sum, r);
         fold<1>(sum, r);
+        if constexpr (kWaves > 1) {
+          // (a page's sums in the place of those two pages ago, which wave 0 has read before it came to the barrier of the page between)
+          float(&part)[kWaves][kPage] = parts[turn++ & 1];
+          part[wave][lane] = sum[0];
+          __syncthreads();
+          if (wave != 0) continue;
+#pragma unroll
+          for (int o = 1; o < kWaves; ++o) sum[0] += part[o][lane];
+        }
         p.out_weight[weights + int64_t(at_page) * kPage + lane] = lane < valid ? had * p.decay + (pg < 0 ? 0.0f : sum[0]) : 0.0f;
       }
   }
 }
 
-template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void weigh_kernel(const WeighParams p) {
+template <typename T, int D, int RT, int kWaves> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void weigh_kernel(const WeighParams p) {
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), tid = int(threadIdx.x);
-  const int64_t waves = int64_t(gridDim.x) * 4, me = int64_t(blockIdx.x) * 4 + wave;
-  // The wave's share of all pages, counted sequence by sequence, head by head; then the sequence in which it begins.
+  const int64_t teams = int64_t(gridDim.x) * (4 / kWaves), me = kWaves > 1 ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + wave;
+  uint32_t turn = 0;
+  // The wave's, or the workgroup's, share of all pages, counted sequence by sequence, head by head; then the sequence in which it begins.
   int64_t total = 0;
   for (int64_t b0 = 0; b0 < p.B; b0 += 64) {
     int64_t n = b0 + lane < p.B ? sequence_pages(p.c, b0 + lane) : 0;
@@ -159,7 +192,7 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     total += n;
   }
   total = uniform(total) * p.c.heads;
-  const int64_t share = (total + waves - 1) / waves;
+  const int64_t share = (total + teams - 1) / teams;
   int64_t left = min(share, total - me * share), skip = me * share;
   for (int64_t b0 = 0; b0 < p.B && left > 0; b0 += 64) {
     const int n = b0 + lane < p.B ? sequence_pages(p.c, b0 + lane) : 0;
@@ -175,16 +208,16 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
       const int pages = __builtin_amdgcn_readlane(n, k);
       const int64_t in = skip - (uniform(__shfl(upto, k)) - int64_t(pages) * p.c.heads);
       const int h = int(in / pages), page = int(in % pages), count = int(min<int64_t>(left, pages - page));
-      weigh_pages<T, D, RT>(p, b0 + k, h, page, count);
+      weigh_pages<T, D, RT, kWaves>(p, b0 + k, h, page, count, kWaves > 1 ? wave : 0, turn);
       left -= count;
       skip += count;
     }
     skip -= all;
   }
   // Nothing lies behind a sequence's last page.
-  for (int64_t row = me; row < p.B * p.c.heads; row += waves) {
+  for (int64_t row = me; row < p.B * p.c.heads; row += teams) {
     float* out = p.out_weight + row * p.c.width * kPage;
-    for (int64_t i = int64_t(sequence_pages(p.c, row / p.c.heads)) * kPage + lane; i < p.c.width * kPage; i += 64) out[i] = 0;
+    for (int64_t i = int64_t(sequence_pages(p.c, row / p.c.heads)) * kPage + (kWaves > 1 ? tid : lane); i < p.c.width * kPage; i += 64 * kWaves) out[i] = 0;
   }
   if (p.status)
     for (int64_t b = blockIdx.x; b < p.B; b += gridDim.x) {
@@ -198,7 +231,5 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
       if (tid == 0) p.status[b] = bad ? kBadPage : 0;
     }
 }
-// Most tiles of rows that there are registers for.
-template <typename T, int D> constexpr int weigh_tiles() { return sizeof(T) == 2 ? (D == 256 ? 2 : 4) : D == 64 ? 2 : 1; }
 
 }  // namespace tslt

@@ -243,6 +243,26 @@ def test_weights_are_those_of_the_attention(tslt, dtype, D, H, G, n, lengths, de
         assert np.all(total.cpu().numpy() <= count.cpu().numpy() * H * G * (1 + 1e-4))
 
 
+@pytest.mark.parametrize("dtype,D,H,G,n,lengths", [("bf16", 128, 2, 4, 41, [64, 700, 0, 1]), ("f32", 128, 1, 8, 37, [130, 65, 7, 640]),
+                                                   ("f16", 256, 2, 2, 90, [1, 200, 64, 128]), ("f32", 64, 1, 1, 150, [70, 3, 0, 129]),
+                                                   ("f32", 256, 1, 3, 47, [90, 64, 1, 300]), ("bf16", 64, 3, 1, 333, [127, 64, 300, 9])])
+def test_weights_of_many_rows_on_few_pages(tslt, dtype, D, H, G, n, lengths):
+    rng = np.random.default_rng([D, n, 5])
+    B = len(lengths)
+    host = make_cache(rng, H, D, lengths, spare=1)
+    cache, pages, length = on_gpu(*host)
+    (q, k, v), (qh, kh, vh) = projection(rng, B, n, H * G, H, D, DTYPES[dtype])
+    for counts in ([n, n - 1, 1, n], [0, n, 17, 33]):             # (of few of them some waves have none)
+        count = torch.tensor(counts, dtype=torch.int32, device=DEV)
+        att = tslt.cache_attend(q, cache, pages, length, k=k, v=v, count=count)
+        weight = torch.rand(B, H, pages.shape[1] * 64, device=DEV)
+        got = tslt.cache_weigh(q, att["lse"], cache, pages, length, weight, decay=0.7, count=count)
+        torch.cuda.synchronize()
+        check_weigh(got, O.weigh(qh, att["lse"].double().cpu().numpy(), *host, weight.cpu().numpy(), 0.7, count.cpu().numpy()), weight)
+        again = tslt.cache_weigh(q, att["lse"], cache, pages, length, weight, decay=0.7, count=count)
+        assert torch.equal(again["weight"], got["weight"]) and not got["status"].any()
+
+
 def same_values(got, want, table, length, H):
     """Codes as the numbers they stand for, wherever there is a token; scales bit for bit."""
     for b, L in enumerate(length):
