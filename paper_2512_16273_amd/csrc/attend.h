@@ -10,8 +10,8 @@
 //   attend_stream_kernel, few rows: bound by memory (4 sequences of 131000 tokens, 8 heads of 128, 4 rows: 172 us, 1029 MB at 6.0 TB/s; a large read runs at 7.0).  Codes go from memory straight into the operand registers of the products (the
 //     order in which the cache holds them is made for that).  A workgroup's four waves have the same rows and take pages in turn.
 //   attend_rows_kernel, many rows: bound by the products and the exponentials.  A workgroup brings a page to LDS once, as operands, for
-//     all of its waves, each with rows of its own (2048 bfloat16 tokens on 16000, 32 heads of 128 on 8: 834 us, 571 GFLOP by the formula at 685
-//     TFLOP/s, 1030 with the weights' second term; a large matrix product runs at 1200.  It is 3.5 vector instructions a product that keep it from that).
+//     all of its waves, each with rows of its own (2048 bfloat16 tokens on 16000, 32 heads of 128 on 8: 797 us, 571 GFLOP by the formula at 717
+//     TFLOP/s, 1075 with the weights' second term; a large matrix product runs at 1200.  It is 3.5 vector instructions a product that keep it from that).
 // A sequence is cut into chunks of pages where its rows alone do not fill the GPU; whichever of its workgroups ends last joins them.
 //
 // Rounding.  Codes, and queries of 16 bits, enter the first product exactly; queries of 32 bits as three bfloat16 terms,
@@ -93,56 +93,78 @@ struct FreshShared {
   int odd;                                 // a value that is not finite has been left out
 };
 
-// Brings 64 new tokens from j0 on to LDS, zeros where there are fewer.  A value that is not finite is left out (0), and that it was
-// noted: a product would carry it to rows that do not see the token, as 0 times it (see add_odd_values).
-template <typename T, int D, int NT>
-__device__ __forceinline__ void stage_fresh(const AttendParams& p, int64_t b, int h, int j0, int there, uint8_t* lds, FreshShared& sh) {
+// 64 new tokens from j0 on, on their way from memory to LDS in the registers of NT threads; zeros where there are fewer.  A value that is not finite is left out (0), and
+// that it was noted: a product would carry it to rows that do not see the token, as 0 times it (see add_odd_values).
+template <typename T, int D, int NT, bool kHold> struct FreshTile {
   typedef Staged<T, D> F;
-  const int tid = int(threadIdx.x);
-  const T* kp = reinterpret_cast<const T*>(p.k.data) + b * p.k.seq + h * p.k.head;
-  const T* vp = reinterpret_cast<const T*>(p.v.data) + b * p.v.seq + h * p.v.head;
-  constexpr int kChunks = D / F::kPer;
-#pragma unroll 4
-  for (int it = 0; it < kPage * kChunks / NT; ++it) {
-    const int idx = it * NT + tid, chunk = idx % kChunks, token = idx / kChunks;
-    u32x4 w = load16(kp + min(j0 + token, there - 1) * p.k.token + chunk * F::kPer);
-    if (j0 + token >= there) w = u32x4{0, 0, 0, 0};
-    *reinterpret_cast<u32x4*>(lds + F::key_at(chunk, Tile::place(token))) = w;
+  static constexpr int kWide = F::kBytes == 4 ? 1 : 2;   // channels of a value to a thread: a word
+  static constexpr int kChunks = D / F::kPer, kKeys = kPage * kChunks / NT, kValues = (8 * (D / kWide) + NT - 1) / NT;
+  static constexpr bool kAll = 8 * (D / kWide) % NT == 0;
+  // 16 bits, many rows: the next tile is asked for before this one is met (46 sequences, 8 heads of 128, 319 tokens on some 30: 128 us without, 89 so).  fp32, whose rows and
+  // terms leave no registers, and few rows, which seldom have a second tile: read when it is put there, a few at a time.
+  static constexpr bool kHeld = kHold && F::kBytes == 2;
+  u32x4 k[kHeld ? kKeys : 1];
+  uint32_t v[kHeld ? kValues : 1][8];
+  __device__ __forceinline__ static u32x4 keys(const AttendParams& p, int64_t b, int h, int j0, int there, int it) {
+    const int idx = it * NT + int(threadIdx.x), chunk = idx % kChunks, token = idx / kChunks;
+    return load16(reinterpret_cast<const T*>(p.k.data) + b * p.k.seq + h * p.k.head + min(j0 + token, there - 1) * p.k.token + chunk * F::kPer);
   }
-  constexpr int kWide = F::kBytes == 4 ? 1 : 2;          // channels to a thread: a word
-#pragma unroll 2
-  for (int it = 0; it < (8 * (D / kWide) + NT - 1) / NT; ++it) {
-    const int idx = it * NT + tid, at = idx % (D / kWide), eight = idx / (D / kWide);
-    if (8 * (D / kWide) % NT != 0 && eight >= 8) continue;
-    uint32_t w[8];
+  __device__ __forceinline__ static void values(const AttendParams& p, int64_t b, int h, int j0, int there, int it, uint32_t (&w)[8]) {
+    const int idx = it * NT + int(threadIdx.x), at = idx % (D / kWide), eight = idx / (D / kWide) & 7;
+    const T* vp = reinterpret_cast<const T*>(p.v.data) + b * p.v.seq + h * p.v.head;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int token = j0 + eight * 8 + e;
-      w[e] = *as_global(reinterpret_cast<const uint32_t*>(vp + min(token, there - 1) * p.v.token + at * kWide));
-      if (token >= there) w[e] = 0;
+    for (int e = 0; e < 8; ++e) w[e] = *as_global(reinterpret_cast<const uint32_t*>(vp + min(j0 + eight * 8 + e, there - 1) * p.v.token + at * kWide));
+  }
+  __device__ __forceinline__ void load(const AttendParams& p, int64_t b, int h, int j0, int there) {
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int it = 0; it < kKeys; ++it) k[it] = keys(p, b, h, j0, there, it);
+#pragma unroll
+      for (int it = 0; it < kValues; ++it) values(p, b, h, j0, there, it, v[it]);
+    }
+  }
+  __device__ __forceinline__ void put(const AttendParams& p, int64_t b, int h, int j0, int there, uint8_t* lds, FreshShared& sh) const {
+    const int tid = int(threadIdx.x);
+    constexpr int kKeysAtOnce = kHeld ? kKeys : 4, kValuesAtOnce = kHeld ? kValues : 2;
+#pragma unroll kKeysAtOnce
+    for (int it = 0; it < kKeys; ++it) {
+      const int idx = it * NT + tid, chunk = idx % kChunks, token = idx / kChunks;
+      u32x4 w;
+      if constexpr (kHeld) w = k[it];
+      else w = keys(p, b, h, j0, there, it);
+      *reinterpret_cast<u32x4*>(lds + F::key_at(chunk, Tile::place(token))) = j0 + token < there ? w : u32x4{0, 0, 0, 0};
     }
     bool odd = false;
+#pragma unroll kValuesAtOnce
+    for (int it = 0; it < kValues; ++it) {
+      const int idx = it * NT + tid, at = idx % (D / kWide), eight = idx / (D / kWide);
+      if (!kAll && eight >= 8) continue;
+      uint32_t w[8];
+      if constexpr (!kHeld) values(p, b, h, j0, there, it, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (not_finite<T>(w[e])) { odd = true; w[e] = kWide == 1 ? 0 : w[e] & 0xFFFF0000u; }
-      if (kWide == 2 && not_finite<T>(w[e] >> 16)) { odd = true; w[e] &= 0xFFFFu; }
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (kHeld) w[e] = v[it][e];
+        if (j0 + eight * 8 + e >= there) w[e] = 0;
+        if (not_finite<T>(w[e])) { odd = true; w[e] = kWide == 1 ? 0 : w[e] & 0xFFFF0000u; }
+        if (kWide == 2 && not_finite<T>(w[e] >> 16)) { odd = true; w[e] &= 0xFFFFu; }
+      }
+      if constexpr (kWide == 1) {
+        *reinterpret_cast<u32x4*>(lds + F::value_at(eight, 0, at)) = u32x4{w[0], w[1], w[2], w[3]};
+        *reinterpret_cast<u32x4*>(lds + F::value_at(eight, 1, at)) = u32x4{w[4], w[5], w[6], w[7]};
+      } else {
+        u32x4 a, c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[e] = (w[2 * e] & 0xFFFFu) | w[2 * e + 1] << 16;
+          c[e] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xFFFF0000u);
+        }
+        *reinterpret_cast<u32x4*>(lds + F::value_at(eight, 0, 2 * at)) = a;
+        *reinterpret_cast<u32x4*>(lds + F::value_at(eight, 0, 2 * at + 1)) = c;
+      }
     }
     if (odd) sh.odd = 1;
-    if constexpr (kWide == 1) {
-      *reinterpret_cast<u32x4*>(lds + F::value_at(eight, 0, at)) = u32x4{w[0], w[1], w[2], w[3]};
-      *reinterpret_cast<u32x4*>(lds + F::value_at(eight, 1, at)) = u32x4{w[4], w[5], w[6], w[7]};
-    } else {
-      u32x4 a, c;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        a[e] = (w[2 * e] & 0xFFFFu) | w[2 * e + 1] << 16;
-        c[e] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xFFFF0000u);
-      }
-      *reinterpret_cast<u32x4*>(lds + F::value_at(eight, 0, 2 * at)) = a;
-      *reinterpret_cast<u32x4*>(lds + F::value_at(eight, 0, 2 * at + 1)) = c;
-    }
   }
-}
+};
 
 // What a wave keeps for its rows: of row r of each tile the running maximum, the lane's part of the sum of weights, and of channels 16 d + 4 g .. + 3 the sums.
 template <int D, int RT> struct RowState {
@@ -233,6 +255,13 @@ template <int N> __device__ __forceinline__ void split_weight(float x, int i, bf
 // Vector instructions and matrix products stay in the order in which they are written down; memory's may move.
 __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x3F4); }
 
+// f(kFrom), f(kFrom + 1) .. f(kTo - 1), written out by a few at a time: the compiler gives up on a loop of many, and indexes registers by numbers that it does not
+// know (fp32, D = 256, 700 tokens of 4 sequences on 100 to 900, 16 heads on 4: 6750 us so, 420 written out).
+template <int kFrom, int kTo, typename F> __device__ __forceinline__ void in_parts(const F& f) {
+#pragma unroll
+  for (int n = kFrom; n < (kTo < kFrom + 16 ? kTo : kFrom + 16); ++n) f(n);
+  if constexpr (kTo > kFrom + 16) in_parts<kFrom + 16, kTo>(f);
+}
 // A page's scores into weights, these and its values into the rows' sums, and beside that, the scores of the page after it, so that the products
 // run while the exponentials are made.  keys(t, i): operand of instruction t and step i of the next page; values(d, k): of this page's channels 16 d ..
 // and the k-th eight of the lane's 16 tokens; each is asked for kAhead operands before it is met.  The order is written out: a product, then a
@@ -262,22 +291,20 @@ __device__ __forceinline__ void page_round(const Queries<T, D, RT>& q, f32x4 (&s
   };
 #pragma unroll
   for (int f = 0; f < kAhead; ++f) ask(f);
-#pragma unroll
-  for (int n = 0; n < kScores; ++n) {
+  in_parts<0, kScores>([&](int n) __attribute__((always_inline)) {
     const int rt = n % RT, e = n / RT % kTerms, f = n / (RT * kTerms), t = f % 4, i = f / 4;
     if (n % (RT * kTerms) == 0) ask(f + kAhead);
     next[rt][t] = mfma(key[f % kRing], q.v[rt][i][e], i == 0 && e == 0 ? f32x4{0, 0, 0, 0} : next[rt][t]);
     if ((n + 1) * kElements / kScores > n * kElements / kScores) weight(0, n * kElements / kScores);
     keep_order();
-  }
-#pragma unroll
-  for (int n = 0; n < 2 * kValues; ++n) {
+  });
+  in_parts<0, 2 * kValues>([&](int n) __attribute__((always_inline)) {
     const int k = n / kValues, rt = n % RT, e = n / RT % kW, f = n / (RT * kW), d = f % kHalf;
     if (n % (RT * kW) == 0) ask(kKeys + f + kAhead);
     st.o[rt][d] = mfma(value[f % kRing], w[rt][k][e], st.o[rt][d]);
     if (k == 0 && (n + 1) * kElements / kValues > n * kElements / kValues) weight(1, n * kElements / kValues);
     keep_order();
-  }
+  });
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     st.l[rt] += sum[rt];
@@ -333,7 +360,7 @@ __device__ __forceinline__ uint32_t seen_of(const AttendParams& p, const uint32_
 }
 
 // The call's own tokens, all of them that the wave's rows see, tile after tile; `turns` waves that share rows take turns.
-template <typename T, int D, int RT, int NT>
+template <typename T, int D, int RT, int NT, bool kHold>
 __device__ __forceinline__ void attend_fresh(const AttendParams& p, int64_t b, int h, int first_row, int last_row, int there, int turns, int my_turn,
                                              const Queries<T, D, RT>& q, RowState<D, RT>& st, uint8_t* lds, FreshShared& sh) {
   typedef Staged<T, D> F;
@@ -342,6 +369,8 @@ __device__ __forceinline__ void attend_fresh(const AttendParams& p, int64_t b, i
   const uint32_t* mask = p.mask ? p.mask + b * p.mask_seq : nullptr;
   // (a token sees none behind itself where there is no mask: tiles behind the workgroup's last row's token are not looked at)
   const int reach = mask ? there : min(there, last_row / p.group + 1);
+  FreshTile<T, D, NT, kHold> tile;
+  tile.load(p, b, h, 0, there);
   for (int j0 = 0, turn = 0; j0 < reach; j0 += kPage, ++turn) {
     uint32_t seen[RT];                     // (a bit to each of the lane's scores)
     bool mine = false;
@@ -353,8 +382,10 @@ __device__ __forceinline__ void attend_fresh(const AttendParams& p, int64_t b, i
     const bool any = ballot(mine) != 0;
     if (any && lane == 0) sh.wanted[turn & 1] = turn + 1;
     __syncthreads();                       // (also: what was staged before has been read)
-    if (sh.wanted[turn & 1] != turn + 1) continue;
-    stage_fresh<T, D, NT>(p, b, h, j0, there, lds, sh);
+    const bool wanted = sh.wanted[turn & 1] == turn + 1;
+    if (wanted) tile.put(p, b, h, j0, there, lds, sh);
+    if (j0 + kPage < reach) tile.load(p, b, h, j0 + kPage, there);
+    if (!wanted) continue;
     __syncthreads();
     if (!any || turn % turns != my_turn) continue;
     f32x4 s[RT][4];
@@ -643,7 +674,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(co
   if (fresh) {
     if (tid == 0) sh.wanted[0] = sh.wanted[1] = sh.odd = 0;
     __syncthreads();
-    attend_fresh<T, D, RT, 256>(p, at.b, at.h, first_row, min(at.rows, first_row + kRows) - 1, at.there, KS, wave, q, st, lds, sh);
+    attend_fresh<T, D, RT, 256, false>(p, at.b, at.h, first_row, min(at.rows, first_row + kRows) - 1, at.there, KS, wave, q, st, lds, sh);
   }
 
   // The waves' parts meet in LDS.
@@ -795,7 +826,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_r
   if (fresh) {
     if (tid == 0) sh.wanted[0] = sh.wanted[1] = sh.odd = 0;
     __syncthreads();
-    attend_fresh<T, D, RT, NT>(p, at.b, at.h, first_row, min(at.rows, (at.rg + 1) * kRows) - 1, at.there, 1, 0, q, st, lds, sh);
+    attend_fresh<T, D, RT, NT, true>(p, at.b, at.h, first_row, min(at.rows, (at.rg + 1) * kRows) - 1, at.there, 1, 0, q, st, lds, sh);
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
