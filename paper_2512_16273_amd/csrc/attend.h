@@ -7,11 +7,11 @@
 // keys, so the products are dense in tiles of 16 rows, and one pass keeps a running maximum m and sum l for each row.
 //
 // One wave takes 64 keys at a time against tiles of 16 rows (see Tile), in two kernels:
-//   attend_stream_kernel, few rows: bound by memory (4 sequences of 131000 tokens, 8 heads of 128, 4 rows: 172 us, 1029 MB at 6.0 TB/s; a large read runs at 7.0).  Codes go from memory straight into the operand registers of the products (the
+//   attend_stream_kernel, few rows: bound by memory (4 sequences of 131000 tokens, 8 heads of 128, 4 rows: 173 us, 1029 MB at 5.9 TB/s; a large read runs at 7.0).  Codes go from memory straight into the operand registers of the products (the
 //     order in which the cache holds them is made for that).  A workgroup's four waves have the same rows and take pages in turn.
 //   attend_rows_kernel, many rows: bound by the products and the exponentials.  A workgroup brings a page to LDS once, as operands, for
-//     all of its waves, each with rows of its own (2048 bfloat16 tokens on 16000, 32 heads of 128 on 8: 797 us, 571 GFLOP by the formula at 717
-//     TFLOP/s, 1075 with the weights' second term; a large matrix product runs at 1200.  It is 3.5 vector instructions a product that keep it from that).
+//     all of its waves, each with rows of its own (2048 bfloat16 tokens on 16000, 32 heads of 128 on 8: 800 us, 571 GFLOP by the formula at 714
+//     TFLOP/s, 1071 with the weights' second term; a large matrix product runs at 1200.  It is 3.5 vector instructions a product that keep it from that).
 // A sequence is cut into chunks of pages where its rows alone do not fill the GPU; whichever of its workgroups ends last joins them.
 //
 // Rounding.  Codes, and queries of 16 bits, enter the first product exactly; queries of 32 bits as three bfloat16 terms,
