@@ -26,18 +26,20 @@ struct EvictParams {
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64, kEvictBins = 2048;
 
-// Larger weight, larger key; NaN below everything.
-__device__ __forceinline__ uint32_t weight_key(float w) { return w != w ? 0u : mono_key(w + 0.0f); }
+// Larger weight, larger key; NaN below everything, and no token has key 0.
+constexpr uint32_t kKeyNan = 1u, kKeyNoToken = 0u;
+__device__ __forceinline__ uint32_t weight_key(float w) { return w != w ? kKeyNan : mono_key(w + 0.0f); }
 
-// The keys of the weights that a wave has a stretch of: kHeld to a lane in registers, or (kHeld = 0) made from memory every time.  Places behind
-// the last token have the least key: they come after every token that may have it too, and as many tokens as are looked for there are.
+// The keys of the weights that a wave has a stretch of: kHeld to a lane in registers, or (kHeld = 0) made from memory every time.  Places behind a
+// stretch's last token (its last 256 are looked at together, and every stretch but the last may end inside them) have a key below every token's: as
+// many tokens as are looked for there are, so the least key that stays is a token's and no such place is ever counted or kept.
 template <int kHeld> struct Stretch {
   uint32_t key[kHeld > 0 ? kHeld : 1];
   const float* from;
   int lo, hi;                              // tokens of the stretch
   // (read whether or not there is one, the last one instead: so all are on their way at the same time)
   __device__ __forceinline__ float read(int i0) const { return as_global(from)[max(0, min(i0 + lane_id(), hi - 1))]; }
-  __device__ __forceinline__ uint32_t made(float w, int i0) const { return lane_id() < hi - i0 ? weight_key(w) : 0u; }
+  __device__ __forceinline__ uint32_t made(float w, int i0) const { return lane_id() < hi - i0 ? weight_key(w) : kKeyNoToken; }
   __device__ __forceinline__ void load(const float* weight, int first, int last) {
     from = weight;
     lo = first;

@@ -1,0 +1,54 @@
+"""The calls around the 8-bit cache where numbers are not finite, sequences are long or tables wide: values that the cases of
+test_gpu_cache.py do not hold and paths that their sizes do not reach.  Tolerances are that file's."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as O
+from tests.test_gpu_cache import DEV, make_cache, on_gpu, same_values
+
+pytestmark = pytest.mark.gpu
+
+
+def weights_with_nan(rng, B, H, tokens, kind):
+    weight = rng.random((B, H, tokens)).astype(np.float32) ** 4
+    if kind == "all":
+        weight[:] = np.nan
+    elif kind == "late":
+        weight[:, :, 3 * tokens // 4:] = np.nan
+    elif kind == "third":
+        weight[rng.random(weight.shape) < 0.33] = np.nan
+        weight[rng.random(weight.shape) < 0.1] = -np.inf
+    else:
+        weight[rng.random(weight.shape) < 0.6] = np.nan
+    return weight
+
+
+# (tables of up to 64 and 512 pages: weights' keys in registers, four or 32 to a lane; of more: from memory every time)
+@pytest.mark.parametrize("D,H,lengths,keep,recent,width", [(64, 2, [100, 128, 70], 90, 0, 2), (64, 1, [990, 1000, 130], 890, 0, 16),
+                                                           (128, 2, [1000, 300], 999, 7, 65), (64, 1, [5000, 700], 4900, 0, 79),
+                                                           (64, 2, [1000, 130], 900, 0, 513), (64, 1, [5000, 700], 4900, 11, 700)])
+@pytest.mark.parametrize("kind", ["all", "late", "third", "most"])
+def test_evict_keeps_the_first_of_the_weights_that_are_nan(tslt, D, H, lengths, keep, recent, width, kind):
+    """Weights that are NaN and have to stay, in stretches of more waves than one: the first of them, each once, in order."""
+    rng = np.random.default_rng([D, keep, recent, len(kind)])
+    B = len(lengths)
+    codes, scale, tables, length = make_cache(rng, H, D, lengths)
+    tables = np.concatenate([tables, np.full((B, width - tables.shape[1]), -1, np.int32)], 1)
+    W, first = -(-keep // 64), codes.shape[0]
+    codes = np.concatenate([codes, np.full((B * W,) + codes.shape[1:], 127, np.uint8)])
+    scale = np.concatenate([scale, np.full((B * W,) + scale.shape[1:], 1e30, np.float32)])
+    new = (first + rng.permutation(B * W)).reshape(B, W).astype(np.int32)
+    weight = weights_with_nan(rng, B, H, tables.shape[1] * 64, kind)
+    if kind == "late":
+        for b, x in enumerate(lengths):
+            weight[b, :, 3 * x // 4:] = np.nan
+    cache, pages, lens = on_gpu(codes, scale, tables, length)
+    got = tslt.cache_evict(cache, pages, lens, torch.from_numpy(weight).to(DEV), keep, recent, torch.from_numpy(new).to(DEV))
+    torch.cuda.synchronize()
+    want = O.evict(codes, scale, tables, length, weight, keep, recent, new)
+    assert got["status"].tolist() == [0] * B
+    assert np.array_equal(got["length"].cpu().numpy(), want[2])
+    assert np.array_equal(got["kept"].cpu().numpy(), want[3])
+    assert np.array_equal(got["weight"].cpu().numpy(), want[4], equal_nan=True)
+    same_values((cache["codes"].cpu().numpy(), cache["scale"].cpu().numpy()), want[:2], new, want[2], H)
