@@ -548,8 +548,9 @@ template <typename T, int D, int NT, int kRows> __device__ __forceinline__ void 
       const int64_t to = (at.b * p.n + i) * p.heads_q + at.h * p.group + row % p.group;
       for (int e = 0; e < 2; ++e)
         if (odd[e] != 0) {
+          // (a row that is NaN without them stays NaN)
           if constexpr (sizeof(T) == 4) reinterpret_cast<float*>(p.out)[to * D + d + e] += odd[e];
-          else reinterpret_cast<uint16_t*>(p.out)[to * D + d + e] = odd_bits<T>(odd[e]);
+          else if (!__builtin_isnan(load_elem<T>(reinterpret_cast<const T*>(p.out), to * D + d + e))) reinterpret_cast<uint16_t*>(p.out)[to * D + d + e] = odd_bits<T>(odd[e]);
         }
     }
   }

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import cache_oracle as O
-from tests.test_gpu_cache import DEV, make_cache, on_gpu, same_values
+from tests.test_gpu_cache import DEV, DTYPES, make_cache, on_gpu, projection, same_values
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,28 @@ def test_evict_keeps_the_first_of_the_weights_that_are_nan(tslt, D, H, lengths, 
     assert np.array_equal(got["kept"].cpu().numpy(), want[3])
     assert np.array_equal(got["weight"].cpu().numpy(), want[4], equal_nan=True)
     same_values((cache["codes"].cpu().numpy(), cache["scale"].cpu().numpy()), want[:2], new, want[2], H)
+
+
+# (one chunk and several; the kernel for few rows and the one for many)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,G,length", [(3, 2, 70), (3, 2, 6000), (40, 4, 70), (40, 4, 6000)])
+def test_a_row_that_is_nan_stays_nan_where_it_sees_an_infinity(tslt, dtype, n, G, length):
+    rng = np.random.default_rng([n, length])
+    D, H = 64, 2
+    codes, scale, tables, lengths = make_cache(rng, H, D, [length])
+    codes[tables[0, 0], 1, 1].reshape(4, D, 16)[0, 9, 3] = 127      # a cached value of head 1: its rows are NaN in channel 9
+    cache, pages, lens = on_gpu(codes, scale, tables, lengths)
+    (q, k, v), _ = projection(rng, 1, n, H * G, H, D, DTYPES[dtype])
+    v[0, 0, :, 9], v[0, 0, :, 5] = float("inf"), -float("inf")      # token 0 is seen by all
+    q[0, n - 1, 0] = float("nan")
+    assert (tslt.cache_attend_workspace_bytes(1, n, H * G, H, D, pages.shape[1]) > 0) == (length > 1000)
+    got = tslt.cache_attend(q, cache, pages, lens, k=k, v=v)
+    torch.cuda.synchronize()
+    out = got["out"].float().cpu()
+    assert out[0, n - 1, 0].isnan().all() and got["lse"][0, n - 1, 0].isnan()
+    rest = torch.ones(n, H * G, dtype=torch.bool)
+    rest[n - 1, 0] = False
+    assert (out[0, :, G:, 9]).isnan().all()
+    assert (out[0, :, :G, 9][rest[:, :G]] == float("inf")).all() and (out[0][..., 5][rest] == -float("inf")).all()
+    fine = [d for d in range(D) if d not in (5, 9)]
+    assert out[0][rest][:, fine].isfinite().all()
