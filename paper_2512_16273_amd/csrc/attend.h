@@ -556,6 +556,15 @@ template <typename T, int D, int NT, int kRows> __device__ __forceinline__ void 
   }
 }
 
+// A chunk's sum of values in units of another maximum.  A weight is positive, also one that is 0 in these units: a sum that its chunk's seen values have
+// made infinite stays infinite.
+__device__ __forceinline__ f32x4 in_units(f32x4 o, float f) {
+  f32x4 x = o * f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = __builtin_isinf(o[e]) ? o[e] : x[e];
+  return x;
+}
+
 // All threads of a workgroup that has given its rows: the last one of a sequence's chunks joins them, and says how the sequence's pages were.
 template <typename T, int D, int NT, int kRows>
 __device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, bool bad, int (&told)[2]) {
@@ -598,7 +607,7 @@ __device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, boo
           const float mu = as_f32(uint32_t(ml[u])), most = fmaxf(m, mu);
           const float f = exp2_fast(m - most), fu = exp2_fast(mu - most);
           l = l * f + as_f32(uint32_t(ml[u] >> 32)) * fu;
-          o = o * f + f32x4{as_f32(uint32_t(x[u][0])), as_f32(uint32_t(x[u][0] >> 32)), as_f32(uint32_t(x[u][1])), as_f32(uint32_t(x[u][1] >> 32))} * fu;
+          o = in_units(o, f) + in_units(f32x4{as_f32(uint32_t(x[u][0])), as_f32(uint32_t(x[u][0] >> 32)), as_f32(uint32_t(x[u][1])), as_f32(uint32_t(x[u][1] >> 32))}, fu);
           m = most;
         }
     }

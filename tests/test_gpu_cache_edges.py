@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import cache_oracle as O
-from tests.test_gpu_cache import DEV, DTYPES, make_cache, on_gpu, projection, same_values
+from tests.test_gpu_cache import DEV, DTYPES, check_attend, make_cache, on_gpu, projection, same_values
 
 pytestmark = pytest.mark.gpu
 
@@ -77,3 +77,36 @@ def test_a_row_that_is_nan_stays_nan_where_it_sees_an_infinity(tslt, dtype, n, G
     assert (out[0, :, :G, 9][rest[:, :G]] == float("inf")).all() and (out[0][..., 5][rest] == -float("inf")).all()
     fine = [d for d in range(D) if d not in (5, 9)]
     assert out[0][rest][:, fine].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,G,length", [(3, 2, 70), (3, 2, 6000), (40, 4, 70), (40, 4, 6000)])
+@pytest.mark.parametrize("apart", [0, 200])
+def test_infinities_are_the_same_in_one_chunk_and_in_several(tslt, dtype, n, G, length, apart):
+    """New tokens with infinite values whose scores lie as high as the cached ones', or, with the whole chunk they are in, so far below them
+    (2 * 200 / ln 2 powers of two) that fp32 holds no weight for them: a weight is positive all the same."""
+    rng = np.random.default_rng([n, length, apart])
+    D, H = 64, 2
+    codes, scale, tables, lengths = make_cache(rng, H, D, [length])
+    scale[..., 0] = 1.0
+    for w, page in enumerate(tables[0]):                            # keys: 1 in the first half of the cache, -1 behind it, in channel 0 alone
+        codes[page, :, 0] = 0
+        codes[page, :, 0].reshape(H, 64, D)[..., 0] = 0x38 if 2 * w < len(tables[0]) or length < 100 else 0xB8
+    cache, pages, lens = on_gpu(codes, scale, tables, lengths)
+    (q, k, v), _ = projection(rng, 1, n, H * G, H, D, DTYPES[dtype])
+    q[..., 0], q[..., 1:] = apart, 0
+    k[..., 0] = -1
+    qh, kh, vh = (t.double().cpu().numpy() for t in (q, k, v))
+    v[0, 0, :, 5], v[0, 1, 1, 8] = float("inf"), -float("inf")
+    v[0, 0, 0, 9], v[0, 1, 0, 9] = float("inf"), -float("inf")      # which add up to NaN
+    got = tslt.cache_attend(q, cache, pages, lens, k=k, v=v, scale=1.0)
+    torch.cuda.synchronize()
+    out = got["out"].float().cpu()
+    assert (out[0, :, :, 5] == float("inf")).all()
+    assert (out[0, 1:, G:, 8] == -float("inf")).all() and out[0, 0, G:, 8].isfinite().all() and out[0, :, :G, 8].isfinite().all()
+    assert (out[0, 0, :G, 9] == float("inf")).all() and out[0, 1:, :G, 9].isnan().all() and out[0, :, G:, 9].isfinite().all()
+    want = O.attend(qh, codes, scale, tables, lengths, kh, vh, softmax_scale=1.0)
+    for where in (np.s_[0, :, :, 5], np.s_[0, 1:, G:, 8], np.s_[0, :, :G, 9]):
+        got["out"][where] = torch.from_numpy(want[0][where]).to(DEV).to(got["out"].dtype)
+        want[0][where] = got["out"][where].double().cpu().numpy()
+    check_attend(got, want, DTYPES[dtype])
