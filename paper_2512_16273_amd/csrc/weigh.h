@@ -136,8 +136,11 @@ template <typename T, int D, int RT, int kWaves> __device__ __forceinline__ void
                 for (int e = 0; e < Operand<T>::kTerms; ++e)
 #pragma unroll
                   for (int t = 0; t < 2; ++t) s[t] = mfma(keys[t][j], q.v[rt][j][e], s[t]);
+              // (a row that saw nothing, and one that is not there, may hold anything: its scores are not looked at)
+              if (off[rt] != -INFINITY) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) sum[8 * half + e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][e & 3], c, off[rt]));
+                for (int e = 0; e < 8; ++e) sum[8 * half + e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][e & 3], c, off[rt]));
+              }
             }
           }
         };

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import cache_oracle as O
-from tests.test_gpu_cache import DEV, DTYPES, check_attend, make_cache, on_gpu, projection, same_values
+from tests.test_gpu_cache import DEV, DTYPES, check_attend, check_weigh, make_cache, on_gpu, projection, same_values
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,48 @@ def test_infinities_are_the_same_in_one_chunk_and_in_several(tslt, dtype, n, G, 
         got["out"][where] = torch.from_numpy(want[0][where]).to(DEV).to(got["out"].dtype)
         want[0][where] = got["out"][where].double().cpu().numpy()
     check_attend(got, want, DTYPES[dtype])
+
+
+# (few rows; more than there are registers for; many rows on few pages, two sets of rows in registers and one)
+WEIGH = [("bf16", 128, 2, 4, 9, [64, 700, 1, 130]), ("f32", 64, 1, 1, 5, [150, 65, 300, 7]), ("f16", 64, 8, 3, 30, [3000, 2000, 4096, 70]),
+         ("bf16", 128, 2, 4, 41, [64, 700, 90, 1]), ("f32", 256, 1, 3, 47, [90, 64, 1, 300]), ("f16", 256, 1, 2, 90, [1, 200, 64, 128])]
+
+
+@pytest.mark.parametrize("dtype,D,H,G,n,lengths", WEIGH)
+@pytest.mark.parametrize("odd", [float("nan"), float("inf")])
+def test_rows_that_saw_nothing_add_nothing_whatever_they_hold(tslt, dtype, D, H, G, n, lengths, odd):
+    """cache_weigh without the count that cache_attend was given: the rows behind it have -inf."""
+    rng = np.random.default_rng([D, n, H])
+    B = len(lengths)
+    codes, scale, tables, length = make_cache(rng, H, D, lengths)
+    codes[tables[3, 0], 0, 0, 5] = 127                              # a key of the sequence whose rows all are such
+    cache, pages, lens = on_gpu(codes, scale, tables, length)
+    (q, k, v), (qh, kh, vh) = projection(rng, B, n, H * G, H, D, DTYPES[dtype])
+    counts = np.array([n - 2, 1, n, 0], np.int32)
+    count = torch.from_numpy(counts).to(DEV)
+    for b, m in enumerate(counts):
+        q[b, m:] = odd
+    att = tslt.cache_attend(q, cache, pages, lens, k=k, v=v, count=count)
+    weight = torch.rand(B, H, pages.shape[1] * 64, device=DEV)
+    for given in (None, count):
+        got = tslt.cache_weigh(q, att["lse"], cache, pages, lens, weight, decay=0.5, count=given)
+        torch.cuda.synchronize()
+        assert torch.equal(got["weight"][3, :, :lengths[3]], weight[3, :, :lengths[3]] * 0.5)
+        codes[tables[3, 0], 0, 0, 5] = 0                            # (the oracle multiplies NaN by 0)
+        lse = att["lse"].double().cpu().numpy()
+        check_weigh(got, O.weigh(qh, lse, codes, scale, tables, length, weight.cpu().numpy(), 0.5, counts), weight)
+
+
+@pytest.mark.parametrize("dtype,D,H,G,n,lengths", WEIGH)
+def test_a_row_that_is_nan_makes_nan_of_its_heads_weights(tslt, dtype, D, H, G, n, lengths):
+    rng = np.random.default_rng([D, n, H])
+    B = len(lengths)
+    cache, pages, lens = on_gpu(*make_cache(rng, H, D, lengths))
+    (q, k, v), _ = projection(rng, B, n, H * G, H, D, DTYPES[dtype])
+    q[2, n - 1, (H - 1) * G] = float("nan")
+    att = tslt.cache_attend(q, cache, pages, lens, k=k, v=v)
+    weight = torch.rand(B, H, pages.shape[1] * 64, device=DEV)
+    got = tslt.cache_weigh(q, att["lse"], cache, pages, lens, weight)["weight"].cpu()
+    assert got[2, H - 1, :lengths[2]].isnan().all() and not got[2, H - 1, lengths[2]:].any()
+    got[2, H - 1] = 0
+    assert got.isfinite().all()
