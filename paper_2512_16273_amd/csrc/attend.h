@@ -27,6 +27,9 @@ namespace tslt {
 
 constexpr float kLag = 8.0f;
 constexpr float kNoMax = -3.4028235e38f;   // running maximum of a row that has met nothing yet
+// Scores (as powers of two) beyond which the maximum's own rounding, which a fused multiplication and subtraction does not share, is as much as a factor of
+// 2 on a weight: there scores are rounded first, as the maximum is, so that the weight of its token is 1 (and not 0 or infinite from 2^31 on).
+constexpr float kLarge = 16777216.0f;
 
 struct AttendParams {
   CacheView c;
@@ -170,8 +173,10 @@ template <typename T, int D, int NT, bool kHold> struct FreshTile {
 template <int D, int RT> struct RowState {
   f32x4 o[RT][D / 16];
   float m[RT], l[RT];
+  bool large;                              // of all lanes: a maximum has been beyond kLarge
 };
 template <int D, int RT> __device__ __forceinline__ void begin(RowState<D, RT>& st) {
+  st.large = false;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     st.m[rt] = kNoMax;
@@ -184,6 +189,7 @@ template <int D, int RT> __device__ __forceinline__ void begin(RowState<D, RT>& 
 template <int D, int RT> __device__ __forceinline__ void follow(RowState<D, RT>& st, int rt, float most) {
   if (ballot(most > st.m[rt] + kLag) == 0) return;
   const float m = over_groups_max(fmaxf(most, st.m[rt]));
+  st.large |= ballot(fabsf(m) > kLarge) != 0;
   const float f = exp2_fast(st.m[rt] - m);
   st.m[rt] = m;
   st.l[rt] *= f;
@@ -196,8 +202,8 @@ __device__ __forceinline__ float most_of(const f32x4 (&s)[4]) {
   for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i >> 2][i & 3]);
   return most;
 }
-// A page's scores without those of tokens from `there` on, which do not count, and the maximum.
-template <int D, int RT> __device__ __forceinline__ void page_maximum(f32x4 (&s)[RT][4], RowState<D, RT>& st, float c, int there, int g) {
+// A page's scores without those of tokens from `there` on, which do not count, and the maximum.  Returns what a score is to be multiplied by.
+template <int D, int RT> __device__ __forceinline__ float page_maximum(f32x4 (&s)[RT][4], RowState<D, RT>& st, float c, int there, int g) {
   if (there < kPage) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
@@ -207,6 +213,12 @@ template <int D, int RT> __device__ __forceinline__ void page_maximum(f32x4 (&s)
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) follow(st, rt, most_of(s[rt]) * c);
+  if (!st.large) return c;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[rt][t] *= c;
+  return 1.0f;
 }
 
 // Of 16 bytes, one a token, those of the first `there` tokens: what lies behind them may be anything.
@@ -671,8 +683,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(co
       key_products(kt, q, s);
       const uint8_t* next = page_codes(p.c, max(0, list.page_at(min(i + 1, some - 1))), at.h, D);
       if (i + 1 < some) kt.load(next, lane);
-      const float c = p.scale2 * list.k_at(i);
-      page_maximum(s, st, c, valid, g);
+      const float c = page_maximum(s, st, p.scale2 * list.k_at(i), valid, g);
       bf16x8 w[RT][2][Terms<T>::kW];
       page_weights<T, D, RT>(s, st, c, w);
       if (valid < kPage) vt.cut(valid - g * 16);
@@ -818,8 +829,7 @@ __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_r
         const int i = i0 + u;
         if (i >= some) break;
         if (first_row < at.rows) {
-          const float c = p.scale2 * list.k_at(i);
-          page_maximum(s, st, c, valid_of(i), g);
+          const float c = page_maximum(s, st, p.scale2 * list.k_at(i), valid_of(i), g);
           const uint8_t *tile = lds + (i & 1) * page_lds_bytes<D>(), *next_tile = lds + ((i + 1) & 1) * page_lds_bytes<D>();
           // (behind the last page: scores of what lies there, which are not used)
           page_round<kAhead>(q, s, st, c, [&](int t, int i) { return key_operand(next_tile, t, i); },

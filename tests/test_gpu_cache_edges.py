@@ -155,3 +155,29 @@ def test_a_row_that_is_nan_makes_nan_of_its_heads_weights(tslt, dtype, D, H, G, 
     assert got[2, H - 1, :lengths[2]].isnan().all() and not got[2, H - 1, lengths[2]:].any()
     got[2, H - 1] = 0
     assert got.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,G,length", [(2, 4, 1), (2, 4, 129), (2, 4, 6000), (20, 4, 1), (20, 4, 129), (20, 4, 6000)])
+def test_scores_beyond_2_to_the_31(tslt, dtype, n, G, length):
+    """Equal keys and scores so large that half a step of fp32 is many powers of two: weights are equal all the same, and the output is the mean."""
+    rng = np.random.default_rng([n, length])
+    D, H = 64, 1
+    codes, scale, tables, lengths = make_cache(rng, H, D, [length])
+    codes[:, :, 0] = 0
+    codes[:, 0, 0].reshape(-1, 64, D)[..., 0] = 0x7E                # 448
+    scale[..., 0] = 2.0 ** 12
+    host = (codes, scale, tables, lengths)
+    cache, pages, lens = on_gpu(*host)
+    q = torch.zeros(1, n, G, D, dtype=DTYPES[dtype], device=DEV)
+    q[0, :, :, 0] = (1 + torch.arange(n * G, device=DEV) % 8 / 8).view(n, G) * 2.0 ** 11 * (1 + torch.arange(n * G, device=DEV) // 8).view(n, G)
+    got = tslt.cache_attend(q, cache, pages, lens, scale=1.0)
+    torch.cuda.synchronize()
+    _, value, _ = O.cached(*host[:3][:2], tables[0], length, 0)
+    half = torch.finfo(DTYPES[dtype]).eps / 2
+    mean, size = value.mean(0), np.abs(value).mean(0)
+    off = np.abs(got["out"].double().cpu().numpy() - mean)
+    assert np.all(off <= half * np.abs(mean) * (1 + 2.0 ** -10) + (2.0 ** -16 if dtype != "f32" else 2.0 ** -22) * size + 2 * (8 * 2.0 ** -24 + 2.0 ** -21) * size + torch.finfo(DTYPES[dtype]).tiny)
+    want = q[..., 0].double().cpu().numpy() * 448 * 2.0 ** 12 + np.log(length)
+    assert want.min() > 2.0 ** 31
+    assert np.all(np.abs(got["lse"].double().cpu().numpy() / want - 1) <= 2.0 ** -21)
