@@ -568,14 +568,8 @@ template <typename T, int D, int NT, int kRows> __device__ __forceinline__ void 
   }
 }
 
-// A chunk's sum of values in units of another maximum.  A weight is positive, also one that is 0 in these units: a sum that its chunk's seen values have
-// made infinite stays infinite.
-__device__ __forceinline__ f32x4 in_units(f32x4 o, float f) {
-  f32x4 x = o * f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = __builtin_isinf(o[e]) ? o[e] : x[e];
-  return x;
-}
+// A chunk's maximum to another's units.  A weight is positive, however small: never 0, so that a sum which a chunk's seen values have made infinite stays so.
+__device__ __forceinline__ float in_units(float x) { return fmaxf(exp2_fast(x), 1.4012985e-45f); }
 
 // All threads of a workgroup that has given its rows: the last one of a sequence's chunks joins them, and says how the sequence's pages were.
 template <typename T, int D, int NT, int kRows>
@@ -617,9 +611,9 @@ __device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, boo
       for (int u = 0; u < 4; ++u)
         if (c0 + u < chunks) {
           const float mu = as_f32(uint32_t(ml[u])), most = fmaxf(m, mu);
-          const float f = exp2_fast(m - most), fu = exp2_fast(mu - most);
+          const float f = in_units(m - most), fu = in_units(mu - most);
           l = l * f + as_f32(uint32_t(ml[u] >> 32)) * fu;
-          o = in_units(o, f) + in_units(f32x4{as_f32(uint32_t(x[u][0])), as_f32(uint32_t(x[u][0] >> 32)), as_f32(uint32_t(x[u][1])), as_f32(uint32_t(x[u][1] >> 32))}, fu);
+          o = o * f + f32x4{as_f32(uint32_t(x[u][0])), as_f32(uint32_t(x[u][0] >> 32)), as_f32(uint32_t(x[u][1])), as_f32(uint32_t(x[u][1] >> 32))} * fu;
           m = most;
         }
     }
