@@ -438,7 +438,8 @@ int tslt_cache_append(const tslt_cache* cache, const int32_t* pages, int64_t wid
  *   mask        [B][n][ceil(n / 32)] uint32, bit j % 32 of word j / 32 of row i: token i sees token j (for a tree: its
  *               ancestors and itself).  mask_seq_stride words from a sequence's rows to the next's, 0 where all share one mask.
  *               NULL: token i sees tokens 0..i
- *   count       [B] int32: how many of the n tokens there are (0..n; the others' rows come out empty); NULL: n
+ *   count       [B] int32: how many of the n tokens there are (0..n, another counts as the nearest and sets TSLT_ROW_BAD_INDEX; the others' rows
+ *               come out empty); NULL: n
  *   scale       > 0
  *   out         [B][n][heads_q][D] of type dt, dense, 16-byte aligned
  *   out_lse     [B][n][heads_q] fp32: ln sum_j exp(scale * q_i . k_j)

@@ -474,7 +474,7 @@ __device__ __forceinline__ bool place_in_sequence(const AttendParams& p, Place& 
   at.len = cached_tokens(p.c, at.b, at.bad_length);
   at.n_pages = (at.len + kPage - 1) / kPage;
   at.active = max(1, (at.n_pages + p.chunk - 1) / p.chunk);
-  at.there = p.count ? min(max(as_global(p.count)[at.b], 0), p.n) : p.n;
+  at.there = counted(p.count, at.b, p.n);
   at.chunk = at.active - 1 - at.chunk;
   return at.chunk >= 0;
 }
@@ -579,7 +579,7 @@ __device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, boo
   if (at.active == 1) {
     if (!speaks) return;
     bad = __syncthreads_or(bad) != 0;
-    if (tid == 0) p.status[at.b] = bad ? kBadPage : 0;
+    if (tid == 0) p.status[at.b] = sequence_status(p.count, at.b, p.n, bad);
     return;
   }
   uint64_t* words = p.words + ((at.b * p.c.heads + at.h) * p.row_groups + at.rg) * int64_t(p.chunks);
@@ -626,7 +626,7 @@ __device__ __forceinline__ void join_chunks(const AttendParams& p, Place at, boo
       bad |= page < 0 || page >= p.c.n_pages;
     }
     bad = __syncthreads_or(bad) != 0;
-    if (tid == 0) p.status[at.b] = bad ? kBadPage : 0;
+    if (tid == 0) p.status[at.b] = sequence_status(p.count, at.b, p.n, bad);
   }
 }
 

@@ -49,6 +49,11 @@ __device__ __forceinline__ int cached_tokens(const CacheView& c, int64_t b, bool
   bad = len < 0 || len > most;
   return int(len < 0 ? 0 : len > most ? most : len);
 }
+// New tokens of a sequence, of n: its count (null: all), kept inside 0 .. n; and a sequence's status, which says where that was needed.
+__device__ __forceinline__ int counted(const int32_t* count, int64_t b, int n) { return count ? min(max(as_global(count)[b], 0), n) : n; }
+__device__ __forceinline__ int sequence_status(const int32_t* count, int64_t b, int n, bool bad_page) {
+  return (bad_page ? kBadPage : 0) | (count && as_global(count)[b] != counted(count, b, n) ? kBadIndex : 0);
+}
 __device__ __forceinline__ const uint8_t* page_codes(const CacheView& c, int64_t page, int head, int D) {
   return c.codes + (page * c.heads + head) * (2 * kPage * D);
 }

@@ -68,7 +68,7 @@ template <typename T, int D, int RT, int kWaves> __device__ __forceinline__ void
   bool bad;
   const int len = cached_tokens(p.c, b, bad);
   const int32_t* table = p.c.pages + b * p.c.width;
-  const int there = p.count ? min(max(as_global(p.count)[b], 0), p.n) : p.n;
+  const int there = counted(p.count, b, p.n);
   const int rows = there * p.group, blocks = (rows + 16 * RT - 1) / (16 * RT);
   const int64_t weights = (b * p.c.heads + h) * p.c.width * kPage;
 
@@ -231,7 +231,7 @@ template <typename T, int D, int RT, int kWaves> __global__ __launch_bounds__(25
         bad |= page < 0 || page >= p.c.n_pages;
       }
       bad = __syncthreads_or(bad) != 0;
-      if (tid == 0) p.status[b] = bad ? kBadPage : 0;
+      if (tid == 0) p.status[b] = sequence_status(p.count, b, p.n, bad);
     }
 }
 

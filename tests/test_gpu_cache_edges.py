@@ -181,3 +181,26 @@ def test_scores_beyond_2_to_the_31(tslt, dtype, n, G, length):
     want = q[..., 0].double().cpu().numpy() * 448 * 2.0 ** 12 + np.log(length)
     assert want.min() > 2.0 ** 31
     assert np.all(np.abs(got["lse"].double().cpu().numpy() / want - 1) <= 2.0 ** -21)
+
+
+@pytest.mark.parametrize("length", [70, 6000])                      # one chunk and several
+@pytest.mark.parametrize("n,G", [(3, 2), (40, 4)])
+def test_counts_outside_the_call_are_told_and_count_as_the_nearest(tslt, length, n, G):
+    rng = np.random.default_rng([n, length])
+    D, H = 64, 2
+    host = make_cache(rng, H, D, [length, 70, 5, 64])
+    cache, pages, lens = on_gpu(*host)
+    pages[2, 0] = -1
+    (q, k, v), (qh, kh, vh) = projection(rng, 4, n, H * G, H, D, torch.bfloat16)
+    count = torch.tensor([n + 1, -1, n + 5, n - 1], dtype=torch.int32, device=DEV)
+    fit = count.clamp(0, n)
+    got = tslt.cache_attend(q, cache, pages, lens, k=k, v=v, count=count)
+    weight = torch.rand(4, H, pages.shape[1] * 64, device=DEV)
+    w = tslt.cache_weigh(q, got["lse"], cache, pages, lens, weight, count=count)
+    want = tslt.cache_attend(q, cache, pages, lens, k=k, v=v, count=fit)
+    want_w = tslt.cache_weigh(q, got["lse"], cache, pages, lens, weight, count=fit)
+    torch.cuda.synchronize()
+    assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"]) and torch.equal(w["weight"], want_w["weight"])
+    bad = tslt.ROW_BAD_INDEX
+    assert got["status"].tolist() == w["status"].tolist() == [bad, bad, bad | tslt.ROW_BAD_PAGE, 0]
+    assert want["status"].tolist() == want_w["status"].tolist() == [0, 0, tslt.ROW_BAD_PAGE, 0]
