@@ -670,9 +670,12 @@ def cache_evict(cache: dict, pages: torch.Tensor, length: torch.Tensor, weight: 
                 new_pages: torch.Tensor, out: Optional[dict] = None) -> dict:
     """tslt_cache_evict: of every head the `recent` last tokens and those of most weight, `keep` in all, copied to the pages
     new_pages [B, new_width] of the same cache.  Returns length [B], kept [B, heads, keep], weight [B, heads, new_width * 64] and status [B]."""
+    keep, recent = int(keep), int(recent)
+    if not all(-(1 << 31) <= x < 1 << 31 for x in (keep, recent)):         # (ctypes would cut them)
+        raise TsltError(f"keep and recent must fit 32 bits (got {keep}, {recent})")
     lib = load()
     if _fast is not None and out is not None and weight.is_cuda:
-        code = _fast.cache_evict(cache, pages, length, weight, int(keep), int(recent), new_pages, out, _stream())
+        code = _fast.cache_evict(cache, pages, length, weight, keep, recent, new_pages, out, _stream())
         if code is not None:
             if code:
                 _check(code)
@@ -682,13 +685,13 @@ def cache_evict(cache: dict, pages: torch.Tensor, length: torch.Tensor, weight: 
     _dev(weight, torch.float32, "weight"); _dev(new_pages, torch.int32, "new_pages")
     if weight.numel() != B * heads * width * PAGE_TOKENS or new_pages.dim() != 2 or new_pages.shape[0] != B:
         raise TsltError("cache_evict: shapes do not agree")
-    keep, new_width = int(keep), new_pages.shape[1]
+    new_width = new_pages.shape[1]
     if out is None:
         out = {"length": torch.empty(B, dtype=torch.int32, device=weight.device),
                "kept": torch.empty(B, heads, max(keep, 0), dtype=torch.int32, device=weight.device),
                "weight": torch.empty(B, heads, new_width * PAGE_TOKENS, dtype=torch.float32, device=weight.device),
                "status": torch.empty(B, dtype=torch.int32, device=weight.device)}
-    _check(lib.tslt_cache_evict(c, pages.data_ptr(), width, length.data_ptr(), B, weight.data_ptr(), keep, int(recent), new_pages.data_ptr(),
+    _check(lib.tslt_cache_evict(c, pages.data_ptr(), width, length.data_ptr(), B, weight.data_ptr(), keep, recent, new_pages.data_ptr(),
                                 new_width, _sized(out, "length", torch.int32, B), _sized(out, "kept", torch.int32, B * heads * max(keep, 0)),
                                 _sized(out, "weight", torch.float32, B * heads * new_width * PAGE_TOKENS),
                                 _sized(out, "status", torch.int32, B, optional=True), _stream()))

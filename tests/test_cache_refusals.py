@@ -101,6 +101,14 @@ def test_python_binding_refuses_what_is_not_on_a_gpu_or_does_not_fit():
         tslt._rows_of(_Fake(x), "k", (1, 2, 2, 64), torch.float32)
 
 
+@pytest.mark.parametrize("keep,recent", [((1 << 32) + 5, 0), (5, 1 << 32), (1 << 31, 5), (5, -(1 << 32)), (-(1 << 32) + 5, 0)])
+def test_numbers_of_an_eviction_that_do_not_fit_are_refused_and_not_cut(keep, recent):
+    c = tslt.cache_create(4, 2, 64, device="cpu")
+    pages, length = torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(tslt.TsltError, match="32 bits"):
+        tslt.cache_evict(c, pages, length, torch.zeros(1, 2, 128), keep, recent, pages)
+
+
 class _Fake:
     """A tensor that says it lies on a GPU, for checks that come before anything is done with it."""
     is_cuda = True
