@@ -18,7 +18,9 @@
 // exactly.  Sums are fp32.  A weight enters the second product as the sum of two bfloat16 terms, 16 bits, and of three, 24, in fp32
 // calls; values enter it as bfloat16 times their page's scale, exactly.  (One bfloat16 term would be off by 2^-9, as much as the output's
 // own rounding; one binary16 term by 2^-12, but it loses weights below 2^-30 of the largest, and where that one's value is 0 they are the result.)
-// The running maximum is followed only when a row exceeds it by kLag powers of two: weights, in units of it, stay below 2^kLag.
+// The running maximum is followed only when a row exceeds it by kLag powers of two: weights, in units of it, stay below 2^kLag.  Sums of values are in
+// units of 2^16, so that many weights that are not small yet and values near fp32's largest do not pass it before they are divided by the weights' sum:
+// 65536 of them do where weights are 1, 256 where they are 2^kLag.  (A page's scale takes that in for nothing, exactly; of new tokens the weights do.)
 #pragma once
 #include "cache.h"
 #include "handover.h"
@@ -26,6 +28,7 @@
 namespace tslt {
 
 constexpr float kLag = 8.0f;
+constexpr float kUnit = 65536.0f;          // of sums of values
 constexpr float kNoMax = -3.4028235e38f;   // running maximum of a row that has met nothing yet
 // Scores (as powers of two) beyond which the maximum's own rounding, which a fused multiplication and subtraction does not share, is as much as a factor of
 // 2 on a weight: there scores are rounded first, as the maximum is, so that the weight of its token is 1 (and not 0 or infinite from 2^31 on).
@@ -324,9 +327,9 @@ __device__ __forceinline__ void page_round(const Queries<T, D, RT>& q, f32x4 (&s
     for (int t = 0; t < 4; ++t) s[rt][t] = next[rt][t];
   }
 }
-// The same for the kernel whose waves read operands of their own: a page's weights, then its values.
+// The same for the kernel whose waves read operands of their own: a page's weights, times `unit` for its values, then these.
 template <typename T, int D, int RT>
-__device__ __forceinline__ void page_weights(const f32x4 (&s)[RT][4], RowState<D, RT>& st, float c, bf16x8 (&w)[RT][2][Terms<T>::kW]) {
+__device__ __forceinline__ void page_weights(const f32x4 (&s)[RT][4], RowState<D, RT>& st, float c, float unit, bf16x8 (&w)[RT][2][Terms<T>::kW]) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float sum = 0;
@@ -334,7 +337,7 @@ __device__ __forceinline__ void page_weights(const f32x4 (&s)[RT][4], RowState<D
     for (int i = 0; i < 16; ++i) {
       const float x = exp2_fast(__builtin_fmaf(s[rt][i >> 2][i & 3], c, -st.m[rt]));
       sum += x;
-      split_weight(x, i & 7, w[rt][i >> 3]);
+      split_weight(x * unit, i & 7, w[rt][i >> 3]);
     }
     st.l[rt] += sum;
   }
@@ -428,7 +431,7 @@ __device__ __forceinline__ void attend_fresh(const AttendParams& p, int64_t b, i
       follow(st, rt, most_of(s[rt]));
     }
     bf16x8 w[RT][2][W::kW];
-    page_weights<T, D, RT>(s, st, 1.0f, w);
+    page_weights<T, D, RT>(s, st, 1.0f, 1.0f / kUnit, w);
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
 #pragma unroll
@@ -491,7 +494,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void load_querie
 // Up to 64 entries of a sequence's table with the scales of their pages, one a lane: entries first, first + step, ...
 struct PageList {
   int page;                                // -1: outside the cache
-  float k_scale, v_scale;
+  float k_scale, v_scale;                  // (for sums in units of kUnit)
   __device__ __forceinline__ void ask(const AttendParams& p, const Place& at, int first, int step, int some) {
     page = -1;
     if (lane_id() < some) page = as_global(p.c.pages + at.b * p.c.width)[first + step * lane_id()];
@@ -508,7 +511,7 @@ struct PageList {
     else {
       const float* sc = p.c.scales + (int64_t(page) * p.c.heads + at.h) * 2;
       k_scale = as_global(sc)[0];
-      v_scale = as_global(sc)[1];
+      v_scale = as_global(sc)[1] * (1.0f / kUnit);
     }
     return bad;
   }
@@ -530,7 +533,7 @@ template <typename T, int D> __device__ __forceinline__ void give(const AttendPa
   const bool none = i >= at.there || l == 0;
   const int64_t to = (at.b * p.n + i) * p.heads_q + at.h * p.group + row % p.group;
   if (d == 0) p.lse[to] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-  store4<T>(p.out, to * D + d, none ? f32x4{0, 0, 0, 0} : o * (1.0f / l));
+  store4<T>(p.out, to * D + d, none ? f32x4{0, 0, 0, 0} : o * (kUnit / l));
 }
 
 // Seen values that are not finite, to the rows that see them: a weight is positive, so that the sum becomes what they add up to alone.
@@ -679,7 +682,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_stream_kernel(co
       if (i + 1 < some) kt.load(next, lane);
       const float c = page_maximum(s, st, p.scale2 * list.k_at(i), valid, g);
       bf16x8 w[RT][2][Terms<T>::kW];
-      page_weights<T, D, RT>(s, st, c, w);
+      page_weights<T, D, RT>(s, st, c, 1.0f, w);
       if (valid < kPage) vt.cut(valid - g * 16);
       page_values(vt, w, st, list.v_at(i));
       if (i + 1 < some) vt.load(next + kPage * D, lane);

@@ -204,3 +204,26 @@ def test_counts_outside_the_call_are_told_and_count_as_the_nearest(tslt, length,
     bad = tslt.ROW_BAD_INDEX
     assert got["status"].tolist() == w["status"].tolist() == [bad, bad, bad | tslt.ROW_BAD_PAGE, 0]
     assert want["status"].tolist() == want_w["status"].tolist() == [0, 0, tslt.ROW_BAD_PAGE, 0]
+
+
+# (new tokens alone; a cache in one chunk, and in several; the kernel for few rows, and the one for many)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,G", [(5, 2), (70, 2)])
+@pytest.mark.parametrize("length", [0, 70, 6000])
+def test_values_near_the_largest_do_not_overflow(tslt, dtype, n, G, length):
+    """Outputs are means of values: finite where these are, though the values times their weights, before the division, would pass fp32's largest."""
+    rng = np.random.default_rng([n, length])
+    D, H = 64, 2
+    codes, scale, tables, lengths = make_cache(rng, H, D, [length])
+    codes[:, :, 1][(codes[:, :, 1] & 127) == 127] = 0               # (none of the NaN behind the length)
+    codes[:, :, 1].reshape(-1, H, 4, D, 16)[:, :, :, :5] = 0x7E     # of channels 0 .. 4 all 448, the others up to that
+    scale[..., 1] = 2.0 ** 118
+    host = (codes, scale, tables, lengths)
+    cache, pages, lens = on_gpu(*host)
+    (q, k, v), _ = projection(rng, 1, n, H * G, H, D, DTYPES[dtype])
+    v[:] = torch.sign(v) * 1.5e38
+    v[..., :5] = 1.5e38
+    qh, kh, vh = (t.double().cpu().numpy() for t in (q, k, v))
+    got = tslt.cache_attend(q, cache, pages, lens, k=k, v=v)
+    torch.cuda.synchronize()
+    check_attend(got, O.attend(qh, *host, kh, vh), DTYPES[dtype])
