@@ -227,3 +227,95 @@ def test_values_near_the_largest_do_not_overflow(tslt, dtype, n, G, length):
     got = tslt.cache_attend(q, cache, pages, lens, k=k, v=v)
     torch.cuda.synchronize()
     check_attend(got, O.attend(qh, *host, kh, vh), DTYPES[dtype])
+
+
+def reference_rows(cache, pages, length, q, scale, b, h, G):
+    """Scores [n * G, length], values and, by torch in fp64 on the GPU, what attention over the cached tokens alone gives the rows of one head."""
+    codes, sc = cache["codes"][:, h], cache["scale"][:, h].double()
+    D = codes.shape[-1] // 64
+    grid = torch.from_numpy(O.decode(np.arange(256, dtype=np.uint8))).to(DEV)
+    keys = grid[codes[:, 0].long()].view(-1, 64, D) * sc[:, 0, None, None]
+    values = grid[codes[:, 1].long()].view(-1, 4, D, 16).transpose(2, 3).reshape(-1, 64, D) * sc[:, 1, None, None]
+    L = int(length[b])
+    at = pages[b, :-(-L // 64)].long()
+    k, v = keys[at].reshape(-1, D)[:L], values[at].reshape(-1, D)[:L]
+    rows = q[b, :, h * G:(h + 1) * G].reshape(-1, D).double()
+    s = rows @ k.T.contiguous() * scale
+    lse = torch.logsumexp(s, 1)
+    p = torch.exp(s - lse[:, None])
+    return s, lse, p @ v, p @ v.abs(), (rows.abs() @ k.abs().T.contiguous()).amax(1) * scale
+
+
+@pytest.mark.parametrize("dtype,D,H,G,n,B,long", [("bf16", 64, 8, 2, 2, 66, 70000),      # few rows: more than 64 turns of a wave
+                                                  ("f32", 64, 8, 2, 2, 66, 70000),
+                                                  ("f16", 128, 8, 4, 10, 66, 45000),     # 40 rows: chunks of more than 64 pages
+                                                  ("f32", 64, 4, 4, 20, 130, 15000),     # 80 rows
+                                                  ("bf16", 128, 4, 8, 16, 130, 15000)])  # 128 rows
+def test_page_lists_of_more_than_64_entries(tslt, dtype, D, H, G, n, B, long):
+    """Long sequences, enough of them that their chunks, and shares of a wave, are long too; they lie on the same pages.  More than 64 sequences."""
+    rng = np.random.default_rng([D, H, B])
+    n_pages, width = 300, -(-long // 64)
+    codes = rng.integers(0, 256, (n_pages, H, 2, 64 * D)).astype(np.uint8)
+    codes[(codes & 127) >= 120] ^= 64
+    scale = np.ldexp(1.0, rng.integers(-9, -4, (n_pages, H, 2))).astype(np.float32)
+    tables = rng.integers(0, n_pages, (B, width)).astype(np.int32)
+    lengths = rng.integers(long - 3000, long + 1, B).astype(np.int32)
+    lengths[:4] = [long, 0, 70, 64 * 64 + 1]
+    cache, pages, length = on_gpu(codes, scale, tables, lengths)
+    (q, _, _), _ = projection(rng, B, n, H * G, H, D, DTYPES[dtype])
+    got = tslt.cache_attend(q, cache, pages, length)
+    weight = torch.rand(B, H, width * 64, device=DEV)
+    w = tslt.cache_weigh(q, got["lse"], cache, pages, length, weight, decay=0.5)
+    torch.cuda.synchronize()
+    assert not got["status"].any() and not w["status"].any()
+    place = torch.arange(width * 64, device=DEV)
+    assert not w["weight"][(place >= length[:, None])[:, None].expand(B, H, -1)].any()
+    assert not got["out"][1].any() and torch.isneginf(got["lse"][1]).all()
+    half, weight_bits = torch.finfo(DTYPES[dtype]).eps / 2, 2.0 ** -22 if dtype == "f32" else 2.0 ** -16
+    for b in (0, 2, 3, 5, 40, 63, 64, 65, B - 1):
+        for h in (0, H - 1):
+            L = int(lengths[b])
+            s, lse, out, size, reach = reference_rows(cache, pages, lengths, q, D ** -0.5, b, h, G)
+            rel = 2 * (8 * 2.0 ** -24 * reach + 2.0 ** -21)
+            mine = got["out"][b, :, h * G:(h + 1) * G].reshape(-1, D).double()
+            tol = half * out.abs() * (1 + 2.0 ** -10) + (weight_bits + rel[:, None]) * size + torch.finfo(DTYPES[dtype]).tiny
+            assert ((mine - out).abs() <= tol).all(), (b, h, float(((mine - out).abs() / tol).max()))
+            got_lse = got["lse"][b, :, h * G:(h + 1) * G].reshape(-1).double()
+            assert ((got_lse - lse).abs() <= rel + 2.0 ** -22 * lse.abs()).all(), (b, h)
+            want = 0.5 * weight[b, h, :L].double() + torch.exp(s - got_lse[:, None]).sum(0)
+            rel_w = 2 * (8 * 2.0 ** -24 * (reach + got_lse.abs()).max() + 2.0 ** -21)
+            assert ((w["weight"][b, h, :L].double() - want).abs() <= (rel_w + 2.0 ** -21) * want + 2.0 ** -30).all(), (b, h)
+
+
+def test_evict_from_more_than_32768_tokens(tslt):
+    """Weights read from memory every time.  All pages of one scale, so that codes are moved as they are."""
+    rng = np.random.default_rng(91)
+    D, H, lengths, keep, recent = 64, 2, [40001, 300], 25000, 100
+    codes, scale, tables, length = make_cache(rng, H, D, lengths)
+    scale[:] = 2.0 ** -6
+    W, first = -(-keep // 64), codes.shape[0]
+    codes = np.concatenate([codes, np.full((2 * W,) + codes.shape[1:], 127, np.uint8)])
+    scale = np.concatenate([scale, np.full((2 * W,) + scale.shape[1:], 1e30, np.float32)])
+    new = (first + rng.permutation(2 * W)).reshape(2, W).astype(np.int32)
+    weight = np.floor(rng.random((2, H, tables.shape[1] * 64)) * 1000).astype(np.float32)       # (many are equal)
+    weight[0, 1, rng.random(weight.shape[2]) < 0.6] = np.nan
+    cache, pages, lens = on_gpu(codes, scale, tables, length)
+    got = tslt.cache_evict(cache, pages, lens, torch.from_numpy(weight).to(DEV), keep, recent, torch.from_numpy(new).to(DEV))
+    torch.cuda.synchronize()
+    assert got["length"].tolist() == [keep, 300] and got["status"].tolist() == [0, 0]
+    after = cache["codes"].cpu().numpy()
+
+    def tokens(table, h, part):
+        x = after[table, h, part].reshape(len(table), *((64, D) if part == 0 else (4, D, 16)))
+        return (x if part == 0 else x.transpose(0, 1, 3, 2)).reshape(-1, D)
+    for b, L in enumerate(lengths):
+        m, r = min(L, keep), min(recent, min(L, keep))
+        for h in range(H):
+            old = weight[b, h, :L - r]
+            order = np.lexsort((np.arange(L - r), -np.where(np.isnan(old), -np.inf, old), np.isnan(old)))
+            mine = np.sort(np.concatenate([order[:m - r], np.arange(L - r, L)]))
+            assert np.array_equal(got["kept"][b, h, :m].cpu().numpy(), mine) and (got["kept"][b, h, m:] == -1).all()
+            assert np.array_equal(got["weight"][b, h, :m].cpu().numpy(), weight[b, h, mine], equal_nan=True) and not got["weight"][b, h, m:].any()
+            for part in (0, 1):
+                assert np.array_equal(tokens(new[b], h, part)[:m], tokens(tables[b, :-(-L // 64)], h, part)[mine]), (b, h, part)
+    assert (cache["scale"].cpu().numpy()[new[0]] == 2.0 ** -6).all()
