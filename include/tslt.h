@@ -458,7 +458,7 @@ int tslt_cache_attend(const tslt_cache* cache, const int32_t* pages, int64_t wid
 /* The attention weight that each cached token got in a round, added to what it had:
  * out_weight_j = decay * weight_j + sum over the n tokens and the query heads that share a head of exp(scale * q_i . k_j - lse_i).
  *
- *   q, count, scale   as tslt_cache_attend was given them, and lse its out_lse (a row with -inf adds nothing)
+ *   q, count, scale   as tslt_cache_attend was given them, and lse its out_lse (a row with -inf adds nothing, whatever it holds)
  *   weight, out_weight  [B][heads][width * 64] fp32, may be the same array; 0 is written at and behind a sequence's length, so that tokens
  *               appended later begin with 0
  *   status      [B] int32; may be NULL

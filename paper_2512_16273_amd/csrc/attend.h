@@ -7,11 +7,11 @@
 // keys, so the products are dense in tiles of 16 rows, and one pass keeps a running maximum m and sum l for each row.
 //
 // One wave takes 64 keys at a time against tiles of 16 rows (see Tile), in two kernels:
-//   attend_stream_kernel, few rows: bound by memory (4 sequences of 131000 tokens, 8 heads of 128, 4 rows: 173 us, 1029 MB at 5.9 TB/s; a large read runs at 7.0).  Codes go from memory straight into the operand registers of the products (the
+//   attend_stream_kernel, few rows: bound by memory (4 sequences of 131000 tokens, 8 heads of 128, 4 rows: 174 us, 1029 MB at 5.9 TB/s; a large read runs at 7.0).  Codes go from memory straight into the operand registers of the products (the
 //     order in which the cache holds them is made for that).  A workgroup's four waves have the same rows and take pages in turn.
 //   attend_rows_kernel, many rows: bound by the products and the exponentials.  A workgroup brings a page to LDS once, as operands, for
 //     all of its waves, each with rows of its own (2048 bfloat16 tokens on 16000, 32 heads of 128 on 8: 800 us, 571 GFLOP by the formula at 714
-//     TFLOP/s, 1071 with the weights' second term; a large matrix product runs at 1200.  It is 3.5 vector instructions a product that keep it from that).
+//     TFLOP/s, 1071 with the weights' second term; a large matrix product runs at 1200.  It is 3.6 vector instructions a product that keep it from that).
 // A sequence is cut into chunks of pages where its rows alone do not fill the GPU; whichever of its workgroups ends last joins them.
 //
 // Rounding.  Codes, and queries of 16 bits, enter the first product exactly; queries of 32 bits as three bfloat16 terms,
@@ -857,7 +857,9 @@ __global__ __launch_bounds__(NW * 64, D == 256 && NW == 4 ? 1 : 2) void attend_r
   join_chunks<T, D, NT, kRows>(p, at, bad, told);
 }
 
-// Tiles of rows to a wave of the kernel for many rows, so that two waves to a SIMD have registers enough (one for fp32 and D = 256).
+// Tiles of rows to a wave of the kernel for many rows, so that two waves to a SIMD have registers enough, one where D = 256 and four waves share a page.  (Not
+// quite: 16 spill with bfloat16, D = 128, two tiles, 8 with fp32, D = 128, 64 rows, one with 16 bits, D = 256, eight waves.  They are addresses, written
+// once and read outside of the loop over pages, in that over new tokens one or two a tile.)
 template <typename T, int D> constexpr int rows_tiles() { return D == 64 || (D == 128 && sizeof(T) == 2) ? 2 : 1; }
 // The launches, for each type of the call in a source file of its own (attend_launch.h, attend_*.hip).
 template <typename T> hipError_t launch_attend(const AttendParams& p, int D, hipStream_t s);

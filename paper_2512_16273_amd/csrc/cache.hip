@@ -89,7 +89,9 @@ template <typename T, int D> struct Weigh {
   }
 };
 
-// How an attention call is cut: row groups, and chunks of a sequence's pages (what the host knows of lengths is the width of the page table).
+// How an attention call is cut: row groups, and chunks of a sequence's pages (what the host knows of lengths is the width of the page table; where sequences are
+// much shorter than it most chunks are empty and the others long).  `slots` counts two workgroups to a compute unit.  Of D = 256, and of eight waves (fp32, D = 128,
+// and 16 bits, D = 256, of more than 64 rows), one fits: a round of those is two.
 //   Few rows.  Where the rows make fewer workgroups than fit the GPU, chunks fill it: twice over with 16 rows, so that whoever has ended early finds
 //   more, once with 32, whose parts cost more to join.  us by one round of workgroups / two: 4 sequences of 131000 tokens 167 / 172.  Where there are
 //   enough without, 16 rows are still cut in four, as sequences differ in length: 64 sequences of 100 to 8000 tokens, 8 heads, in one / four: 4 rows
@@ -236,7 +238,7 @@ int tslt_cache_weigh(const tslt_cache* cache, const int32_t* pages, int64_t widt
   p.B = B; p.n = n; p.group = heads_q / cache->heads; p.heads_q = heads_q; p.count = count; p.lse = lse;
   p.scale2 = float(double(scale) * 1.4426950408889634074);
   p.decay = decay; p.weight = weight; p.out_weight = out_weight; p.status = status;
-  // One round of workgroups, two to a compute unit, or a page to each wave.
+  // One round of workgroups, two to a compute unit (of D = 256 one fits: two rounds), or a page to each wave.
   const int64_t blocks = std::min<int64_t>(2 * int64_t(tslt::compute_units()), (std::min<int64_t>(B * cache->heads, 1 << 20) * width + 3) / 4);
   by_type<Weigh>(dt, cache->head_dim, p, unsigned(blocks), reinterpret_cast<hipStream_t>(stream));
   return launched("tslt_cache_weigh launch");
@@ -262,7 +264,7 @@ int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t widt
   int code;
   if (!grid_fits(who, std::max(heads, moves), code)) return code;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  // (weights in registers where the longest sequence's fit: 16 waves of 64 lanes)
+  // (weights in registers where as many fit as the table has room for: 16 waves of 64 lanes)
   const auto select = width <= 64 ? tslt::evict_select_kernel<4> : width <= 512 ? tslt::evict_select_kernel<32> : tslt::evict_select_kernel<0>;
   hipLaunchKernelGGL(select, dim3(unsigned(heads)), dim3(tslt::kEvictThreads), 0, s, p);
   const auto move = cache->head_dim == 64 ? tslt::evict_move_kernel<64> : cache->head_dim == 128 ? tslt::evict_move_kernel<128> : tslt::evict_move_kernel<256>;

@@ -7,8 +7,8 @@
 // nothing is exchanged between waves (but for the sums of four that share a page, in an order that does not change).  Bound by the bytes of the keys where the rows are few, by the products and the exponentials where they are many.
 // Where there are fewer pages than workgroups fit the GPU and many rows, a workgroup's four waves share a page and its rows.
 // All pages of all sequences and heads are dealt out to one round of waves in equal shares, as sequences differ in length and the host does not know
-// how (32 sequences of 1000 to 16000 tokens, 8 heads, 36 rows: 97 us with as many workgroups to each head of each sequence, 78 so:
-// 315 MB at 4.0 TB/s, 32 GFLOP).
+// how (32 sequences of 1000 to 16000 tokens, 8 heads, 36 rows: 97 us with as many workgroups to each head of each sequence, 78 so: 298 MB that it
+// cannot do without at 3.8 TB/s, 351 moved, 20 GFLOP; matrix units are busy an eighth of the time: a tile's products and its exponentials take turns).
 #pragma once
 #include "cache.h"
 
@@ -47,7 +47,7 @@ template <int kHalf> __device__ __forceinline__ void fold(float (&sum)[16], int 
   }
 }
 
-// Most tiles of rows that there are registers for.
+// Most tiles of rows that there are registers for (none spills; 16 bits, D = 128, four tiles: 253 of 256).
 template <typename T, int D> constexpr int weigh_tiles() { return sizeof(T) == 2 ? (D == 256 ? 2 : 4) : D == 64 ? 2 : 1; }
 
 // Pages of a sequence.
