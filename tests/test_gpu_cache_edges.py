@@ -319,3 +319,28 @@ def test_evict_from_more_than_32768_tokens(tslt):
             for part in (0, 1):
                 assert np.array_equal(tokens(new[b], h, part)[:m], tokens(tables[b, :-(-L // 64)], h, part)[mine]), (b, h, part)
     assert (cache["scale"].cpu().numpy()[new[0]] == 2.0 ** -6).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,G,length", [(3, 4, 70), (3, 4, 6000), (40, 4, 70), (40, 4, 6000)])
+def test_scores_beyond_2_to_the_31_of_cached_and_new_tokens_alike(tslt, dtype, n, G, length):
+    rng = np.random.default_rng([n, length, 1])
+    D, H = 64, 1
+    codes, scale, tables, lengths = make_cache(rng, H, D, [length])
+    codes[:, :, 0] = 0
+    codes[:, 0, 0].reshape(-1, 64, D)[..., 0] = 0x7E                # 448
+    scale[..., 0] = 2.0 ** 12
+    cache, pages, lens = on_gpu(codes, scale, tables, lengths)
+    (q, k, v), (_, _, vh) = projection(rng, 1, n, G, H, D, DTYPES[dtype])
+    q[:], k[:] = 0, 0
+    q[0, :, :, 0] = (1 + torch.arange(n * G, device=DEV) % 8 / 8).view(n, G) * 2.0 ** 11
+    k[..., 0] = 448 * 2.0 ** 12
+    got = tslt.cache_attend(q, cache, pages, lens, k=k, v=v, scale=1.0)
+    torch.cuda.synchronize()
+    _, value, _ = O.cached(codes, scale, tables[0], length, 0)
+    half, weight_bits = torch.finfo(DTYPES[dtype]).eps / 2, 2.0 ** -22 if dtype == "f32" else 2.0 ** -16
+    for i in range(n):
+        seen = np.concatenate([value, vh[0, :i + 1, 0]])
+        off = np.abs(got["out"][0, i].double().cpu().numpy() - seen.mean(0))
+        tol = half * np.abs(seen.mean(0)) * (1 + 2.0 ** -10) + (weight_bits + 2 * (8 * 2.0 ** -24 + 2.0 ** -21)) * np.abs(seen).mean(0)
+        assert np.all(off <= tol), (i, float((off / tol).max()))
