@@ -482,6 +482,63 @@ int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t widt
                      int32_t keep, int32_t recent, const int32_t* new_pages, int64_t new_width, int32_t* out_length, int32_t* out_kept,
                      float* out_weight, int32_t* status, void* stream);
 
+/* ---- Around attention and verification ---------------------------------------------------------------------------
+ *
+ * What a round computes between those calls: the norms and the rotation of queries and keys before they are attended to or cached (tslt_rotate),
+ * with its gradients, for a draft model that learns from what was accepted.  Rows of tokens are tslt_rows as above, also where they are written to;
+ * `count` [B] int32 says how many of a sequence's n tokens there are, the first ones: 0..n, another
+ * counts as the nearest and sets TSLT_ROW_BAD_INDEX; NULL: all.  What belongs to the others is not read, and is left as it was. */
+
+/* Queries and keys of every head, normed and rotated: x^ = weight * x / sqrt(mean x^2 + eps), then of each pair j of the first `rotary` channels
+ * (u, v) -> (u cos - v sin, v cos + u sin) by the angle (base[b] + position[b][i][axis[j]]) * freq[j].
+ *
+ *   position    [B][n][axes] int32, position_seq_stride numbers from a sequence's to the next's, 0 where all share them (a tree's
+ *               depths); NULL: token i of a sequence is at i on every axis
+ *   base        [B] int32, added to every one of a sequence's positions (they are summed in 64 bits); NULL: 0
+ *   freq        [rotary / 2] fp32, radians a position
+ *   axis        [rotary / 2] int32: the axis of each pair (time, height, width of an image's tokens), 0..axes-1; another counts as the
+ *               nearest and sets TSLT_ROW_BAD_INDEX.  NULL: axis 0
+ *   axes        1..TSLT_MAX_AXES
+ *   rotary      a multiple of 16, at most head_dim; channels behind it are not rotated.  0: none are, and position, base, freq, axis do not count
+ *   adjacent    0: pair j is channels j and j + rotary / 2; 1: channels 2j and 2j + 1
+ *   eps         >= 0; negative: no norm
+ *   q_weight, k_weight  [head_dim] fp32, with a norm only; NULL: 1 */
+#define TSLT_MAX_AXES 4
+typedef struct {
+  const int32_t* position;
+  int64_t position_seq_stride;
+  const int32_t* base;
+  const float* freq;
+  const int32_t* axis;
+  int32_t axes;
+  int32_t rotary;
+  int32_t adjacent;
+  float eps;
+  const float* q_weight;
+  const float* k_weight;
+} tslt_rotation;
+
+/*   q           [B][n][heads_q][head_dim] of type dt;  k [B][n][heads][head_dim], NULL: none (heads does not count then)
+ *   out_q, out_k  the same shapes and type; each may be its input itself (the same place and strides)
+ *   status      [B] int32; may be NULL
+ * head_dim is 64, 128 or 256.  Angles are fp64 until they are brought into one turn, sums of squares fp64, the rest fp32, rounded once.  A row that
+ * holds a number that is not finite comes out as those rules give.  No workspace. */
+int tslt_rotate(const tslt_rows* q, const tslt_rows* k, tslt_dtype dt, int64_t B, int32_t n, int32_t heads_q, int32_t heads, int32_t head_dim,
+                const tslt_rotation* how, const int32_t* count, const tslt_rows* out_q, const tslt_rows* out_k, int32_t* status, void* stream);
+
+/* Its gradients, from those of its results.
+ *
+ *   grad_q, grad_k  of out_q and out_k (grad_k NULL: no keys);  q, k  what tslt_rotate was given (may be NULL without a norm)
+ *   out_q, out_k    gradients of q and k; each may be grad_q, grad_k itself.  Of tokens that do not count they are zeros
+ *   out_q_weight, out_k_weight  [head_dim] fp32: the weights' gradients, summed over all sequences, tokens and heads; each may be NULL,
+ *               and is without a norm
+ * The same call gives the same bits.  Workspace: tslt_rotate_backward_workspace_bytes of the same arguments, 256-byte aligned, where a weight's gradient is
+ * asked for; it need not be cleared. */
+size_t tslt_rotate_backward_workspace_bytes(int64_t B, int32_t n, int32_t heads_q, int32_t heads, int32_t head_dim);
+int tslt_rotate_backward(const tslt_rows* grad_q, const tslt_rows* grad_k, const tslt_rows* q, const tslt_rows* k, tslt_dtype dt, int64_t B, int32_t n,
+                         int32_t heads_q, int32_t heads, int32_t head_dim, const tslt_rotation* how, const int32_t* count, const tslt_rows* out_q,
+                         const tslt_rows* out_k, float* out_q_weight, float* out_k_weight, int32_t* status, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

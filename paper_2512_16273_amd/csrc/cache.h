@@ -9,7 +9,7 @@
 // relative rounding smaller; and where a page's scale has to grow for a token that comes later, its codes are brought to
 // the new scale exactly (but for those that become subnormal).
 #pragma once
-#include "common.h"
+#include "rows.h"
 
 namespace tslt {
 
@@ -25,16 +25,12 @@ struct CacheView {
   int64_t width;
   const int32_t* length;                   // [B]
 };
-struct RowsView { const void* data; int64_t seq, token, head; };       // strides in elements
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-constexpr int kBadPage = 16, kBadIndex = 32;           // TSLT_ROW_BAD_PAGE, TSLT_ROW_BAD_INDEX
 
 // a / b of two powers of two; kept inside the normal numbers, where it is not exact any more.
 __device__ __forceinline__ float power_ratio(float a, float b) {
@@ -49,16 +45,9 @@ __device__ __forceinline__ int cached_tokens(const CacheView& c, int64_t b, bool
   bad = len < 0 || len > most;
   return int(len < 0 ? 0 : len > most ? most : len);
 }
-// New tokens of a sequence, of n: its count (null: all), kept inside 0 .. n; and a sequence's status, which says where that was needed.
-__device__ __forceinline__ int counted(const int32_t* count, int64_t b, int n) { return count ? min(max(as_global(count)[b], 0), n) : n; }
-__device__ __forceinline__ int sequence_status(const int32_t* count, int64_t b, int n, bool bad_page) {
-  return (bad_page ? kBadPage : 0) | (count && as_global(count)[b] != counted(count, b, n) ? kBadIndex : 0);
-}
 __device__ __forceinline__ const uint8_t* page_codes(const CacheView& c, int64_t page, int head, int D) {
   return c.codes + (page * c.heads + head) * (2 * kPage * D);
 }
-
-__device__ __forceinline__ u32x4 load16(const void* p) { return *as_global(reinterpret_cast<const u32x4*>(p)); }
 
 // The same of what no other workgroup reads: it need not stay in a cache (4 x 131000 tokens 167 us so, 185 without).
 __device__ __forceinline__ u32x4 load16_once(const void* p) { return __builtin_nontemporal_load(as_global(reinterpret_cast<const u32x4*>(p))); }

@@ -6,16 +6,13 @@
 
 #include "append.h"
 #include "attend.h"
-#include "error.h"
+#include "checks.h"
 #include "evict.h"
 #include "weigh.h"
 
 namespace {
 
 using tslt::fail;
-
-int elem_bytes(tslt_dtype dt) { return dt == TSLT_F32 ? 4 : 2; }
-bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 // What every call says of its cache and its sequences; 0 if the kernels can take it.
 int check_cache(const char* who, const tslt_cache* c, const int32_t* pages, int64_t width, const int32_t* length, int64_t B) {
@@ -30,30 +27,9 @@ int check_cache(const char* who, const tslt_cache* c, const int32_t* pages, int6
   if (!aligned(c->codes, 16)) return fail(TSLT_ERR_INVALID_ARG, "%s: codes not aligned to 16 bytes", who);
   return TSLT_OK;
 }
-// Rows of new tokens: 16 bytes at a time are read of each.
-int check_rows(const char* who, const char* what, const tslt_rows* r, tslt_dtype dt) {
-  if (!r || !r->data) return fail(TSLT_ERR_INVALID_ARG, "%s: null %s", who, what);
-  const int64_t unit = 16 / elem_bytes(dt);
-  if (!aligned(r->data, 16) || r->seq_stride % unit || r->token_stride % unit || r->head_stride % unit)
-    return fail(TSLT_ERR_INVALID_ARG, "%s: rows of %s must begin at multiples of 16 bytes", who, what);
-  return TSLT_OK;
-}
-bool valid_dtype(tslt_dtype dt) { return dt == TSLT_F32 || dt == TSLT_BF16 || dt == TSLT_F16; }
 tslt::CacheView view(const tslt_cache* c, const int32_t* pages, int64_t width, const int32_t* length) {
   return tslt::CacheView{c->codes, c->scales, c->n_pages, int(c->heads), pages, width, length};
 }
-tslt::RowsView view(const tslt_rows* r) {
-  return r ? tslt::RowsView{r->data, r->seq_stride, r->token_stride, r->head_stride} : tslt::RowsView{nullptr, 0, 0, 0};
-}
-bool grid_fits(const char* who, int64_t blocks, int& code) {
-  code = blocks > 0x7FFFFFFF ? fail(TSLT_ERR_UNSUPPORTED, "%s: too many workgroups for one launch", who) : 0;
-  return code == 0;
-}
-int launched(const char* who) {
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? TSLT_OK : tslt::hip_fail(e, who);
-}
-
 template <template <typename, int> class Launch, typename P> void by_type(tslt_dtype dt, int D, const P& p, unsigned blocks, hipStream_t s) {
 #define TSLT_BY_D(T) (D == 64 ? Launch<T, 64>::go(p, blocks, s) : D == 128 ? Launch<T, 128>::go(p, blocks, s) : Launch<T, 256>::go(p, blocks, s))
   dt == TSLT_F32 ? TSLT_BY_D(float) : dt == TSLT_BF16 ? TSLT_BY_D(tslt::Bf16) : TSLT_BY_D(tslt::F16);

@@ -36,7 +36,8 @@ EXPORTS = ("tslt_version", "tslt_last_error", "tslt_workspace_bytes", "tslt_trun
            "tslt_pack_bound_words", "tslt_pack", "tslt_pack_cleared", "tslt_unpack",
            "tslt_verify", "tslt_verify_accept", "tslt_verify_resample", "tslt_verify_staged", "tslt_verify_accept_staged",
            "tslt_verify_static", "tslt_truncation_stats", "tslt_multicandidate_stats", "tslt_calibrate_read", "tslt_verify_tree",
-           "tslt_cache_append", "tslt_cache_attend", "tslt_cache_attend_workspace_bytes", "tslt_cache_weigh", "tslt_cache_evict")
+           "tslt_cache_append", "tslt_cache_attend", "tslt_cache_attend_workspace_bytes", "tslt_cache_weigh", "tslt_cache_evict",
+           "tslt_rotate", "tslt_rotate_backward", "tslt_rotate_backward_workspace_bytes")
 
 class _Cache(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("heads", ctypes.c_int32),
@@ -45,6 +46,12 @@ class _Cache(ctypes.Structure):
 
 class _Rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("position", ctypes.c_void_p), ("position_seq_stride", ctypes.c_int64), ("base", ctypes.c_void_p), ("freq", ctypes.c_void_p),
+                ("axis", ctypes.c_void_p), ("axes", ctypes.c_int32), ("rotary", ctypes.c_int32), ("adjacent", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
 
 
 _lib = None
@@ -115,6 +122,13 @@ def load(path: Optional[str] = None):
     lib.tslt_cache_weigh.argtypes = [cache, vp, i64, vp, i64, i32, i32, rows, c.c_int, vp, vp, f32, vp, f32, vp, vp, vp]
     lib.tslt_cache_evict.restype = c.c_int
     lib.tslt_cache_evict.argtypes = [cache, vp, i64, vp, i64, vp, i32, i32, vp, i64, vp, vp, vp, vp, vp]
+    how = c.POINTER(_Rotation)
+    lib.tslt_rotate.restype = c.c_int
+    lib.tslt_rotate.argtypes = [rows, rows, c.c_int, i64, i32, i32, i32, i32, how, vp, rows, rows, vp, vp]
+    lib.tslt_rotate_backward_workspace_bytes.restype = sz
+    lib.tslt_rotate_backward_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    lib.tslt_rotate_backward.restype = c.c_int
+    lib.tslt_rotate_backward.argtypes = [rows, rows, rows, rows, c.c_int, i64, i32, i32, i32, i32, how, vp, rows, rows, vp, vp, vp, vp, sz, vp]
     _fast = _native_binding()
     if _fast is not None:
         _fast.bind(*[c.cast(getattr(lib, fn), vp).value for fn in (
@@ -695,4 +709,124 @@ def cache_evict(cache: dict, pages: torch.Tensor, length: torch.Tensor, weight: 
                                 new_width, _sized(out, "length", torch.int32, B), _sized(out, "kept", torch.int32, B * heads * max(keep, 0)),
                                 _sized(out, "weight", torch.float32, B * heads * new_width * PAGE_TOKENS),
                                 _sized(out, "status", torch.int32, B, optional=True), _stream()))
+    return out
+
+
+# ---- around attention and verification ---------------------------------------------------------------------------
+
+def _here(t: torch.Tensor, name: str) -> int:
+    """The current stream; t, a tensor of the call, has to live on its device."""
+    device = torch.cuda.current_device()
+    if t.device.index != device:
+        raise TsltError(f"{name} lives on {t.device}, the current device is cuda:{device}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _optional(t: Optional[torch.Tensor], name: str, dtype, shape) -> Optional[int]:
+    if t is None:
+        return None
+    _dev(t, dtype, name)
+    if tuple(t.shape) != tuple(shape):
+        raise TsltError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _given(out: dict, name: str) -> torch.Tensor:
+    if out.get(name) is None:
+        raise TsltError(f"out holds no {name}")
+    return out[name]
+
+
+def _rotation(B: int, n: int, D: int, position, freq, axis, base, q_weight, k_weight, eps, adjacent) -> _Rotation:
+    pairs = 0
+    if freq is not None:
+        _dev(freq, torch.float32, "freq")
+        if freq.dim() != 1:
+            raise TsltError("freq must be [rotary / 2]")
+        pairs = freq.numel()
+    axes, seq = 1, 0
+    if position is not None:
+        _dev(position, torch.int32, "position")
+        if position.dim() != 3 or position.shape[0] not in (1, B) or position.shape[1] != n:
+            raise TsltError(f"position must be [B or 1, {n}, axes], got {list(position.shape)}")
+        axes, seq = position.shape[2], n * position.shape[2] if position.shape[0] > 1 else 0
+    eps = -1.0 if eps is None else float(eps)
+    if eps < 0 and (q_weight is not None or k_weight is not None):
+        raise TsltError("weights belong to a norm: eps is needed")
+    return _Rotation(_ptr(position), seq, _counted(base, "base", B), _ptr(freq), _counted(axis, "axis", pairs), axes, 2 * pairs, 1 if adjacent else 0, eps,
+                     _optional(q_weight, "q_weight", torch.float32, (D,)), _optional(k_weight, "k_weight", torch.float32, (D,)))
+
+
+def rotate(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[torch.Tensor], freq: Optional[torch.Tensor],
+           axis: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+           k_weight: Optional[torch.Tensor] = None, eps: Optional[float] = None, adjacent: bool = False, count: Optional[torch.Tensor] = None,
+           out: Optional[dict] = None) -> dict:
+    """tslt_rotate: q [B, n, heads_q, D] and k [B, n, heads, D] (or None; any strides that keep rows 16-byte aligned) normed where eps is given, with
+    the weights q_weight, k_weight [D], and rotated by the angles (base [B] + position [B or 1, n, axes]) * freq [rotary / 2].  axis [rotary / 2]:
+    which axis each pair goes by; position None: token i is at i.  Returns q, k and status [B]; out may hold q and k themselves."""
+    lib = load()
+    _dev(q, name="q", contiguous=False)
+    if q.dim() != 4:
+        raise TsltError("q must be [B, n, heads_q, D]")
+    B, n, heads_q, D = q.shape
+    heads = 0
+    if k is not None:
+        if k.dim() != 4:
+            raise TsltError("k must be [B, n, heads, D]")
+        heads = k.shape[2]
+    qr, kr = _rows_of(q, "q", q.shape, q.dtype), None if k is None else _rows_of(k, "k", (B, n, heads, D), q.dtype)
+    how = _rotation(B, n, D, position, freq, axis, base, q_weight, k_weight, eps, adjacent)
+    if out is None:
+        out = {"q": torch.empty(B, n, heads_q, D, dtype=q.dtype, device=q.device),
+               "k": None if k is None else torch.empty(B, n, heads, D, dtype=q.dtype, device=q.device),
+               "status": torch.empty(B, dtype=torch.int32, device=q.device)}
+    _check(lib.tslt_rotate(qr, kr, _dtype_code(q), B, n, heads_q, heads, D, how, _counted(count, "count", B),
+                           _rows_of(_given(out, "q"), "out q", q.shape, q.dtype),
+                           None if k is None else _rows_of(_given(out, "k"), "out k", k.shape, q.dtype),
+                           _sized(out, "status", torch.int32, B, optional=True), _here(q, "q")))
+    return out
+
+
+def rotate_backward_workspace_bytes(B: int, n: int, heads_q: int, heads: int, head_dim: int) -> int:
+    return int(load().tslt_rotate_backward_workspace_bytes(B, n, heads_q, heads, head_dim))
+
+
+def rotate_backward(grad_q: torch.Tensor, grad_k: Optional[torch.Tensor], q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                    position: Optional[torch.Tensor], freq: Optional[torch.Tensor], axis: Optional[torch.Tensor] = None,
+                    base: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                    eps: Optional[float] = None, adjacent: bool = False, count: Optional[torch.Tensor] = None, out: Optional[dict] = None,
+                    workspace: Optional[torch.Tensor] = None) -> dict:
+    """tslt_rotate_backward: the gradients q and k of rotate's inputs from those of its results, and of the weights that were given (q_weight, k_weight [D]
+    fp32); q and k as rotate was given them (None without a norm).  Returns q, k, q_weight, k_weight and status [B]; out may hold grad_q and grad_k
+    themselves."""
+    lib = load()
+    _dev(grad_q, name="grad_q", contiguous=False)
+    if grad_q.dim() != 4:
+        raise TsltError("grad_q must be [B, n, heads_q, D]")
+    B, n, heads_q, D = grad_q.shape
+    dtype, dev, heads = grad_q.dtype, grad_q.device, 0
+    if grad_k is not None:
+        if grad_k.dim() != 4:
+            raise TsltError("grad_k must be [B, n, heads, D]")
+        heads = grad_k.shape[2]
+    gq = _rows_of(grad_q, "grad_q", grad_q.shape, dtype)
+    gk = None if grad_k is None else _rows_of(grad_k, "grad_k", (B, n, heads, D), dtype)
+    qr = None if q is None or eps is None else _rows_of(q, "q", grad_q.shape, dtype)
+    kr = None if k is None or eps is None or grad_k is None else _rows_of(k, "k", grad_k.shape, dtype)
+    how = _rotation(B, n, D, position, freq, axis, base, q_weight, k_weight, eps, adjacent)
+    if out is None:
+        out = {"q": torch.empty(B, n, heads_q, D, dtype=dtype, device=dev),
+               "k": None if grad_k is None else torch.empty(B, n, heads, D, dtype=dtype, device=dev),
+               "q_weight": None if q_weight is None else torch.empty(D, dtype=torch.float32, device=dev),
+               "k_weight": None if k_weight is None or grad_k is None else torch.empty(D, dtype=torch.float32, device=dev),
+               "status": torch.empty(B, dtype=torch.int32, device=dev)}
+    dq, dk = _sized(out, "q_weight", torch.float32, D, optional=True), _sized(out, "k_weight", torch.float32, D, optional=True)
+    ws = workspace
+    if ws is None and (dq or dk):
+        ws = _workspace(rotate_backward_workspace_bytes(B, n, heads_q, heads, D), dev)
+    _check(lib.tslt_rotate_backward(gq, gk, qr, kr, _dtype_code(grad_q), B, n, heads_q, heads, D, how, _counted(count, "count", B),
+                                    _rows_of(_given(out, "q"), "out q", grad_q.shape, dtype),
+                                    None if grad_k is None else _rows_of(_given(out, "k"), "out k", grad_k.shape, dtype), dq, dk,
+                                    _sized(out, "status", torch.int32, B, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
+                                    _here(grad_q, "grad_q")))
     return out

@@ -1,0 +1,75 @@
+"""What the calls around attention and verification refuse, found on the host before anything is launched."""
+import pytest
+import torch
+
+from paper_2512_16273_amd import tslt
+
+FAKE = 0x10000
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return tslt.load()
+
+
+def rows(data=FAKE, seq=1024, token=256, head=64):
+    return tslt._Rows(data, seq, token, head)
+
+
+def how(position=FAKE, seq=8, base=None, freq=FAKE, axis=None, axes=1, rotary=64, adjacent=0, eps=-1.0, qw=None, kw=None):
+    return tslt._Rotation(position, seq, base, freq, axis, axes, rotary, adjacent, eps, qw, kw)
+
+
+def message(lib):
+    return lib.tslt_last_error().decode()
+
+
+def rotation_refusals(lib, call):
+    assert call(D=80) == -2 and "head_dim" in message(lib)
+    assert call(dt=7) == -1 and call(B=-1) == -1 and call(n=0) == -1 and call(hq=0) == -1 and call(h=0) == -1
+    assert call(B=1 << 31) == -2 and call(hq=1 << 22) == -2
+    assert call(r=None) == -1
+    for rotary in (-16, 8, 72, 80):
+        assert call(r=how(rotary=rotary)) == -1 and "rotary" in message(lib)
+    assert call(r=how(axes=0)) == -1 and call(r=how(axes=5)) == -1 and "axes" in message(lib)
+    assert call(r=how(freq=None)) == -1 and call(r=how(seq=-1)) == -1
+    assert call(r=how(eps=NAN)) == -1 and call(r=how(eps=INF)) == -1
+    assert call(r=how(qw=FAKE)) == -1 and "norm" in message(lib)
+    assert call(q=None) == -1 and call(q=rows(data=FAKE + 2)) == -1 and call(q=rows(token=100)) == -1 and "16 bytes" in message(lib)
+    assert call(oq=rows(head=3)) == -1 and call(ok=None) == -1 and "together" in message(lib)
+    assert call(oq=rows(seq=2048)) == -1 and "in place" in message(lib)
+
+
+def test_rotate(lib):
+    def call(q=rows(), k=rows(), dt=1, B=2, n=4, hq=4, h=2, D=64, r=how(), oq=rows(FAKE * 2), ok=rows(FAKE * 3)):
+        if oq is not None and oq.seq_stride == 2048:
+            oq = rows(seq=2048)
+        return lib.tslt_rotate(q, k, dt, B, n, hq, h, D, r, None, oq, ok, None, None)
+    rotation_refusals(lib, call)
+    assert call(k=None) == -1 and "together" in message(lib)
+    assert call(B=0) == 0
+
+
+def test_rotate_backward(lib):
+    def call(q=rows(), k=rows(), dt=1, B=2, n=4, hq=4, h=2, D=64, r=how(), oq=rows(FAKE * 2), ok=rows(FAKE * 3), x=rows(FAKE * 4), y=rows(FAKE * 5), dq=None, dk=None,
+             ws=None, ws_bytes=0):
+        return lib.tslt_rotate_backward(q, k, x, y, dt, B, n, hq, h, D, r, None, oq, ok, dq, dk, None, ws, ws_bytes, None)
+    rotation_refusals(lib, call)
+    normed = how(eps=1e-6)
+    assert call(r=normed, x=None) == -1 and call(r=normed, y=rows(data=None)) == -1
+    assert call(dq=FAKE) == -1 and "norm" in message(lib)
+    assert call(r=normed, dk=FAKE, k=None, ok=None) == -1 and "keys" in message(lib)
+    need = lib.tslt_rotate_backward_workspace_bytes(2, 4, 4, 2, 64)
+    assert need > 0
+    for ws, size in ((None, need), (FAKE + 16, need), (FAKE, need - 1)):
+        assert call(r=normed, dq=FAKE, ws=ws, ws_bytes=size) == -3
+    assert lib.tslt_rotate_backward_workspace_bytes(2, 4, 4, 2, 80) == 0 and lib.tslt_rotate_backward_workspace_bytes(1 << 31, 4, 4, 2, 64) == 0
+
+
+def test_rotate_of_tensors():
+    cpu = torch.zeros(1, 2, 2, 64)
+    with pytest.raises(tslt.TsltError, match="GPU"):
+        tslt.rotate(cpu, None, None, None)
+    with pytest.raises(tslt.TsltError, match="GPU"):
+        tslt.rotate_backward(cpu, None, cpu, None, None, None)
