@@ -485,8 +485,9 @@ int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t widt
 /* ---- Around attention and verification ---------------------------------------------------------------------------
  *
  * What a round computes between those calls: the norms and the rotation of queries and keys before they are attended to or cached (tslt_rotate),
- * with its gradients, for a draft model that learns from what was accepted.  Rows of tokens are tslt_rows as above, also where they are written to;
- * `count` [B] int32 says how many of a sequence's n tokens there are, the first ones: 0..n, another
+ * and what a server answers with beside the verified tokens (tslt_logprob); with their gradients, for a draft model that learns from what was
+ * accepted.  Rows of tokens are tslt_rows as above, also where they are written to;
+ * `count` [B] int32 says how many of a sequence's n tokens (or entries) there are, the first ones: 0..n, another
  * counts as the nearest and sets TSLT_ROW_BAD_INDEX; NULL: all.  What belongs to the others is not read, and is left as it was. */
 
 /* Queries and keys of every head, normed and rotated: x^ = weight * x / sqrt(mean x^2 + eps), then of each pair j of the first `rotary` channels
@@ -538,6 +539,42 @@ size_t tslt_rotate_backward_workspace_bytes(int64_t B, int32_t n, int32_t heads_
 int tslt_rotate_backward(const tslt_rows* grad_q, const tslt_rows* grad_k, const tslt_rows* q, const tslt_rows* k, tslt_dtype dt, int64_t B, int32_t n,
                          int32_t heads_q, int32_t heads, int32_t head_dim, const tslt_rotation* how, const int32_t* count, const tslt_rows* out_q,
                          const tslt_rows* out_k, float* out_q_weight, float* out_k_weight, int32_t* status, void* ws, size_t ws_bytes, void* stream);
+
+/* Log probabilities under s = z * fl32(1 / T): of given tokens, ln p(t) = s_t - lse with lse = ln sum e^s, the entropy -sum p ln p, and the `top`
+ * likeliest tokens in canonical order.
+ *
+ *   logits      [B][n] rows of V logits, seq_stride elements from a sequence's first row to the next's, row_stride from row to row
+ *   index       [B][m] int32: the rows asked for (for a tree, the nodes on its verified path); outside 0..n-1 sets TSLT_ROW_BAD_INDEX
+ *               and the entry's results are those of a row that cannot be used.  NULL: m = n, row i
+ *   count       [B] int32: how many of the m entries (with tslt_verify's accept_len + 1, what was emitted); one outside 0..m is told in the status
+ *               of the sequence's first entry
+ *   tokens      [B][m] int32; -1: none asked for (its log probability is NaN); another outside 0..V-1 likewise, with TSLT_ROW_BAD_INDEX.  NULL: none
+ *   top         0..TSLT_MAX_TOP
+ *   out_logp, out_entropy, out_lse  [B][m] fp32; each may be NULL
+ *   out_top_idx [B][m][top] int32, out_top_logp [B][m][top] fp32; -1 and -inf where a row has fewer logits above -inf
+ *   status      [B][m] int32 TSLT_ROW_*; may be NULL
+ * NaN or +inf in a row (TSLT_ROW_NONFINITE), or nothing above -inf (TSLT_ROW_EMPTY): NaN, and no likeliest tokens (lse is -inf of an empty row).
+ * Terms are fp32, added up in fp32 for a lane's share and in fp64 beyond.  Workspace: tslt_logprob_workspace_bytes, 256-byte aligned; it need not be cleared.  0 where none
+ * is needed. */
+#define TSLT_MAX_TOP 32
+size_t tslt_logprob_workspace_bytes(int64_t B, int32_t m, int64_t V, int32_t top);
+int tslt_logprob(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_t V, int64_t seq_stride, int64_t row_stride, float temperature,
+                 const int32_t* index, int32_t m, const int32_t* count, const int32_t* tokens, int32_t top, float* out_logp, float* out_entropy,
+                 float* out_lse, int32_t* out_top_idx, float* out_top_logp, int32_t* status, void* ws, size_t ws_bytes, void* stream);
+
+/* The gradient of the logits, from those of tslt_logprob's results without an index (m = n):
+ * dz_j = fl32(1 / T) * (p_j (g_lse - g_logp - sum g_top - g_entropy (s_j - lse + entropy)) + g_logp [j = token] + sum_i g_top_i [j = top_idx_i]).
+ *
+ *   tokens, lse, entropy, top_idx   [B][n], top_idx [B][n][top]: as tslt_logprob was given them, and gave them.  entropy is needed with grad_entropy,
+ *               tokens with grad_logp, top_idx with grad_top.  A token or index outside 0..V-1 has no part
+ *   grad_logp, grad_entropy, grad_lse  [B][n] fp32, grad_top [B][n][top] fp32; NULL: 0
+ *   out         [B][n] rows like the logits', of their type, out_seq_stride and out_row_stride; may be the logits themselves (the same place and
+ *               strides).  Rows that do not count get zeros; rows whose lse is not finite get NaN
+ * No workspace. */
+int tslt_logprob_backward(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_t V, int64_t seq_stride, int64_t row_stride, float temperature,
+                          const int32_t* count, const int32_t* tokens, const float* lse, const float* entropy, const int32_t* top_idx, int32_t top,
+                          const float* grad_logp, const float* grad_entropy, const float* grad_lse, const float* grad_top, void* out,
+                          int64_t out_seq_stride, int64_t out_row_stride, void* stream);
 
 #ifdef __cplusplus
 }

@@ -67,10 +67,11 @@ def logprob_row(z, rT, token, top):
         return dict(none, status=1)
     if np.isneginf(z).all():
         return dict(none, lse=-np.inf, status=2)
-    s = z * rT
-    m = s.max()
-    lse = m + np.log(np.exp(s - m).sum())
-    logp = s - lse
+    m = z.max()
+    d = (z - m) * rT                                   # (of numbers near fp32's largest, lse itself has no room for ln S)
+    ln_S = np.log(np.exp(d).sum())
+    lse = m * rT + ln_S
+    logp = d - ln_S
     p = np.exp(logp)
     seen = p > 0
     order = np.lexsort((np.arange(z.size), -z))[:top]

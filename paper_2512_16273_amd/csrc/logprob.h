@@ -1,0 +1,540 @@
+// tslt_logprob: of rows of logits the normaliser, a token's log probability, the entropy and the likeliest tokens, in one pass; and the gradient of
+// the logits.
+//
+// With k = log2(e) / T and a reference c of the row's logits (the largest that a wave has met), a term is e_j = 2^(k z_j - fl(k c)), one multiply-add and
+// one exponential; S = sum e_j and E = sum e_j log2 e_j.  Then, with rho = k c - fl(k c) (added up in fp64 where terms are), lse = c / T + ln S - rho ln 2 and
+// H = ln S - ln 2 E / S.  A wave whose logits pass its reference takes the larger one: S 2^d and 2^d (E + d S), d < 0 the difference.
+//
+// The `top` largest: each wave keeps a list in LDS of the logits above what it knows `top` of its logits to reach, and cuts the list down to `top`
+// when it is full.  What it knows at first are the largest logits of its lanes in the first loads: `top` of those 64 numbers are reached by as many
+// logits.  So a logit costs nothing but its share of a comparison a load, which the reference needs as well.
+//
+// Few rows: several workgroups to a row, whose sums and lists the last of them to end joins (handover.h).
+#pragma once
+#include "handover.h"
+#include "rows.h"
+
+namespace tslt {
+
+constexpr int kMaxTop = 32;
+constexpr int kListRoom = 256;           // records of a wave's list
+
+struct LogprobParams {
+  const void* logits;
+  int64_t seq_stride, row_stride, V;
+  float rT, k2;                          // fl(1 / T), fl(log2(e) / T)
+  int64_t B;
+  int n, m, top;
+  const int32_t *index, *count, *tokens;
+  float *logp, *entropy, *lse, *top_logp;
+  int32_t *top_idx, *status;
+  int slices;                            // workgroups of a row
+  uint64_t* words;                       // [entries][slices]
+  uint64_t* part;                        // [entries][slices][3 + top]: reference, S, E, the list
+  Tag tag;
+};
+
+// Sums of a wave or of more: reference (raw logit), S and E as above.
+struct RowSums { float c; double S, E; };
+// Both with one reference.  (A side that has nothing has S = 0.)
+__device__ __forceinline__ RowSums join(const RowSums& a, const RowSums& b, double k2) {
+  const float c = fmaxf(a.c, b.c);
+  RowSums r{c, 0.0, 0.0};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const RowSums& x = i ? b : a;
+    if (x.S == 0.0) continue;
+    const double d = x.c == c ? 0.0 : k2 * (double(x.c) - double(c)), f = exp2(d);
+    r.S += f * x.S;
+    r.E += f * (x.E + d * x.S);
+  }
+  return r;
+}
+
+// A wave's list of candidate records (make_cand): value descending, index ascending, in no order.
+struct List {
+  uint64_t* at;                          // kListRoom records of LDS
+  int n;                                 // the same in all lanes, as is the threshold
+  float above;                           // nothing that is not greater than this can be among the `top`
+};
+
+// The wave's list cut down to its `top` largest records, in no order; the threshold is the least of them.
+__device__ __forceinline__ void cut(List& l, int top) {
+  wave_sync();
+  if (l.n <= top) return;
+  const int lane = lane_id();
+  uint64_t r[kListRoom / 64];
+#pragma unroll
+  for (int i = 0; i < kListRoom / 64; ++i) r[i] = lane + 64 * i < l.n ? l.at[lane + 64 * i] : 0;
+  // the largest number that `top` records reach, a bit at a time: first their values, and where several have the same their indices
+  uint64_t least = 0;
+  for (int bit = 63; bit >= 0; --bit) {
+    const uint64_t trial = least | uint64_t(1) << bit;
+    int reach = 0;
+#pragma unroll
+    for (int i = 0; i < kListRoom / 64; ++i) reach += __popcll(ballot(r[i] >= trial));
+    if (reach >= top) least = trial;
+    if (reach == top) break;
+  }
+  wave_sync();
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kListRoom / 64; ++i) {
+    const uint64_t keep = ballot(r[i] >= least);
+    if (r[i] >= least) l.at[n + lanes_below(keep)] = r[i];
+    n += __popcll(keep);
+  }
+  wave_sync();
+  l.n = n;
+  // the least value among them
+  uint32_t low = 0xFFFFFFFFu;
+#pragma unroll
+  for (int i = 0; i < kListRoom / 64; ++i)
+    if (r[i] >= least) low = min(low, uint32_t(r[i] >> 32));
+  l.above = key_to_f32(~wave_max_u32(~low));
+}
+// Records of those lanes that have one.
+__device__ __forceinline__ void offer(List& l, bool mine, uint64_t record, int top) {
+  const uint64_t who = ballot(mine);
+  if (who == 0) return;
+  if (mine) l.at[l.n + lanes_below(who)] = record;
+  l.n += __popcll(who);
+  if (l.n > kListRoom - 64) cut(l, top);
+}
+// A first threshold from the largest of every lane: `top` of them reach it.
+__device__ __forceinline__ float reached_by(float largest, int top) {
+  const uint32_t key = mono_key(largest + 0.0f);
+  uint32_t least = 0;
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t trial = least | 1u << bit;
+    if (__popcll(ballot(key >= trial)) >= top) least = trial;
+  }
+  // the number before it (before both zeros, which are equal)
+  return least > kKeyNegInf ? key_to_f32(least == 0x80000000u ? least - 2 : least - 1) : -INFINITY;
+}
+
+// What a wave has of a row.
+struct RowWave {
+  float c = -INFINITY, kc = 0.0f;        // reference, fl(k c)
+  float S = 0.0f, E = 0.0f;
+  bool far = false;                      // k c is too large for rho to be small: differences are taken first
+  List list;
+  // A vector's terms, added up by themselves first; nothing of what is -inf.
+  template <int N> __device__ __forceinline__ void terms(const float (&z)[N], float k2) {
+    float s[N], t[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float d = far ? (z[e] - c) * k2 : fmaf(z[e], k2, -kc);
+      s[e] = fast_exp2(d);
+      const float u = fmaxf(d, -200.0f);                 // (2^-200 is 0, and 0 times a number is 0)
+      t[e] = e < N / 2 || N == 1 ? s[e] * u : fmaf(s[e], u, t[e - N / 2]);
+    }
+#pragma unroll
+    for (int w = N / 2; w > 0; w /= 2)
+#pragma unroll
+      for (int e = 0; e < w; ++e) {
+        s[e] += s[e + w];
+        if (w < N / 2) t[N / 2 + e] += t[N / 2 + e + w];
+      }
+    S += s[0];
+    E += t[N / 2];
+  }
+  __device__ __forceinline__ void refer(float most, float k2) {
+    if (c != -INFINITY) {
+      const float d = (c - most) * k2, f = fast_exp2(d);
+      E = f > 0.0f ? f * fmaf(d, S, E) : 0.0f;
+      S = f * S;
+    }
+    c = most;
+    kc = c * k2;
+    far = !(fabsf(kc) < 4194304.0f);
+  }
+};
+
+struct LogprobShared {
+  uint64_t list[4][kListRoom];
+  double S[4], E[4];
+  float c[4];
+  int n[4];
+  int told, mine;
+};
+
+// Values of a vector's elements that lie past the row's end: -inf, which adds nothing and is never chosen.
+template <typename T> __device__ __forceinline__ uint4 row_vector(const uint4* body, int64_t v, int64_t end) {
+  return v < end ? load_vec_stream(body + v) : neg_inf_vec<T>();
+}
+
+template <int E> __device__ __forceinline__ float largest_of(const float (&z)[E]) {
+  const float most = max3f(z[0], z[1], z[2]);
+  if constexpr (E == 4) return fmaxf(most, z[3]);
+  else return max3f(max3f(most, z[3], z[4]), max3f(z[5], z[6], z[7]), most);
+}
+
+// All lanes of a wave: their vector's numbers, of indices first .. first + E - 1.  (A vector's numbers are not met in their order: what is offered
+// goes by the threshold from before it, which all of those behind its numbers have reached with lower indices.)
+template <typename T> __device__ __forceinline__ void take(RowWave& w, const uint4& x, int64_t first, float k2, int top) {
+  constexpr int E = ElemTraits<T>::kPerVec;
+  float z[E];
+  unpack<T>(x, z);
+  const float most = largest_of(z), above = w.list.above;
+  if (ballot(most > above) != 0) {
+    if (ballot(most > w.c) != 0) w.refer(wave_max_f32(fmaxf(most, w.c)), k2);
+    if (top == 0) w.list.above = w.c;
+    else
+#pragma unroll
+      for (int e = 0; e < E; ++e) offer(w.list, z[e] > above, make_cand(z[e], uint32_t(first + e)), top);
+  }
+  w.terms(z, k2);
+}
+
+constexpr int kAhead = 4;                // vectors of a lane that are asked for together
+
+template <typename T> __device__ void row_share(const void* row, const LogprobParams& p, int slice, LogprobShared& sh) {
+  constexpr int E = ElemTraits<T>::kPerVec;
+  const int wave = wave_id(), lane = lane_id(), top = p.top;
+  const RowSplit rs = split_row<T>(row, p.V);
+  const int64_t each = (rs.nvec + p.slices - 1) / p.slices, begin = min(each * slice, rs.nvec), end = min(begin + each, rs.nvec);
+  RowWave w;
+  w.list = List{sh.list[wave], 0, -INFINITY};
+  bool first = true;
+  // numbers before the aligned ones are the row's first, those behind them its last: equal numbers are met in their order
+  const auto edge = [&](int from, int to) {
+    const bool mine = from + lane < to;
+    const int64_t i = edge_index<T>(rs, mine ? from + lane : from);
+    const float z = mine ? load_elem<T>(row, i) : -INFINITY, most = wave_max_f32(z);
+    if (most > w.c) w.refer(most, p.k2);
+    if (top > 0) offer(w.list, z > w.list.above, make_cand(z, uint32_t(i)), top);
+    const float one[1] = {z};
+    w.terms(one, p.k2);
+  };
+  if (slice == 0 && wave == 0 && rs.head > 0) edge(0, rs.head);
+  for (int64_t v0 = begin + wave * 64; v0 < end; v0 += 4 * 64 * kAhead) {
+    uint4 x[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) x[u] = row_vector<T>(rs.body, v0 + u * 256 + lane, end);
+    if (first) {
+      float most = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        float z[E];
+        unpack<T>(x[u], z);
+        most = fmaxf(most, largest_of(z));
+      }
+      const float all = wave_max_f32(fmaxf(most, w.c));
+      if (all > w.c) w.refer(all, p.k2);
+      w.list.above = top > 0 ? fmaxf(w.list.above, reached_by(most, top)) : w.c;
+      first = false;
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) take<T>(w, x[u], rs.head + (v0 + u * 256 + lane) * E, p.k2, top);
+  }
+  if (slice == p.slices - 1 && wave == 0 && rs.tail > 0) edge(rs.head, rs.head + rs.tail);
+  const double S = wave_sum_f64(double(w.S)), Es = wave_sum_f64(double(w.E));
+  if (top > 0) cut(w.list, top);
+  if (lane == 0) {
+    // (the terms' common factor 2^rho goes here, so that sums of different references can be joined)
+    const double rho = w.far || w.c == -INFINITY ? 0.0 : double(p.k2) * double(w.c) - double(w.kc), f = exp2(-rho);
+    sh.S[wave] = f * S;
+    sh.E[wave] = f * (Es - rho * S);
+    sh.c[wave] = w.c;
+    sh.n[wave] = w.list.n;
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ RowSums all_waves(const LogprobShared& sh, double k2) {
+  RowSums r{sh.c[0], sh.S[0], sh.E[0]};
+#pragma unroll
+  for (int w = 1; w < 4; ++w) r = join(r, RowSums{sh.c[w], sh.S[w], sh.E[w]}, k2);
+  return r;
+}
+
+// The results of an entry, from its row's sums and the waves' lists.
+template <typename T> __device__ void finish(const LogprobParams& p, int64_t entry, const void* row, const RowSums& sums, int status, LogprobShared& sh) {
+  const int tid = threadIdx.x, top = p.top;
+  status |= sums.S != sums.S || sums.c == INFINITY ? 1 : sums.c == -INFINITY ? 2 : 0;
+  // (log probabilities from differences to the reference: of logits near fp32's largest the normaliser has no room for ln S)
+  const double rT = p.rT, c = sums.c, ln_S = log(sums.S), lse = c * rT + ln_S;
+  if (tid == 0) {
+    const int32_t token = p.tokens ? as_global(p.tokens)[entry] : -1;
+    const bool there = token >= 0 && token < p.V;
+    double logp = NAN;
+    if (there && (status & 3) == 0) logp = (double(load_elem<T>(row, token)) - c) * rT - ln_S;
+    if (!there && token != -1) status |= kBadIndex;
+    const bool usable = (status & 3) == 0;
+    if (p.logp) p.logp[entry] = float(logp);
+    if (p.entropy) p.entropy[entry] = usable ? float(fmax(ln_S - 0.69314718055994530942 * sums.E / sums.S, 0.0)) : NAN;
+    if (p.lse) p.lse[entry] = usable ? float(lse) : status & 1 ? NAN : -INFINITY;
+    if (p.status) p.status[entry] = status;
+  }
+  if (top == 0) return;
+  // the lists of four waves: a record's place is how many are larger
+  uint64_t mine = 0;
+  int place = 0;
+  if ((status & 3) == 0 && tid < 4 * top) {
+    const int w = tid / top, i = tid - w * top;
+    if (i < sh.n[w]) mine = sh.list[w][i];
+  }
+  int total = 0;
+  for (int w = 0; w < 4; ++w) {
+    const int n = sh.n[w];
+    total += n;
+    for (int i = 0; i < n; ++i) place += sh.list[w][i] > mine ? 1 : 0;
+  }
+  if ((status & 3) != 0) total = 0;
+  if (mine != 0 && place < top) {
+    p.top_idx[entry * top + place] = int32_t(cand_index(mine));
+    p.top_logp[entry * top + place] = float((double(cand_value(mine)) - c) * rT - ln_S);
+  }
+  if (tid < top && tid >= total) {
+    p.top_idx[entry * top + tid] = -1;
+    p.top_logp[entry * top + tid] = -INFINITY;
+  }
+}
+
+// An entry whose row cannot be used.
+__device__ __forceinline__ void refuse(const LogprobParams& p, int64_t entry, int status) {
+  const int tid = threadIdx.x;
+  if (tid == 0) {
+    if (p.logp) p.logp[entry] = NAN;
+    if (p.entropy) p.entropy[entry] = NAN;
+    if (p.lse) p.lse[entry] = NAN;
+    if (p.status) p.status[entry] = status;
+  }
+  if (tid < p.top) {
+    p.top_idx[entry * p.top + tid] = -1;
+    p.top_logp[entry * p.top + tid] = -INFINITY;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void logprob_kernel(const LogprobParams p) {
+  __shared__ LogprobShared sh;
+  const int tid = threadIdx.x, wave = wave_id(), lane = lane_id();
+  const uint32_t entry = blockIdx.x / uint32_t(p.slices);
+  const int slice = int(blockIdx.x - entry * uint32_t(p.slices));
+  const uint32_t b = entry / uint32_t(p.m);
+  const int j = int(entry - b * uint32_t(p.m));
+  // (a count that does not fit is told in the status of the sequence's first entry, also where that one does not count)
+  const int odd = j == 0 && p.count && as_global(p.count)[b] != counted(p.count, b, p.m) ? kBadIndex : 0;
+  if (j >= counted(p.count, b, p.m)) {
+    if (odd && slice == 0 && tid == 0 && p.status) p.status[entry] = odd;
+    return;
+  }
+  const int at = p.index ? as_global(p.index)[entry] : j;
+  if (at < 0 || at >= p.n) {
+    if (slice == 0) refuse(p, entry, kBadIndex);
+    return;
+  }
+  const void* row = reinterpret_cast<const char*>(p.logits) + (int64_t(b) * p.seq_stride + at * p.row_stride) * ElemTraits<T>::kBytes;
+  row_share<T>(row, p, slice, sh);
+  RowSums sums = all_waves(sh, p.k2);
+  if (p.slices > 1) {
+    const int size = 3 + p.top;
+    uint64_t* words = p.words + int64_t(entry) * p.slices;
+    uint64_t* part = p.part + int64_t(entry) * p.slices * size;
+    uint64_t* own = part + slice * size;
+    // this slice's list: the largest of its waves' (0 behind them, which is less than any record)
+    if (p.top > 0) {
+      uint64_t mine = 0;
+      int place = 0, total = 0;
+      if (tid < 4 * p.top) {
+        const int w = tid / p.top, i = tid - w * p.top;
+        if (i < sh.n[w]) mine = sh.list[w][i];
+      }
+      for (int w = 0; w < 4; ++w) {
+        total += sh.n[w];
+        for (int i = 0; i < sh.n[w]; ++i) place += sh.list[w][i] > mine ? 1 : 0;
+      }
+      if (mine != 0 && place < p.top) store_through(own + 3 + place, mine);
+      if (tid < p.top && tid >= total) store_through(own + 3 + tid, 0);
+    }
+    if (tid == 0) {
+      store_through(own, as_u32(sums.c));
+      store_through(own + 1, __builtin_bit_cast(uint64_t, sums.S));
+      store_through(own + 2, __builtin_bit_cast(uint64_t, sums.E));
+    }
+    if (!all_arrived(words, slice, p.slices, p.tag, sh.told)) return;
+    if (wave == 0) {
+      const bool mine = claimed(words, p.slices, p.tag);
+      if (lane == 0) sh.mine = mine;
+    }
+    __syncthreads();
+    if (!sh.mine) return;
+    // A lane has a slice's sums.  The lists lie in the order of the row: of equal numbers the first are met first, so that the threshold from before
+    // 64 records holds for all of them.
+    if (wave == 0) {
+      const uint64_t* from = part + min(lane, p.slices - 1) * size;
+      RowSums got{as_f32(uint32_t(load_through(from))), __builtin_bit_cast(double, load_through(from + 1)), __builtin_bit_cast(double, load_through(from + 2))};
+      if (lane >= p.slices) got = RowSums{-INFINITY, 0.0, 0.0};
+      const RowSums all = join(got, RowSums{wave_max_f32(got.c), 0.0, 0.0}, p.k2);
+      const double S = wave_sum_f64(all.S), Es = wave_sum_f64(all.E);
+      if (lane < 4) { sh.c[lane] = all.c; sh.S[lane] = lane == 0 ? S : 0.0; sh.E[lane] = lane == 0 ? Es : 0.0; }
+    }
+    List list{sh.list[wave], 0, -INFINITY};
+    if (p.top > 0) {
+      const int records = p.slices * p.top, each = (records + 3) / 4, from = wave * each, to = min(from + each, records);
+      for (int r0 = from; r0 < to; r0 += 64 * kAhead) {
+        uint64_t r[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int i = r0 + 64 * u + lane, s = min(i, records - 1) / p.top;
+          r[u] = i < to ? load_through(part + s * size + 3 + (i - s * p.top)) : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) offer(list, r[u] != 0 && cand_value(r[u]) > list.above, r[u], p.top);
+      }
+      cut(list, p.top);
+    }
+    if (lane == 0) sh.n[wave] = list.n;
+    __syncthreads();
+    sums = all_waves(sh, p.k2);
+  }
+  finish<T>(p, entry, row, sums, odd, sh);
+}
+
+// ---- the gradient of the logits ---------------------------------------------------------------------------------
+//
+// dz = (1 / T) (p (c0 + c1 log2 p) + what the token and the likeliest ones were given), p = 2^(k z - k T lse): elementwise, bound by
+// reading a row and writing one.  The few numbers of the second part are put in place by the lanes that have written there.
+
+struct LogprobBackwardParams {
+  const void* logits;
+  void* out;
+  int64_t seq_stride, row_stride, out_seq_stride, out_row_stride, V;
+  float rT, k2;
+  int n, top;
+  const int32_t *count, *tokens, *top_idx;
+  const float *lse, *entropy, *grad_logp, *grad_entropy, *grad_lse, *grad_top;
+  int slices;
+};
+
+// 16 bytes of a row at any alignment of its elements.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+__device__ __forceinline__ uint4 load_any(const void* p) {
+  const u32x4 r = *(const u32x4_any __attribute__((address_space(1)))*)p;
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+template <typename T> __device__ __forceinline__ void store_elem(void* row, int64_t i, float v);
+template <> __device__ __forceinline__ void store_elem<float>(void* row, int64_t i, float v) { reinterpret_cast<float*>(row)[i] = v; }
+template <> __device__ __forceinline__ void store_elem<Bf16>(void* row, int64_t i, float v) { reinterpret_cast<__bf16*>(row)[i] = __bf16(v); }
+template <> __device__ __forceinline__ void store_elem<F16>(void* row, int64_t i, float v) { reinterpret_cast<_Float16*>(row)[i] = _Float16(v); }
+template <typename T> struct Vector16;
+template <> struct Vector16<float> {
+  static __device__ __forceinline__ u32x4 pack(const float (&v)[4]) { return u32x4{as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])}; }
+};
+template <typename T> struct Vector16 {
+  static __device__ __forceinline__ u32x4 pack(const float (&v)[8]) {
+    Eight<T> e;
+    e.set(v);
+    return e.w;
+  }
+};
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobBackwardParams p) {
+  constexpr int E = ElemTraits<T>::kPerVec, kBytes = ElemTraits<T>::kBytes;
+  __shared__ int64_t place[kMaxTop + 1];
+  __shared__ float given[kMaxTop + 1], put[kMaxTop + 1];
+  const int tid = threadIdx.x, lane = lane_id();
+  const uint32_t entry = blockIdx.x / uint32_t(p.slices);
+  const int slice = int(blockIdx.x - entry * uint32_t(p.slices));
+  const uint32_t b = entry / uint32_t(p.n);
+  const int i = int(entry - b * uint32_t(p.n));
+  const char* row = reinterpret_cast<const char*>(p.logits) + (int64_t(b) * p.seq_stride + i * p.row_stride) * kBytes;
+  char* out = reinterpret_cast<char*>(p.out) + (int64_t(b) * p.out_seq_stride + i * p.out_row_stride) * kBytes;
+  // the split goes by where the results lie; the logits may lie otherwise
+  const RowSplit rs = split_row<T>(out, p.V);
+  const int64_t each = (rs.nvec + p.slices - 1) / p.slices, begin = min(each * slice, rs.nvec), end = min(begin + each, rs.nvec);
+  const bool first = slice == 0, last = slice == p.slices - 1, there = i < counted(p.count, b, p.n);
+  const int edges = (first ? rs.head : 0) + (last ? rs.tail : 0);
+  const int64_t edge_at = tid < edges ? edge_index<T>(rs, first ? tid : rs.head + tid) : 0;
+  u32x4* body = reinterpret_cast<u32x4*>(out + size_t(rs.head) * kBytes);
+  const char* from = row + size_t(rs.head) * kBytes;
+
+  // the row's constants, in every wave
+  double c0 = 0.0, c1 = 0.0, rho = 0.0;
+  float far_c = 0.0f, hi = 0.0f;
+  bool known = true, far = false;
+  if (there) {
+    const float lse = as_global(p.lse)[entry];
+    known = fabsf(lse) < INFINITY;
+    const double reference = double(lse) / double(p.rT), scaled = double(p.k2) * reference;
+    far = !(fabs(scaled) < 4194304.0);
+    far_c = float(reference);
+    hi = float(scaled);
+    rho = far ? 0.0 : scaled - double(hi);
+    if (p.grad_lse) c0 += as_global(p.grad_lse)[entry];
+    if (p.grad_entropy) {
+      const double g = as_global(p.grad_entropy)[entry];
+      c0 -= g * as_global(p.entropy)[entry];
+      c1 = -g * 0.69314718055994530942;
+    }
+    int64_t j = -1;
+    float g = 0.0f;
+    if (lane == 0 && p.grad_logp) {
+      j = as_global(p.tokens)[entry];
+      g = as_global(p.grad_logp)[entry];
+    } else if (lane > 0 && lane <= p.top) {
+      j = as_global(p.top_idx)[int64_t(entry) * p.top + lane - 1];
+      g = as_global(p.grad_top)[int64_t(entry) * p.top + lane - 1];
+    }
+    const bool counts = j >= 0 && j < p.V;
+    c0 -= wave_sum_f64(counts ? double(g) : 0.0);
+    if (tid <= p.top) {
+      place[tid] = counts ? j : -1;
+      given[tid] = g;
+    }
+  }
+  const float f = float(exp2(-rho) * double(p.rT)), a0 = f * float(c0 - c1 * rho), a1 = f * float(c1), k2 = p.k2, none = there ? NAN : 0.0f;
+  const bool fill = !there || !known;
+  // (a p of 0 gives 0, whatever its logarithm)
+  const auto gradient = [&](float z) {
+    const float d = far ? (z - far_c) * k2 : fmaf(z, k2, -hi);
+    return fill ? none : fast_exp2(d) * fmaf(a1, fmaxf(d, -200.0f), a0);
+  };
+  __syncthreads();
+  // the given places in this share: their numbers, before the logits are written over (by this share alone)
+  if (!fill && tid <= p.top) {
+    const int64_t j = place[tid];
+    float sum = 0.0f;
+    for (int k = 0; k <= p.top; ++k) sum += place[k] == j ? given[k] : 0.0f;
+    const int64_t lo = first ? 0 : rs.head + begin * E, hi_at = last ? p.V : rs.head + end * E;
+    if (j >= lo && j < hi_at) put[tid] = fmaf(p.rT, sum, gradient(load_elem<T>(row, j)));
+    else if (j >= 0) place[tid] = -1;
+  }
+  __syncthreads();
+  if (tid < edges) store_elem<T>(out, edge_at, gradient(fill ? 0.0f : load_elem<T>(row, edge_at)));
+  constexpr int kAheadBack = 4;
+  for (int64_t v0 = begin + tid; v0 < end; v0 += kBlock * kAheadBack) {
+    uint4 x[kAheadBack];
+#pragma unroll
+    for (int u = 0; u < kAheadBack; ++u)
+      if (!fill && v0 + u * kBlock < end) x[u] = load_any(from + (v0 + u * kBlock) * 16);
+#pragma unroll
+    for (int u = 0; u < kAheadBack; ++u) {
+      if (v0 + u * kBlock >= end) break;
+      float z[E];
+      if (fill) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] = none;
+      } else {
+        unpack<T>(x[u], z);
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] = gradient(z[e]);
+      }
+      body[v0 + u * kBlock] = Vector16<T>::pack(z);
+    }
+  }
+  if (fill) return;
+  // whoever has written there
+  for (int k = 0; k <= p.top; ++k) {
+    const int64_t j = place[k];
+    if (j < 0) continue;
+    const int64_t in_body = j - rs.head, v = in_body / E;
+    const bool edge = in_body < 0 || v >= rs.nvec;
+    if (edge ? tid < edges && edge_at == j : tid == int((v - begin) % kBlock)) store_elem<T>(out, j, put[k]);
+  }
+}
+
+}  // namespace tslt

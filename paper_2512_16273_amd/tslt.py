@@ -29,6 +29,7 @@ OP_TRUNCATE, OP_SAMPLE, OP_VERIFY, OP_VERIFY_TREE, OP_VERIFY_TREE_PATH, OP_TRUNC
 ROW_NONFINITE, ROW_EMPTY, ROW_TOKEN_NOT_IN_SET, ROW_BAD_SET, ROW_EXACT_PATH = 1, 2, 4, 8, 256
 ROW_BAD_PAGE, ROW_BAD_INDEX = 16, 32
 PAGE_TOKENS = 64
+MAX_TOP = 32
 MAX_K_CAP = 1024
 PAYLOAD = {"f32": 0, "bf16": 1, "f16": 2}       # tslt_dtype codes of the formats a payload can travel in
 
@@ -37,7 +38,8 @@ EXPORTS = ("tslt_version", "tslt_last_error", "tslt_workspace_bytes", "tslt_trun
            "tslt_verify", "tslt_verify_accept", "tslt_verify_resample", "tslt_verify_staged", "tslt_verify_accept_staged",
            "tslt_verify_static", "tslt_truncation_stats", "tslt_multicandidate_stats", "tslt_calibrate_read", "tslt_verify_tree",
            "tslt_cache_append", "tslt_cache_attend", "tslt_cache_attend_workspace_bytes", "tslt_cache_weigh", "tslt_cache_evict",
-           "tslt_rotate", "tslt_rotate_backward", "tslt_rotate_backward_workspace_bytes")
+           "tslt_rotate", "tslt_rotate_backward", "tslt_rotate_backward_workspace_bytes",
+           "tslt_logprob", "tslt_logprob_workspace_bytes", "tslt_logprob_backward")
 
 class _Cache(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("heads", ctypes.c_int32),
@@ -129,6 +131,12 @@ def load(path: Optional[str] = None):
     lib.tslt_rotate_backward_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
     lib.tslt_rotate_backward.restype = c.c_int
     lib.tslt_rotate_backward.argtypes = [rows, rows, rows, rows, c.c_int, i64, i32, i32, i32, i32, how, vp, rows, rows, vp, vp, vp, vp, sz, vp]
+    lib.tslt_logprob_workspace_bytes.restype = sz
+    lib.tslt_logprob_workspace_bytes.argtypes = [i64, i32, i64, i32]
+    lib.tslt_logprob.restype = c.c_int
+    lib.tslt_logprob.argtypes = [vp, c.c_int, i64, i32, i64, i64, i64, f32, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.tslt_logprob_backward.restype = c.c_int
+    lib.tslt_logprob_backward.argtypes = [vp, c.c_int, i64, i32, i64, i64, i64, f32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i64, i64, vp]
     _fast = _native_binding()
     if _fast is not None:
         _fast.bind(*[c.cast(getattr(lib, fn), vp).value for fn in (
@@ -829,4 +837,86 @@ def rotate_backward(grad_q: torch.Tensor, grad_k: Optional[torch.Tensor], q: Opt
                                     None if grad_k is None else _rows_of(_given(out, "k"), "out k", grad_k.shape, dtype), dq, dk,
                                     _sized(out, "status", torch.int32, B, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
                                     _here(grad_q, "grad_q")))
+    return out
+
+
+def _logits(t: torch.Tensor, name: str):
+    """[B, n, V], dense along V; strides of sequences and rows."""
+    _dev(t, name=name, contiguous=False)
+    if t.dim() != 3:
+        raise TsltError(f"{name} must be [B, n, V]")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise TsltError(f"{name} must be dense along the vocabulary")
+    return tuple(s if n > 1 else 0 for s, n in zip(t.stride()[:2], t.shape[:2]))
+
+
+def logprob_workspace_bytes(B: int, m: int, V: int, top: int) -> int:
+    return int(load().tslt_logprob_workspace_bytes(B, m, V, top))
+
+
+def logprob(logits: torch.Tensor, temperature: float, tokens: Optional[torch.Tensor] = None, top: int = 0, index: Optional[torch.Tensor] = None,
+            count: Optional[torch.Tensor] = None, out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None) -> dict:
+    """tslt_logprob: logits [B, n, V] (any strides, dense along V); of the rows index [B, m] (None: all n), the first count [B] of them, the log probability
+    of tokens [B, m] (-1: none), the entropy and the normaliser, and the `top` likeliest tokens with theirs.  Returns logp, entropy, lse, status [B, m] and, with
+    top, top_idx and top_logp [B, m, top]; of a given out what it holds."""
+    lib = load()
+    seq, row = _logits(logits, "logits")
+    B, n, V = logits.shape
+    top = int(top)
+    if index is not None and index.dim() != 2:
+        raise TsltError("index must be [B, m]")
+    m = n if index is None else index.shape[1]
+    dev = logits.device
+    if out is None:
+        out = {name: torch.empty(B, m, dtype=torch.float32, device=dev) for name in ("logp", "entropy", "lse")}
+        out["status"] = torch.empty(B, m, dtype=torch.int32, device=dev)
+        if top > 0:
+            out["top_idx"] = torch.empty(B, m, top, dtype=torch.int32, device=dev)
+            out["top_logp"] = torch.empty(B, m, top, dtype=torch.float32, device=dev)
+    ws = workspace
+    if ws is None:
+        ws = _workspace(logprob_workspace_bytes(B, m, V, top) if B else 0, dev)
+    results = [_sized(out, name, torch.float32, B * m, optional=True) for name in ("logp", "entropy", "lse")]
+    _check(lib.tslt_logprob(logits.data_ptr(), _dtype_code(logits), B, n, V, seq, row, float(temperature), _counted(index, "index", B * m), m,
+                            _counted(count, "count", B), _counted(tokens, "tokens", B * m), top, *results,
+                            _sized(out, "top_idx", torch.int32, B * m * top) if top > 0 else None,
+                            _sized(out, "top_logp", torch.float32, B * m * top) if top > 0 else None,
+                            _sized(out, "status", torch.int32, B * m, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
+                            _here(logits, "logits")))
+    return out
+
+
+def logprob_backward(logits: torch.Tensor, temperature: float, tokens: Optional[torch.Tensor], lse: torch.Tensor, entropy: Optional[torch.Tensor] = None,
+                     grad_logp: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None, grad_lse: Optional[torch.Tensor] = None,
+                     top_idx: Optional[torch.Tensor] = None, grad_top: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                     out: Optional[dict] = None) -> dict:
+    """tslt_logprob_backward: the gradient `logits` [B, n, V] of what logprob was given, without an index, from those of its results (None: 0); tokens, lse,
+    entropy, top_idx as it was given them and gave them.  out may hold the logits themselves."""
+    lib = load()
+    seq, row = _logits(logits, "logits")
+    B, n, V = logits.shape
+    top = 0
+    if grad_top is not None:
+        if grad_top.dim() != 3:
+            raise TsltError("grad_top must be [B, n, top]")
+        top = grad_top.shape[2]
+        if not 1 <= top <= MAX_TOP:
+            raise TsltError(f"grad_top must be [B, n, top] with top from 1 to {MAX_TOP}")
+    if out is None:
+        out = {"logits": torch.empty(B, n, V, dtype=logits.dtype, device=logits.device)}
+    made = _given(out, "logits")
+    out_seq, out_row = _logits(made, "out logits")
+    if made.shape != logits.shape or made.dtype != logits.dtype:
+        raise TsltError(f"out logits must be {list(logits.shape)} of {logits.dtype}")
+    if lse is None:
+        raise TsltError("lse is needed")
+
+    def given(t, name):
+        return _optional(t, name, torch.float32, (B, n))
+    _check(lib.tslt_logprob_backward(logits.data_ptr(), _dtype_code(logits), B, n, V, seq, row, float(temperature), _counted(count, "count", B),
+                                     _counted(tokens, "tokens", B * n), given(lse, "lse"), given(entropy, "entropy"),
+                                     _counted(top_idx, "top_idx", B * n * top) if top else None, top, given(grad_logp, "grad_logp"),
+                                     given(grad_entropy, "grad_entropy"), given(grad_lse, "grad_lse"),
+                                     _optional(grad_top, "grad_top", torch.float32, (B, n, top)), made.data_ptr(), out_seq, out_row,
+                                     _here(logits, "logits")))
     return out

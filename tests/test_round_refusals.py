@@ -73,3 +73,43 @@ def test_rotate_of_tensors():
         tslt.rotate(cpu, None, None, None)
     with pytest.raises(tslt.TsltError, match="GPU"):
         tslt.rotate_backward(cpu, None, cpu, None, None, None)
+
+
+def test_logprob(lib):
+    def call(z=FAKE, dt=1, B=2, n=3, V=1000, T=1.0, index=None, m=3, tokens=None, top=0, idx=None, logp=None, ws=FAKE * 2, ws_bytes=1 << 30):
+        return lib.tslt_logprob(z, dt, B, n, V, n * V, V, T, index, m, None, tokens, top, None, None, None, idx, logp, None, ws, ws_bytes, None)
+    assert call(dt=9) == -1 and call(B=-1) == -1 and call(n=0) == -1 and call(V=0) == -1 and call(z=None) == -1
+    assert call(V=1 << 31) == -2 and call(dt=0, V=1 << 30) == -2 and call(B=1 << 31) == -2 and call(index=FAKE, m=1 << 30, B=4) == -2
+    for T in (0.0, -1.0, NAN, INF, 1e-39):
+        assert call(T=T) == -1 and "temperature" in message(lib)
+    assert call(m=2) == -1 and call(index=FAKE, m=0) == -1 and "index" in message(lib)
+    assert call(top=33) == -2 and call(top=-1) == -2 and call(top=4) == -1 and call(top=4, idx=FAKE) == -1
+    assert call(z=FAKE + 1) == -1 and "aligned" in message(lib)
+    need = lib.tslt_logprob_workspace_bytes(2, 3, 100000, 0)
+    assert need > 0
+    for ws, size in ((None, need), (FAKE + 16, need), (FAKE, 64)):
+        assert call(V=100000, ws=ws, ws_bytes=size) == -3 and "workspace" in message(lib)
+    assert call(B=0) == 0
+    assert lib.tslt_logprob_workspace_bytes(0, 3, 1000, 0) == 0 and lib.tslt_logprob_workspace_bytes(1 << 31, 3, 1000, 0) == 0
+    assert lib.tslt_logprob_workspace_bytes(2, 3, 1000, 33) == 0
+
+
+def test_logprob_backward(lib):
+    def call(z=FAKE, dt=1, B=2, n=3, V=1000, T=1.0, tokens=FAKE, lse=FAKE, entropy=FAKE, idx=FAKE, top=2, g=FAKE, gh=FAKE, gt=FAKE, out=FAKE * 2, stride=1000):
+        return lib.tslt_logprob_backward(z, dt, B, n, V, n * V, V, T, None, tokens, lse, entropy, idx, top, g, gh, None, gt, out, n * stride, stride, None)
+    assert call(dt=9) == -1 and call(B=-1) == -1 and call(n=0) == -1 and call(V=0) == -1 and call(z=None) == -1 and call(out=None) == -1 and call(lse=None) == -1
+    assert call(V=1 << 31) == -2 and call(B=1 << 31) == -2 and call(T=0.0) == -1 and call(top=33) == -2
+    assert call(tokens=None) == -1 and "tokens" in message(lib)
+    assert call(entropy=None) == -1 and "entropy" in message(lib)
+    assert call(idx=None) == -1 and call(top=0) == -1 and "top_idx" in message(lib)
+    assert call(z=FAKE + 1) == -1 and call(out=FAKE + 1) == -1
+    assert call(out=FAKE, stride=1008) == -1 and "written over" in message(lib)
+    assert call(B=0) == 0
+
+
+def test_logprob_of_tensors():
+    z = torch.zeros(1, 2, 8)
+    with pytest.raises(tslt.TsltError, match="GPU"):
+        tslt.logprob(z, 1.0)
+    with pytest.raises(tslt.TsltError, match="GPU"):
+        tslt.logprob_backward(z, 1.0, None, z[..., 0])
