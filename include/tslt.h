@@ -484,11 +484,31 @@ int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t widt
 
 /* ---- Around attention and verification ---------------------------------------------------------------------------
  *
- * What a round computes between those calls: the norms and the rotation of queries and keys before they are attended to or cached (tslt_rotate),
- * and what a server answers with beside the verified tokens (tslt_logprob); with their gradients, for a draft model that learns from what was
- * accepted.  Rows of tokens are tslt_rows as above, also where they are written to;
- * `count` [B] int32 says how many of a sequence's n tokens (or entries) there are, the first ones: 0..n, another
+ * What a round of many requests computes between those calls: each sequence's own low-rank adapter beside a projection that all
+ * share (tslt_adapt), the norms and the rotation of queries and keys before they are attended to or cached (tslt_rotate), and what
+ * a server answers with beside the verified tokens (tslt_logprob); with the gradients of the last two, for a draft model that learns from
+ * what was accepted.  Rows of tokens are tslt_rows as above ([B][n][heads][D], or [B][n][width], whose head_stride does not count), also where
+ * they are written to; `count` [B] int32 says how many of a sequence's n tokens (or entries) there are, the first ones: 0..n, another
  * counts as the nearest and sets TSLT_ROW_BAD_INDEX; NULL: all.  What belongs to the others is not read, and is left as it was. */
+
+/* Adapters of many requests: out_t = base_t + scale_a * (x_t A_a^T) B_a^T, a = adapter of the token's sequence.
+ *
+ *   x           [B][n][K] of type dt, what the projection was given;  base [B][n][N], what it gave, in rows of any alignment
+ *   a, b        [n_adapters][R][K] and [n_adapters][N][R] of type dt, 16-byte aligned
+ *   R           a multiple of 16, at most TSLT_MAX_ADAPTER_RANK;  rank [n_adapters] int32: how many of an adapter's R count (0..R,
+ *               another counts as the nearest; the others are not looked at, whatever they hold); NULL: all
+ *   adapter     [B] int32; -1: none, out = base.  Another outside 0..n_adapters-1 counts as none and sets TSLT_ROW_BAD_INDEX
+ *   scale       [n_adapters] fp32; NULL: 1
+ *   out         [B][n][N] of type dt, in rows of any alignment; may be base itself (the same place and strides)
+ *   status      [B] int32; may be NULL
+ * Sums are fp32; x A^T meets B in two terms of the rows' type (16 bits of it for bfloat16, 22 for binary16; fp32 rows: as it is), and the result is
+ * rounded once.  A token whose x A^T is not finite gets NaN, or whatever fp32's rules give.
+ * K a multiple of 16 bytes' elements, N any.  Workspace: tslt_adapt_workspace_bytes of the same arguments, 256-byte aligned; it need not be cleared. */
+#define TSLT_MAX_ADAPTER_RANK 256
+size_t tslt_adapt_workspace_bytes(int64_t B, int32_t n, int32_t K, int32_t N, int32_t R);
+int tslt_adapt(const tslt_rows* x, int32_t K, const tslt_rows* base, const tslt_rows* out, int32_t N, tslt_dtype dt, int64_t B, int32_t n,
+               const void* a, const void* b, int64_t n_adapters, int32_t R, const int32_t* adapter, const float* scale, const int32_t* rank,
+               const int32_t* count, int32_t* status, void* ws, size_t ws_bytes, void* stream);
 
 /* Queries and keys of every head, normed and rotated: x^ = weight * x / sqrt(mean x^2 + eps), then of each pair j of the first `rotary` channels
  * (u, v) -> (u cos - v sin, v cos + u sin) by the angle (base[b] + position[b][i][axis[j]]) * freq[j].

@@ -14,9 +14,9 @@ ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libtslt.so")
 BINDING_PATH = os.path.join(HERE, "_binding.so")
 BINDING_SOURCE = os.path.join(HERE, "csrc", "binding.cpp")
-SOURCES = [os.path.join(HERE, "csrc", n) for n in ("tslt.hip", "cache.hip", "attend_f32.hip", "attend_bf16.hip", "attend_f16.hip", "rotate.hip", "logprob.hip")]
+SOURCES = [os.path.join(HERE, "csrc", n) for n in ("tslt.hip", "cache.hip", "attend_f32.hip", "attend_bf16.hip", "attend_f16.hip", "rotate.hip", "logprob.hip", "adapt.hip")]
 HEADERS = [os.path.join(HERE, "csrc", n) for n in ("common.h", "bins.h", "handover.h", "pow_table.h", "truncate.h", "sample.h", "verify.h", "rowops.h", "rowsample.h", "exp64.h", "tree.h", "wire.h", "stats.h", "calib.h",
-                                                   "error.h", "checks.h", "rows.h", "cache.h", "append.h", "attend.h", "attend_launch.h", "weigh.h", "evict.h", "rotate.h", "logprob.h")] + \
+                                                   "error.h", "checks.h", "rows.h", "cache.h", "append.h", "attend.h", "attend_launch.h", "weigh.h", "evict.h", "rotate.h", "logprob.h", "adapt.h")] + \
           [os.path.join(ROOT, "include", "tslt.h")]
 
 

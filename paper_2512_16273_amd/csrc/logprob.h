@@ -409,12 +409,6 @@ struct LogprobBackwardParams {
   int slices;
 };
 
-// 16 bytes of a row at any alignment of its elements.
-typedef u32x4 u32x4_any __attribute__((aligned(2)));
-__device__ __forceinline__ uint4 load_any(const void* p) {
-  const u32x4 r = *(const u32x4_any __attribute__((address_space(1)))*)p;
-  return make_uint4(r[0], r[1], r[2], r[3]);
-}
 template <typename T> __device__ __forceinline__ void store_elem(void* row, int64_t i, float v);
 template <> __device__ __forceinline__ void store_elem<float>(void* row, int64_t i, float v) { reinterpret_cast<float*>(row)[i] = v; }
 template <> __device__ __forceinline__ void store_elem<Bf16>(void* row, int64_t i, float v) { reinterpret_cast<__bf16*>(row)[i] = __bf16(v); }
@@ -510,7 +504,10 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
     uint4 x[kAheadBack];
 #pragma unroll
     for (int u = 0; u < kAheadBack; ++u)
-      if (!fill && v0 + u * kBlock < end) x[u] = load_any(from + (v0 + u * kBlock) * 16);
+      if (!fill && v0 + u * kBlock < end) {
+        const u32x4 r = load16_any(from + (v0 + u * kBlock) * 16);
+        x[u] = make_uint4(r[0], r[1], r[2], r[3]);
+      }
 #pragma unroll
     for (int u = 0; u < kAheadBack; ++u) {
       if (v0 + u * kBlock >= end) break;

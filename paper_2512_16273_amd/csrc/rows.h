@@ -10,6 +10,10 @@ constexpr int kBadPage = 16, kBadIndex = 32;           // TSLT_ROW_BAD_PAGE, TSL
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ u32x4 load16(const void* p) { return *as_global(reinterpret_cast<const u32x4*>(p)); }
+// The same at any alignment of 16-bit elements.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+__device__ __forceinline__ u32x4 load16_any(const void* p) { return *(const u32x4_any __attribute__((address_space(1)))*)p; }
+__device__ __forceinline__ void store16_any(void* p, u32x4 v) { *(u32x4_any __attribute__((address_space(1)))*)p = v; }
 
 // New tokens of a sequence, of n: its count (null: all), kept inside 0 .. n; and a sequence's status, which says where that was needed.
 __device__ __forceinline__ int counted(const int32_t* count, int64_t b, int n) { return count ? min(max(as_global(count)[b], 0), n) : n; }

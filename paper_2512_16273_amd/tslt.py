@@ -39,7 +39,8 @@ EXPORTS = ("tslt_version", "tslt_last_error", "tslt_workspace_bytes", "tslt_trun
            "tslt_verify_static", "tslt_truncation_stats", "tslt_multicandidate_stats", "tslt_calibrate_read", "tslt_verify_tree",
            "tslt_cache_append", "tslt_cache_attend", "tslt_cache_attend_workspace_bytes", "tslt_cache_weigh", "tslt_cache_evict",
            "tslt_rotate", "tslt_rotate_backward", "tslt_rotate_backward_workspace_bytes",
-           "tslt_logprob", "tslt_logprob_workspace_bytes", "tslt_logprob_backward")
+           "tslt_logprob", "tslt_logprob_workspace_bytes", "tslt_logprob_backward",
+           "tslt_adapt", "tslt_adapt_workspace_bytes")
 
 class _Cache(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("heads", ctypes.c_int32),
@@ -137,6 +138,10 @@ def load(path: Optional[str] = None):
     lib.tslt_logprob.argtypes = [vp, c.c_int, i64, i32, i64, i64, i64, f32, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.tslt_logprob_backward.restype = c.c_int
     lib.tslt_logprob_backward.argtypes = [vp, c.c_int, i64, i32, i64, i64, i64, f32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i64, i64, vp]
+    lib.tslt_adapt_workspace_bytes.restype = sz
+    lib.tslt_adapt_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    lib.tslt_adapt.restype = c.c_int
+    lib.tslt_adapt.argtypes = [rows, i32, rows, rows, i32, c.c_int, i64, i32, vp, vp, i64, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     _fast = _native_binding()
     if _fast is not None:
         _fast.bind(*[c.cast(getattr(lib, fn), vp).value for fn in (
@@ -919,4 +924,43 @@ def logprob_backward(logits: torch.Tensor, temperature: float, tokens: Optional[
                                      given(grad_entropy, "grad_entropy"), given(grad_lse, "grad_lse"),
                                      _optional(grad_top, "grad_top", torch.float32, (B, n, top)), made.data_ptr(), out_seq, out_row,
                                      _here(logits, "logits")))
+    return out
+
+
+def _token_rows(t: torch.Tensor, name: str, shape, dtype) -> _Rows:
+    """[B, n, width], dense along the width."""
+    _dev(t, dtype, name, contiguous=False)
+    if tuple(t.shape) != tuple(shape):
+        raise TsltError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise TsltError(f"{name} must be dense along its last dimension")
+    seq, token = (s if n > 1 else 0 for s, n in zip(t.stride()[:2], t.shape[:2]))
+    return _Rows(t.data_ptr(), seq, token, 0)
+
+
+def adapt_workspace_bytes(B: int, n: int, K: int, N: int, R: int) -> int:
+    return int(load().tslt_adapt_workspace_bytes(B, n, K, N, R))
+
+
+def adapt(x: torch.Tensor, base: torch.Tensor, a: torch.Tensor, b: torch.Tensor, adapter: torch.Tensor, scale: Optional[torch.Tensor] = None,
+          rank: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None, out: Optional[dict] = None,
+          workspace: Optional[torch.Tensor] = None) -> dict:
+    """tslt_adapt: to base [B, n, N], what a projection gave for x [B, n, K], scale (x a^T) b^T of each sequence's adapter [B] (-1: none), of a
+    [adapters, R, K] and b [adapters, N, R], R a multiple of 16, the first rank [adapters] of which count; scale [adapters] fp32.  x: any strides that keep rows
+    16-byte aligned; base and out: any.  Returns out [B, n, N] and status [B]; out may hold base itself."""
+    lib = load()
+    _dev(x, name="x", contiguous=False); _dev(base, name="base", contiguous=False)
+    if x.dim() != 3 or base.dim() != 3 or a.dim() != 3 or b.dim() != 3:
+        raise TsltError("adapt: x must be [B, n, K], base [B, n, N], a [adapters, R, K], b [adapters, N, R]")
+    B, n, K = x.shape
+    N, adapters, R = base.shape[2], a.shape[0], a.shape[1]
+    xr, br = _token_rows(x, "x", x.shape, x.dtype), _token_rows(base, "base", (B, n, N), x.dtype)
+    if out is None:
+        out = {"out": torch.empty(B, n, N, dtype=x.dtype, device=x.device), "status": torch.empty(B, dtype=torch.int32, device=x.device)}
+    ws = workspace if workspace is not None else _workspace(adapt_workspace_bytes(B, n, K, N, R) if B else 0, x.device)
+    _check(lib.tslt_adapt(xr, K, br, _token_rows(_given(out, "out"), "out", (B, n, N), x.dtype), N, _dtype_code(x), B, n,
+                          _optional(a, "a", x.dtype, (adapters, R, K)), _optional(b, "b", x.dtype, (adapters, N, R)), adapters, R,
+                          _counted(adapter, "adapter", B), _optional(scale, "scale", torch.float32, (adapters,)), _counted(rank, "rank", adapters),
+                          _counted(count, "count", B), _sized(out, "status", torch.int32, B, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
+                          _here(x, "x")))
     return out

@@ -113,3 +113,29 @@ def test_logprob_of_tensors():
         tslt.logprob(z, 1.0)
     with pytest.raises(tslt.TsltError, match="GPU"):
         tslt.logprob_backward(z, 1.0, None, z[..., 0])
+
+
+def test_adapt(lib):
+    def call(x=rows(), K=64, base=rows(FAKE * 2), out=rows(FAKE * 3), N=100, dt=1, B=2, n=3, a=FAKE, b=FAKE, adapters=4, R=16, adapter=FAKE, ws=FAKE * 4, ws_bytes=1 << 30):
+        return lib.tslt_adapt(x, K, base, out, N, dt, B, n, a, b, adapters, R, adapter, None, None, None, None, ws, ws_bytes, None)
+    assert call(dt=4) == -1 and call(B=-1) == -1 and call(n=0) == -1 and call(K=0) == -1 and call(N=0) == -1 and call(adapters=0) == -1
+    for R in (0, 8, 24, 272, -16):
+        assert call(R=R) == -2 and "R must be" in message(lib)
+    assert call(K=60) == -2 and call(K=6, dt=0) == -2 and call(K=4) == -2 and "16 bytes" in message(lib)
+    assert call(B=1 << 31) == -2 and call(adapters=1 << 31) == -2 and call(N=1 << 30, B=1 << 20) == -2
+    assert call(x=None) == -1 and call(base=rows(data=None)) == -1 and call(out=rows(FAKE * 3 + 1)) == -1 and call(x=rows(token=12)) == -1
+    assert call(a=None) == -1 and call(b=None) == -1 and call(adapter=None) == -1 and call(a=FAKE + 8) == -1 and call(b=FAKE + 2) == -1
+    assert call(out=rows(FAKE * 2, token=513)) == -1 and "in place" in message(lib)
+    need = lib.tslt_adapt_workspace_bytes(2, 3, 64, 100, 16)
+    assert need > 0
+    for ws, size in ((None, need), (FAKE + 16, need), (FAKE, need - 1)):
+        assert call(ws=ws, ws_bytes=size) == -3 and "workspace" in message(lib)
+    assert call(B=0) == 0
+    for bad in ((0, 3, 64, 100, 16), (2, 3, 64, 100, 24), (1 << 31, 3, 64, 100, 16)):
+        assert lib.tslt_adapt_workspace_bytes(*bad) == 0
+
+
+def test_adapt_of_tensors():
+    x = torch.zeros(1, 2, 64)
+    with pytest.raises(tslt.TsltError, match="GPU"):
+        tslt.adapt(x, x, x, x, torch.zeros(1, dtype=torch.int32))
