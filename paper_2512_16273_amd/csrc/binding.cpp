@@ -7,6 +7,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include <ATen/ATen.h>
@@ -28,12 +29,18 @@ struct Library {
   decltype(&tslt_cache_attend) cache_attend;
   decltype(&tslt_cache_weigh) cache_weigh;
   decltype(&tslt_cache_evict) cache_evict;
+  decltype(&tslt_rotate) rotate;
+  decltype(&tslt_rotate_backward) rotate_backward;
+  decltype(&tslt_logprob) logprob;
+  decltype(&tslt_logprob_backward) logprob_backward;
+  decltype(&tslt_adapt) adapt;
 } lib;
 bool bound = false;
 
 PyObject *k_idx, *k_logit, *k_prob, *k_count, *k_mass, *k_status, *k_token, *k_slot, *k_accept_len, *k_tokens, *k_ratio, *k_beta, *k_seq,
     *k_len, *k_node_token, *k_node_slot, *k_words, *k_row_offset, *k_codes,
-    *k_scale, *k_length, *k_out, *k_lse, *k_weight, *k_kept;
+    *k_scale, *k_length, *k_out, *k_lse, *k_weight, *k_kept, *k_q, *k_k, *k_q_weight, *k_k_weight, *k_logp, *k_entropy, *k_top_idx, *k_top_logp,
+    *k_logits;
 
 // A strided tensor on a GPU that no transform has wrapped, else null.
 const at::Tensor* plain(PyObject* o) {
@@ -77,9 +84,9 @@ bool unread() {
 PyObject* result(int code) { return PyLong_FromLong(code); }
 
 PyObject* py_bind(PyObject*, PyObject* args) {
-  constexpr Py_ssize_t kFunctions = 13;
+  constexpr Py_ssize_t kFunctions = 18;
   if (PyTuple_GET_SIZE(args) != kFunctions) {
-    PyErr_SetString(PyExc_TypeError, "bind takes the addresses of 13 functions");
+    PyErr_SetString(PyExc_TypeError, "bind takes the addresses of 18 functions");
     return nullptr;
   }
   unsigned long long a[kFunctions];
@@ -98,6 +105,11 @@ PyObject* py_bind(PyObject*, PyObject* args) {
   lib.cache_attend = reinterpret_cast<decltype(lib.cache_attend)>(a[10]);
   lib.cache_weigh = reinterpret_cast<decltype(lib.cache_weigh)>(a[11]);
   lib.cache_evict = reinterpret_cast<decltype(lib.cache_evict)>(a[12]);
+  lib.rotate = reinterpret_cast<decltype(lib.rotate)>(a[13]);
+  lib.rotate_backward = reinterpret_cast<decltype(lib.rotate_backward)>(a[14]);
+  lib.logprob = reinterpret_cast<decltype(lib.logprob)>(a[15]);
+  lib.logprob_backward = reinterpret_cast<decltype(lib.logprob_backward)>(a[16]);
+  lib.adapt = reinterpret_cast<decltype(lib.adapt)>(a[17]);
   bound = true;
   Py_RETURN_NONE;
 }
@@ -452,6 +464,238 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return result(code);
 }
 
+// ---- around attention and verification: `device` is the current one, on which the call's tensors live ----
+bool on(const at::Tensor* t, long long device) { return t != nullptr && t->device().index() == device; }
+bool fits(std::initializer_list<int64_t> sizes) { return std::max(sizes) <= 0x7FFFFFFF; }
+// [B][n][heads][D] like the sizes given, dense along D.
+bool read_heads(PyObject* o, at::IntArrayRef sizes, at::ScalarType type, tslt_rows& rows) {
+  const at::Tensor* t = plain(o);
+  if (t == nullptr || t->scalar_type() != type || t->sizes() != sizes || (t->size(3) > 1 && t->stride(3) != 1)) return false;
+  const auto stride = [&](int i) { return t->size(i) > 1 ? t->stride(i) : 0; };
+  rows = {t->data_ptr(), stride(0), stride(1), stride(2)};
+  return true;
+}
+// [B][n][width], dense along the width.
+bool read_tokens(const at::Tensor* t, at::IntArrayRef sizes, at::ScalarType type, int64_t (&stride)[2]) {
+  if (t == nullptr || t->scalar_type() != type || t->sizes() != sizes || (t->size(2) > 1 && t->stride(2) != 1)) return false;
+  for (int i = 0; i < 2; ++i) stride[i] = t->size(i) > 1 ? t->stride(i) : 0;
+  return true;
+}
+// A dense fp32 tensor of these sizes, or None.
+bool read_floats(PyObject* o, at::IntArrayRef sizes, const float*& p) {
+  p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = dense(o, at::kFloat);
+  if (t == nullptr || t->sizes() != sizes) return false;
+  p = ptr<float>(t);
+  return true;
+}
+bool read_workspace(PyObject* o, void*& p, size_t& bytes) {
+  const at::Tensor* t = dense(o, at::kByte);
+  if (t == nullptr) return false;
+  p = t->data_ptr();
+  bytes = size_t(t->numel());
+  return true;
+}
+// position, freq, axis, base, q_weight, k_weight, eps, adjacent: eight arguments from a on.
+bool read_rotation(PyObject* const* a, int64_t B, int64_t n, int64_t D, tslt_rotation& how) {
+  how = {};
+  how.axes = 1;
+  if (a[1] != Py_None) {
+    const at::Tensor* freq = dense(a[1], at::kFloat);
+    if (freq == nullptr || freq->dim() != 1 || freq->numel() > 256) return false;
+    how.freq = ptr<float>(freq);
+    how.rotary = int32_t(2 * freq->numel());
+  }
+  if (a[0] != Py_None) {
+    const at::Tensor* at = dense(a[0], at::kInt);
+    if (at == nullptr || at->dim() != 3 || (at->size(0) != 1 && at->size(0) != B) || at->size(1) != n || at->size(2) > TSLT_MAX_AXES) return false;
+    how.position = ptr<int32_t>(at);
+    how.axes = int32_t(at->size(2));
+    how.position_seq_stride = at->size(0) > 1 ? n * at->size(2) : 0;
+  }
+  if (!read_ints(a[2], how.rotary / 2, how.axis) || !read_ints(a[3], B, how.base)) return false;
+  if (!read_floats(a[4], {D}, how.q_weight) || !read_floats(a[5], {D}, how.k_weight)) return false;
+  how.eps = -1.0f;
+  if (a[6] != Py_None) {
+    how.eps = float(PyFloat_AsDouble(a[6]));
+    if (unread() || !(how.eps >= 0)) return false;
+  } else if (how.q_weight || how.k_weight) {
+    return false;
+  }
+  const int adjacent = PyObject_IsTrue(a[7]);
+  if (unread()) return false;
+  how.adjacent = adjacent;
+  return true;
+}
+
+// rotate(q, k, position, freq, axis, base, q_weight, k_weight, eps, adjacent, count, out, device, stream)
+PyObject* py_rotate(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 14 || !bound) Py_RETURN_NONE;
+  const long long device = PyLong_AsLongLong(a[12]);
+  void* stream = PyLong_AsVoidPtr(a[13]);
+  if (unread()) Py_RETURN_NONE;
+  const at::Tensor *q = plain(a[0]), *k = plain(a[1]);
+  if (!on(q, device) || q->dim() != 4 || (a[1] != Py_None && (k == nullptr || k->dim() != 4)) || !PyDict_CheckExact(a[11])) Py_RETURN_NONE;
+  const int dt = dtype_code(*q);
+  if (dt < 0) Py_RETURN_NONE;
+  const int64_t B = q->size(0), n = q->size(1), heads_q = q->size(2), D = q->size(3), heads = k ? k->size(2) : 0;
+  const at::ScalarType type = q->scalar_type();
+  tslt_rows qr, kr, oq, ok;
+  tslt_rotation how;
+  const int32_t* count;
+  if (!fits({n, heads_q, heads, D})) Py_RETURN_NONE;
+  if (!read_heads(a[0], q->sizes(), type, qr) || !read_heads(PyDict_GetItem(a[11], k_q), q->sizes(), type, oq)) Py_RETURN_NONE;
+  if (k && (!read_heads(a[1], {B, n, heads, D}, type, kr) || !read_heads(PyDict_GetItem(a[11], k_k), k->sizes(), type, ok))) Py_RETURN_NONE;
+  if (!read_rotation(a + 2, B, n, D, how) || !read_ints(a[10], B, count)) Py_RETURN_NONE;
+  bool there = true;
+  int32_t* status = sized<int32_t>(a[11], k_status, at::kInt, B, true, there);
+  if (!there) Py_RETURN_NONE;
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.rotate(&qr, k ? &kr : nullptr, tslt_dtype(dt), B, int32_t(n), int32_t(heads_q), int32_t(heads), int32_t(D), &how, count, &oq, k ? &ok : nullptr, status, stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
+// rotate_backward(grad_q, grad_k, q, k, position, freq, axis, base, q_weight, k_weight, eps, adjacent, count, out, workspace, device, stream)
+PyObject* py_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 17 || !bound) Py_RETURN_NONE;
+  const long long device = PyLong_AsLongLong(a[15]);
+  void* stream = PyLong_AsVoidPtr(a[16]);
+  if (unread()) Py_RETURN_NONE;
+  const at::Tensor *g = plain(a[0]), *gk = plain(a[1]);
+  if (!on(g, device) || g->dim() != 4 || (a[1] != Py_None && (gk == nullptr || gk->dim() != 4)) || !PyDict_CheckExact(a[13])) Py_RETURN_NONE;
+  const int dt = dtype_code(*g);
+  if (dt < 0) Py_RETURN_NONE;
+  const int64_t B = g->size(0), n = g->size(1), heads_q = g->size(2), D = g->size(3), heads = gk ? gk->size(2) : 0;
+  const at::ScalarType type = g->scalar_type();
+  const bool norm = a[10] != Py_None, keys = gk != nullptr;
+  tslt_rows gqr, gkr, qr, kr, oq, ok;
+  tslt_rotation how;
+  const int32_t* count;
+  void* ws;
+  size_t ws_bytes;
+  if (!fits({n, heads_q, heads, D})) Py_RETURN_NONE;
+  if (!read_heads(a[0], g->sizes(), type, gqr) || !read_heads(PyDict_GetItem(a[13], k_q), g->sizes(), type, oq) || (norm && !read_heads(a[2], g->sizes(), type, qr))) Py_RETURN_NONE;
+  if (keys && (!read_heads(a[1], {B, n, heads, D}, type, gkr) || !read_heads(PyDict_GetItem(a[13], k_k), gk->sizes(), type, ok) || (norm && !read_heads(a[3], gk->sizes(), type, kr)))) Py_RETURN_NONE;
+  if (!read_rotation(a + 4, B, n, D, how) || !read_ints(a[12], B, count) || !read_workspace(a[14], ws, ws_bytes)) Py_RETURN_NONE;
+  bool there = true;
+  float* dq = sized<float>(a[13], k_q_weight, at::kFloat, D, true, there);
+  float* dk = sized<float>(a[13], k_k_weight, at::kFloat, D, true, there);
+  int32_t* status = sized<int32_t>(a[13], k_status, at::kInt, B, true, there);
+  if (!there) Py_RETURN_NONE;
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.rotate_backward(&gqr, keys ? &gkr : nullptr, norm ? &qr : nullptr, norm && keys ? &kr : nullptr, tslt_dtype(dt), B, int32_t(n), int32_t(heads_q), int32_t(heads),
+                             int32_t(D), &how, count, &oq, keys ? &ok : nullptr, dq, dk, status, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
+// logprob(logits, temperature, tokens, top, index, count, out, workspace, device, stream)
+PyObject* py_logprob(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 10 || !bound) Py_RETURN_NONE;
+  const double T = PyFloat_AsDouble(a[1]);
+  const long long top = PyLong_AsLongLong(a[3]), device = PyLong_AsLongLong(a[8]);
+  void* stream = PyLong_AsVoidPtr(a[9]);
+  if (unread() || top < 0 || top > TSLT_MAX_TOP) Py_RETURN_NONE;
+  const at::Tensor *z = plain(a[0]), *index = plain(a[4]);
+  if (!on(z, device) || z->dim() != 3 || (a[4] != Py_None && (index == nullptr || index->dim() != 2)) || !PyDict_CheckExact(a[6])) Py_RETURN_NONE;
+  const int dt = dtype_code(*z);
+  int64_t stride[2];
+  if (dt < 0 || !read_tokens(z, z->sizes(), z->scalar_type(), stride)) Py_RETURN_NONE;
+  const int64_t B = z->size(0), n = z->size(1), V = z->size(2), m = index ? index->size(1) : n;
+  if (!fits({n, m})) Py_RETURN_NONE;
+  const int32_t *tokens, *rows, *count;
+  void* ws;
+  size_t ws_bytes;
+  if (!read_ints(a[2], B * m, tokens) || !read_ints(a[4], B * m, rows) || !read_ints(a[5], B, count) || !read_workspace(a[7], ws, ws_bytes)) Py_RETURN_NONE;
+  bool there = true;
+  float* logp = sized<float>(a[6], k_logp, at::kFloat, B * m, true, there);
+  float* entropy = sized<float>(a[6], k_entropy, at::kFloat, B * m, true, there);
+  float* lse = sized<float>(a[6], k_lse, at::kFloat, B * m, true, there);
+  int32_t* top_idx = top ? sized<int32_t>(a[6], k_top_idx, at::kInt, B * m * top, false, there) : nullptr;
+  float* top_logp = top ? sized<float>(a[6], k_top_logp, at::kFloat, B * m * top, false, there) : nullptr;
+  int32_t* status = sized<int32_t>(a[6], k_status, at::kInt, B * m, true, there);
+  if (!there) Py_RETURN_NONE;
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.logprob(z->data_ptr(), tslt_dtype(dt), B, int32_t(n), V, stride[0], stride[1], float(T), rows, int32_t(m), count, tokens, int32_t(top), logp, entropy, lse, top_idx,
+                     top_logp, status, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
+// logprob_backward(logits, temperature, tokens, lse, entropy, grad_logp, grad_entropy, grad_lse, top_idx, grad_top, count, out, device, stream)
+PyObject* py_logprob_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 14 || !bound) Py_RETURN_NONE;
+  const double T = PyFloat_AsDouble(a[1]);
+  const long long device = PyLong_AsLongLong(a[12]);
+  void* stream = PyLong_AsVoidPtr(a[13]);
+  if (unread()) Py_RETURN_NONE;
+  const at::Tensor *z = plain(a[0]), *grad_top = plain(a[9]);
+  if (!on(z, device) || z->dim() != 3 || (a[9] != Py_None && (grad_top == nullptr || grad_top->dim() != 3)) || !PyDict_CheckExact(a[11])) Py_RETURN_NONE;
+  const int dt = dtype_code(*z);
+  int64_t stride[2], out_stride[2];
+  PyObject* made = PyDict_GetItem(a[11], k_logits);
+  const at::Tensor* out = made ? plain(made) : nullptr;
+  if (dt < 0 || !read_tokens(z, z->sizes(), z->scalar_type(), stride) || !read_tokens(out, z->sizes(), z->scalar_type(), out_stride)) Py_RETURN_NONE;
+  const int64_t B = z->size(0), n = z->size(1), V = z->size(2), top = grad_top ? grad_top->size(2) : 0;
+  if (!fits({n}) || (grad_top && (top < 1 || top > TSLT_MAX_TOP))) Py_RETURN_NONE;
+  const int32_t *tokens, *count, *top_idx = nullptr;
+  const float *lse, *entropy, *g_logp, *g_entropy, *g_lse, *g_top;
+  if (!read_ints(a[2], B * n, tokens) || !read_floats(a[3], {B, n}, lse) || !read_floats(a[4], {B, n}, entropy) || !read_floats(a[5], {B, n}, g_logp) ||
+      !read_floats(a[6], {B, n}, g_entropy) || !read_floats(a[7], {B, n}, g_lse) || !read_floats(a[9], {B, n, top}, g_top) || (top && !read_ints(a[8], B * n * top, top_idx)) ||
+      !read_ints(a[10], B, count) || lse == nullptr)
+    Py_RETURN_NONE;
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.logprob_backward(z->data_ptr(), tslt_dtype(dt), B, int32_t(n), V, stride[0], stride[1], float(T), count, tokens, lse, entropy, top_idx, int32_t(top), g_logp, g_entropy,
+                              g_lse, g_top, out->data_ptr(), out_stride[0], out_stride[1], stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
+// adapt(x, base, a, b, adapter, scale, rank, count, out, workspace, device, stream)
+PyObject* py_adapt(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 12 || !bound) Py_RETURN_NONE;
+  const long long device = PyLong_AsLongLong(a[10]);
+  void* stream = PyLong_AsVoidPtr(a[11]);
+  if (unread()) Py_RETURN_NONE;
+  const at::Tensor *x = plain(a[0]), *base = plain(a[1]), *down = plain(a[2]), *up = plain(a[3]);
+  if (!on(x, device) || x->dim() != 3 || !base || base->dim() != 3 || !down || down->dim() != 3 || !up || !PyDict_CheckExact(a[8])) Py_RETURN_NONE;
+  const int dt = dtype_code(*x);
+  if (dt < 0) Py_RETURN_NONE;
+  const at::ScalarType type = x->scalar_type();
+  const int64_t B = x->size(0), n = x->size(1), K = x->size(2), N = base->size(2), adapters = down->size(0), R = down->size(1);
+  if (!fits({n, K, N, R})) Py_RETURN_NONE;
+  const auto dense_as = [&](const at::Tensor* t, at::IntArrayRef sizes) { return t->scalar_type() == type && t->is_contiguous() && t->sizes() == sizes; };
+  int64_t xs[2], bs[2], os[2];
+  PyObject* made = PyDict_GetItem(a[8], k_out);
+  const at::Tensor* out = made ? plain(made) : nullptr;
+  if (!read_tokens(x, x->sizes(), type, xs) || !read_tokens(base, {B, n, N}, type, bs) || !read_tokens(out, {B, n, N}, type, os) ||
+      !dense_as(down, {adapters, R, K}) || !dense_as(up, {adapters, N, R}))
+    Py_RETURN_NONE;
+  const int32_t *adapter, *rank, *count;
+  const float* scale;
+  void* ws;
+  size_t ws_bytes;
+  if (!read_ints(a[4], B, adapter) || !read_floats(a[5], {adapters}, scale) || !read_ints(a[6], adapters, rank) || !read_ints(a[7], B, count) ||
+      !read_workspace(a[9], ws, ws_bytes))
+    Py_RETURN_NONE;
+  bool there = true;
+  int32_t* status = sized<int32_t>(a[8], k_status, at::kInt, B, true, there);
+  if (!there) Py_RETURN_NONE;
+  const tslt_rows xr{x->data_ptr(), xs[0], xs[1], 0}, br{base->data_ptr(), bs[0], bs[1], 0}, orows{out->data_ptr(), os[0], os[1], 0};
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = lib.adapt(&xr, int32_t(K), &br, &orows, int32_t(N), tslt_dtype(dt), B, int32_t(n), down->data_ptr(), up->data_ptr(), adapters, int32_t(R), adapter, scale, rank, count,
+                   status, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return result(code);
+}
+
 // What a call into torch throws (no memory left, say) becomes a Python exception, as from torch itself.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -464,7 +708,8 @@ template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyMethodDef f
 PyMethodDef methods[] = {
     {"bind", py_bind, METH_VARARGS, nullptr}, fast<py_truncate>("truncate"), fast<py_verify>("verify"), fast<py_verify_tree>("verify_tree"),
     fast<py_pack>("pack"), fast<py_unpack>("unpack"), fast<py_cache_append>("cache_append"), fast<py_cache_attend>("cache_attend"),
-    fast<py_cache_weigh>("cache_weigh"), fast<py_cache_evict>("cache_evict"), {nullptr, nullptr, 0, nullptr}};
+    fast<py_cache_weigh>("cache_weigh"), fast<py_cache_evict>("cache_evict"), fast<py_rotate>("rotate"),
+    fast<py_rotate_backward>("rotate_backward"), fast<py_logprob>("logprob"), fast<py_logprob_backward>("logprob_backward"), fast<py_adapt>("adapt"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -474,7 +719,9 @@ PyMODINIT_FUNC PyInit__binding() {
       {&k_idx, "idx"}, {&k_logit, "logit"}, {&k_prob, "prob"}, {&k_count, "count"}, {&k_mass, "mass"}, {&k_status, "status"},
       {&k_token, "token"}, {&k_slot, "slot"}, {&k_accept_len, "accept_len"}, {&k_tokens, "tokens"}, {&k_ratio, "ratio"}, {&k_beta, "beta"},
       {&k_seq, "seq"}, {&k_len, "len"}, {&k_node_token, "node_token"}, {&k_node_slot, "node_slot"}, {&k_words, "words"}, {&k_row_offset, "row_offset"},
-      {&k_codes, "codes"}, {&k_scale, "scale"}, {&k_length, "length"}, {&k_out, "out"}, {&k_lse, "lse"}, {&k_weight, "weight"}, {&k_kept, "kept"}};
+      {&k_codes, "codes"}, {&k_scale, "scale"}, {&k_length, "length"}, {&k_out, "out"}, {&k_lse, "lse"}, {&k_weight, "weight"}, {&k_kept, "kept"},
+      {&k_q, "q"}, {&k_k, "k"}, {&k_q_weight, "q_weight"}, {&k_k_weight, "k_weight"}, {&k_logp, "logp"}, {&k_entropy, "entropy"}, {&k_top_idx, "top_idx"},
+      {&k_top_logp, "top_logp"}, {&k_logits, "logits"}};
   for (const auto& k : keys)
     if ((*k.first = PyUnicode_InternFromString(k.second)) == nullptr) return nullptr;
   PyObject* m = PyModule_Create(&module);

@@ -147,7 +147,8 @@ def load(path: Optional[str] = None):
         _fast.bind(*[c.cast(getattr(lib, fn), vp).value for fn in (
             "tslt_workspace_bytes", "tslt_truncate_sample", "tslt_verify", "tslt_verify_accept", "tslt_verify_resample", "tslt_verify_tree",
             "tslt_pack_bound_words", "tslt_pack_cleared", "tslt_unpack",
-            "tslt_cache_append", "tslt_cache_attend", "tslt_cache_weigh", "tslt_cache_evict")])
+            "tslt_cache_append", "tslt_cache_attend", "tslt_cache_weigh", "tslt_cache_evict",
+            "tslt_rotate", "tslt_rotate_backward", "tslt_logprob", "tslt_logprob_backward", "tslt_adapt")])
     _lib = lib
     return lib
 
@@ -735,6 +736,12 @@ def _here(t: torch.Tensor, name: str) -> int:
     return torch._C._cuda_getCurrentRawStream(device)
 
 
+def _current():
+    """The current device and its current stream."""
+    device = torch.cuda.current_device()
+    return device, torch._C._cuda_getCurrentRawStream(device)
+
+
 def _optional(t: Optional[torch.Tensor], name: str, dtype, shape) -> Optional[int]:
     if t is None:
         return None
@@ -742,6 +749,12 @@ def _optional(t: Optional[torch.Tensor], name: str, dtype, shape) -> Optional[in
     if tuple(t.shape) != tuple(shape):
         raise TsltError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     return t.data_ptr()
+
+
+def _fits(call: str, *sizes: int) -> None:
+    """Sizes that the library takes in 32 bits (ctypes would cut them)."""
+    if max(sizes) >= 1 << 31:
+        raise TsltError(f"{call}: a size of {max(sizes)} does not fit 31 bits")
 
 
 def _given(out: dict, name: str) -> torch.Tensor:
@@ -778,6 +791,12 @@ def rotate(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[torch.
     the weights q_weight, k_weight [D], and rotated by the angles (base [B] + position [B or 1, n, axes]) * freq [rotary / 2].  axis [rotary / 2]:
     which axis each pair goes by; position None: token i is at i.  Returns q, k and status [B]; out may hold q and k themselves."""
     lib = load()
+    if _fast is not None and out is not None and q.is_cuda:
+        code = _fast.rotate(q, k, position, freq, axis, base, q_weight, k_weight, eps, adjacent, count, out, *_current())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     _dev(q, name="q", contiguous=False)
     if q.dim() != 4:
         raise TsltError("q must be [B, n, heads_q, D]")
@@ -787,6 +806,7 @@ def rotate(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[torch.
         if k.dim() != 4:
             raise TsltError("k must be [B, n, heads, D]")
         heads = k.shape[2]
+    _fits("rotate", n, heads_q, heads, D)
     qr, kr = _rows_of(q, "q", q.shape, q.dtype), None if k is None else _rows_of(k, "k", (B, n, heads, D), q.dtype)
     how = _rotation(B, n, D, position, freq, axis, base, q_weight, k_weight, eps, adjacent)
     if out is None:
@@ -813,6 +833,12 @@ def rotate_backward(grad_q: torch.Tensor, grad_k: Optional[torch.Tensor], q: Opt
     fp32); q and k as rotate was given them (None without a norm).  Returns q, k, q_weight, k_weight and status [B]; out may hold grad_q and grad_k
     themselves."""
     lib = load()
+    if _fast is not None and out is not None and workspace is not None and grad_q.is_cuda:
+        code = _fast.rotate_backward(grad_q, grad_k, q, k, position, freq, axis, base, q_weight, k_weight, eps, adjacent, count, out, workspace, *_current())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     _dev(grad_q, name="grad_q", contiguous=False)
     if grad_q.dim() != 4:
         raise TsltError("grad_q must be [B, n, heads_q, D]")
@@ -822,6 +848,7 @@ def rotate_backward(grad_q: torch.Tensor, grad_k: Optional[torch.Tensor], q: Opt
         if grad_k.dim() != 4:
             raise TsltError("grad_k must be [B, n, heads, D]")
         heads = grad_k.shape[2]
+    _fits("rotate_backward", n, heads_q, heads, D)
     gq = _rows_of(grad_q, "grad_q", grad_q.shape, dtype)
     gk = None if grad_k is None else _rows_of(grad_k, "grad_k", (B, n, heads, D), dtype)
     qr = None if q is None or eps is None else _rows_of(q, "q", grad_q.shape, dtype)
@@ -865,12 +892,21 @@ def logprob(logits: torch.Tensor, temperature: float, tokens: Optional[torch.Ten
     of tokens [B, m] (-1: none), the entropy and the normaliser, and the `top` likeliest tokens with theirs.  Returns logp, entropy, lse, status [B, m] and, with
     top, top_idx and top_logp [B, m, top]; of a given out what it holds."""
     lib = load()
+    if _fast is not None and out is not None and workspace is not None and logits.is_cuda:
+        code = _fast.logprob(logits, temperature, tokens, top, index, count, out, workspace, *_current())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     seq, row = _logits(logits, "logits")
     B, n, V = logits.shape
     top = int(top)
     if index is not None and index.dim() != 2:
         raise TsltError("index must be [B, m]")
     m = n if index is None else index.shape[1]
+    if not -(1 << 31) <= top < 1 << 31:
+        raise TsltError(f"top must be 0 to {MAX_TOP} (got {top})")
+    _fits("logprob", n, m)
     dev = logits.device
     if out is None:
         out = {name: torch.empty(B, m, dtype=torch.float32, device=dev) for name in ("logp", "entropy", "lse")}
@@ -898,6 +934,12 @@ def logprob_backward(logits: torch.Tensor, temperature: float, tokens: Optional[
     """tslt_logprob_backward: the gradient `logits` [B, n, V] of what logprob was given, without an index, from those of its results (None: 0); tokens, lse,
     entropy, top_idx as it was given them and gave them.  out may hold the logits themselves."""
     lib = load()
+    if _fast is not None and out is not None and logits.is_cuda:
+        code = _fast.logprob_backward(logits, temperature, tokens, lse, entropy, grad_logp, grad_entropy, grad_lse, top_idx, grad_top, count, out, *_current())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     seq, row = _logits(logits, "logits")
     B, n, V = logits.shape
     top = 0
@@ -907,6 +949,7 @@ def logprob_backward(logits: torch.Tensor, temperature: float, tokens: Optional[
         top = grad_top.shape[2]
         if not 1 <= top <= MAX_TOP:
             raise TsltError(f"grad_top must be [B, n, top] with top from 1 to {MAX_TOP}")
+    _fits("logprob_backward", n)
     if out is None:
         out = {"logits": torch.empty(B, n, V, dtype=logits.dtype, device=logits.device)}
     made = _given(out, "logits")
@@ -949,11 +992,18 @@ def adapt(x: torch.Tensor, base: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
     [adapters, R, K] and b [adapters, N, R], R a multiple of 16, the first rank [adapters] of which count; scale [adapters] fp32.  x: any strides that keep rows
     16-byte aligned; base and out: any.  Returns out [B, n, N] and status [B]; out may hold base itself."""
     lib = load()
+    if _fast is not None and out is not None and workspace is not None and x.is_cuda:
+        code = _fast.adapt(x, base, a, b, adapter, scale, rank, count, out, workspace, *_current())
+        if code is not None:
+            if code:
+                _check(code)
+            return out
     _dev(x, name="x", contiguous=False); _dev(base, name="base", contiguous=False)
     if x.dim() != 3 or base.dim() != 3 or a.dim() != 3 or b.dim() != 3:
         raise TsltError("adapt: x must be [B, n, K], base [B, n, N], a [adapters, R, K], b [adapters, N, R]")
     B, n, K = x.shape
     N, adapters, R = base.shape[2], a.shape[0], a.shape[1]
+    _fits("adapt", n, K, N, R)
     xr, br = _token_rows(x, "x", x.shape, x.dtype), _token_rows(base, "base", (B, n, N), x.dtype)
     if out is None:
         out = {"out": torch.empty(B, n, N, dtype=x.dtype, device=x.device), "status": torch.empty(B, dtype=torch.int32, device=x.device)}
