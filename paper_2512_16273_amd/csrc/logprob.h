@@ -2,12 +2,13 @@
 // the logits.
 //
 // With k = log2(e) / T and a reference c of the row's logits (the largest that a wave has met), a term is e_j = 2^(k z_j - fl(k c)), one multiply-add and
-// one exponential; S = sum e_j and E = sum e_j log2 e_j.  Then, with rho = k c - fl(k c) (added up in fp64 where terms are), lse = c / T + ln S - rho ln 2 and
-// H = ln S - ln 2 E / S.  A wave whose logits pass its reference takes the larger one: S 2^d and 2^d (E + d S), d < 0 the difference.
+// one exponential; S = sum e_j and E = sum e_j log2 e_j.  Then, with rho = k c - fl(k c) (taken back in fp64 where terms are added up), lse = c / T + ln S - rho ln 2
+// and H = ln S - ln 2 E / S.  A wave whose logits pass its reference takes the larger one: S 2^d and 2^d (E + d S), d < 0 the difference.
 //
-// The `top` largest: each wave keeps a list in LDS of the logits above what it knows `top` of its logits to reach, and cuts the list down to `top`
-// when it is full.  What it knows at first are the largest logits of its lanes in the first loads: `top` of those 64 numbers are reached by as many
-// logits.  So a logit costs nothing but its share of a comparison a load, which the reference needs as well.
+// The `top` largest: each wave keeps a list in LDS of the logits above a threshold that `top` of the row's logits are known to reach.  At first that are the largest
+// logits of its lanes in the first loads: `top` of those 64 numbers are reached by as many logits.  Then the waves put their lists together, cut what they have to `top`, and
+// take the least of them as threshold: after the first loads, and again whenever twice as much of the row has been met, so that between two
+// of these about `top` logits are listed.  A logit costs no more than its share of a comparison a load, which the reference needs as well.
 //
 // Few rows: several workgroups to a row, whose sums and lists the last of them to end joins (handover.h).
 #pragma once
@@ -17,7 +18,8 @@
 namespace tslt {
 
 constexpr int kMaxTop = 32;
-constexpr int kListRoom = 256;           // records of a wave's list
+constexpr int kListRoom = 128;           // records of a wave's list
+constexpr int kLogprobWaves = 4, kLogprobThreads = 64 * kLogprobWaves;
 
 struct LogprobParams {
   const void* logits;
@@ -28,37 +30,66 @@ struct LogprobParams {
   const int32_t *index, *count, *tokens;
   float *logp, *entropy, *lse, *top_logp;
   int32_t *top_idx, *status;
-  int slices;                            // workgroups of a row
+  int slices;                            // workgroups of a row, 64 at most
   uint64_t* words;                       // [entries][slices]
-  uint64_t* part;                        // [entries][slices][3 + top]: reference, S, E, the list
+  uint64_t* part;                        // [entries][slices][4 + top]: reference, S, E, the least record of a full list (else 0), the list
   Tag tag;
 };
 
-// Sums of a wave or of more: reference (raw logit), S and E as above.
-struct RowSums { float c; double S, E; };
-// Both with one reference.  (A side that has nothing has S = 0.)
-__device__ __forceinline__ RowSums join(const RowSums& a, const RowSums& b, double k2) {
-  const float c = fmaxf(a.c, b.c);
-  RowSums r{c, 0.0, 0.0};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const RowSums& x = i ? b : a;
-    if (x.S == 0.0) continue;
-    const double d = x.c == c ? 0.0 : k2 * (double(x.c) - double(c)), f = exp2(d);
-    r.S += f * x.S;
-    r.E += f * (x.E + d * x.S);
-  }
-  return r;
-}
-
-// A wave's list of candidate records (make_cand): value descending, index ascending, in no order.
+// A wave's list of candidate records (make_cand): value descending, index ascending; they lie in no order.
 struct List {
   uint64_t* at;                          // kListRoom records of LDS
-  int n;                                 // the same in all lanes, as is the threshold
+  int n;                                 // the same in all lanes, as are the thresholds
   float above;                           // nothing that is not greater than this can be among the `top`
+  uint64_t least;                        // nor a record that is less than this
 };
 
-// The wave's list cut down to its `top` largest records, in no order; the threshold is the least of them.
+// The largest number that `top` of the records reach, a bit at a time (there are more than `top` of them; 0 stands for none).
+template <int N> __device__ __forceinline__ uint64_t least_of_top(const uint64_t (&r)[N], int top) {
+  // values' leading bits that all have in common
+  uint32_t most = 0, low = 0xFFFFFFFFu;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    most = max(most, uint32_t(r[i] >> 32));
+    low = min(low, r[i] != 0 ? uint32_t(r[i] >> 32) : 0xFFFFFFFFu);
+  }
+  most = wave_max_u32(most);
+  low = ~wave_max_u32(~low);
+  const int same = most == low ? 32 : __builtin_clz(most ^ low);
+  uint64_t least = same == 0 ? 0 : uint64_t(most >> (32 - same)) << (64 - same);
+  for (int bit = 63 - same; bit >= 0; --bit) {
+    const uint64_t trial = least | uint64_t(1) << bit;
+    int reach = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) reach += __popcll(ballot(r[i] >= trial));
+    if (reach >= top) least = trial;
+    if (reach == top) break;
+  }
+  return least;
+}
+// Those records that reach `least` to `to`, in no order; how many.
+template <int N> __device__ __forceinline__ int keep_from(const uint64_t (&r)[N], uint64_t least, uint64_t* to) {
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bool mine = r[i] != 0 && r[i] >= least;
+    const uint64_t keep = ballot(mine);
+    if (mine) to[n + lanes_below(keep)] = r[i];
+    n += __popcll(keep);
+  }
+  return n;
+}
+// The least of `top` records as a number that all of them reach and nothing between it and the least one is.
+template <int N> __device__ __forceinline__ uint64_t least_record(const uint64_t (&r)[N], uint64_t least) {
+  uint32_t hi = 0xFFFFFFFFu;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (r[i] != 0 && r[i] >= least) hi = min(hi, uint32_t(r[i] >> 32));
+  hi = ~wave_max_u32(~hi);
+  return max(least, uint64_t(hi) << 32);
+}
+
+// The wave's list cut down to its `top` largest records.
 __device__ __forceinline__ void cut(List& l, int top) {
   wave_sync();
   if (l.n <= top) return;
@@ -66,32 +97,12 @@ __device__ __forceinline__ void cut(List& l, int top) {
   uint64_t r[kListRoom / 64];
 #pragma unroll
   for (int i = 0; i < kListRoom / 64; ++i) r[i] = lane + 64 * i < l.n ? l.at[lane + 64 * i] : 0;
-  // the largest number that `top` records reach, a bit at a time: first their values, and where several have the same their indices
-  uint64_t least = 0;
-  for (int bit = 63; bit >= 0; --bit) {
-    const uint64_t trial = least | uint64_t(1) << bit;
-    int reach = 0;
-#pragma unroll
-    for (int i = 0; i < kListRoom / 64; ++i) reach += __popcll(ballot(r[i] >= trial));
-    if (reach >= top) least = trial;
-    if (reach == top) break;
-  }
+  const uint64_t least = least_of_top(r, top);
   wave_sync();
-  int n = 0;
-#pragma unroll
-  for (int i = 0; i < kListRoom / 64; ++i) {
-    const uint64_t keep = ballot(r[i] >= least);
-    if (r[i] >= least) l.at[n + lanes_below(keep)] = r[i];
-    n += __popcll(keep);
-  }
+  l.n = keep_from(r, least, l.at);
+  l.least = least_record(r, least);
+  l.above = fmaxf(l.above, cand_value(l.least));
   wave_sync();
-  l.n = n;
-  // the least value among them
-  uint32_t low = 0xFFFFFFFFu;
-#pragma unroll
-  for (int i = 0; i < kListRoom / 64; ++i)
-    if (r[i] >= least) low = min(low, uint32_t(r[i] >> 32));
-  l.above = key_to_f32(~wave_max_u32(~low));
 }
 // Records of those lanes that have one.
 __device__ __forceinline__ void offer(List& l, bool mine, uint64_t record, int top) {
@@ -111,6 +122,20 @@ __device__ __forceinline__ float reached_by(float largest, int top) {
   }
   // the number before it (before both zeros, which are equal)
   return least > kKeyNegInf ? key_to_f32(least == 0x80000000u ? least - 2 : least - 1) : -INFINITY;
+}
+
+// Sums of a wave or of more: reference (raw logit), rho, S and E as above.
+struct RowSums { float c; double rho, S, E; };
+// Those of a wave's lanes, with one reference and no rho.  (What has nothing has S = 0.)
+__device__ __forceinline__ RowSums join(const RowSums& x, double k2) {
+  RowSums r{wave_max_f32(x.c), 0.0, 0.0, 0.0};
+  const double d = (x.c == r.c ? 0.0 : k2 * (double(x.c) - double(r.c))) - x.rho;
+  const double f = fast_exp2(float(d));
+  double sum[2] = {x.S == 0.0 ? 0.0 : f * x.S, x.S == 0.0 || f == 0.0 ? 0.0 : f * (x.E + d * x.S)};
+  wave_sums_f64<2>(sum);
+  r.S = sum[0];
+  r.E = sum[1];
+  return r;
 }
 
 // What a wave has of a row.
@@ -152,12 +177,42 @@ struct RowWave {
 };
 
 struct LogprobShared {
-  uint64_t list[4][kListRoom];
-  double S[4], E[4];
-  float c[4];
-  int n[4];
+  uint64_t list[kLogprobWaves][kListRoom];
+  double rho[kLogprobWaves], S[kLogprobWaves], E[kLogprobWaves];
+  float c[kLogprobWaves];
+  int n[kLogprobWaves];
+  uint64_t least;
   int told, mine;
 };
+
+// The waves' lists put together and cut down to `top` records, which the first wave's list then has.  All threads.
+__device__ __forceinline__ void put_together(List& l, int top, LogprobShared& sh) {
+  const int wave = wave_id(), lane = lane_id();
+  if (l.n > 64) cut(l, top);
+  if (lane == 0) sh.n[wave] = l.n;
+  __syncthreads();
+  if (wave == 0) {
+    uint64_t r[kLogprobWaves];
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kLogprobWaves; ++w) {
+      const int n = sh.n[w];
+      r[w] = lane < n ? sh.list[w][lane] : 0;
+      total += n;
+    }
+    uint64_t least = 0;
+    if (total > top) least = least_of_top(r, top);
+    wave_sync();
+    l.n = keep_from(r, least, l.at);
+    if (total >= top) least = least_record(r, least);
+    if (lane == 0) sh.least = least;
+  } else {
+    l.n = 0;
+  }
+  __syncthreads();
+  l.least = sh.least;
+  if (l.least != 0) l.above = fmaxf(l.above, cand_value(l.least));
+}
 
 // Values of a vector's elements that lie past the row's end: -inf, which adds nothing and is never chosen.
 template <typename T> __device__ __forceinline__ uint4 row_vector(const uint4* body, int64_t v, int64_t end) {
@@ -189,14 +244,14 @@ template <typename T> __device__ __forceinline__ void take(RowWave& w, const uin
 
 constexpr int kAhead = 4;                // vectors of a lane that are asked for together
 
-template <typename T> __device__ void row_share(const void* row, const LogprobParams& p, int slice, LogprobShared& sh) {
-  constexpr int E = ElemTraits<T>::kPerVec;
+// A workgroup's share of a row: its waves' sums in LDS, and the likeliest in the first wave's list.
+template <typename T> __device__ void row_share(const void* row, const LogprobParams& p, int slice, LogprobShared& sh, List& list) {
+  constexpr int E = ElemTraits<T>::kPerVec, kRound = kLogprobThreads * kAhead;
   const int wave = wave_id(), lane = lane_id(), top = p.top;
   const RowSplit rs = split_row<T>(row, p.V);
   const int64_t each = (rs.nvec + p.slices - 1) / p.slices, begin = min(each * slice, rs.nvec), end = min(begin + each, rs.nvec);
   RowWave w;
-  w.list = List{sh.list[wave], 0, -INFINITY};
-  bool first = true;
+  w.list = List{sh.list[wave], 0, -INFINITY, 0};
   // numbers before the aligned ones are the row's first, those behind them its last: equal numbers are met in their order
   const auto edge = [&](int from, int to) {
     const bool mine = from + lane < to;
@@ -208,87 +263,89 @@ template <typename T> __device__ void row_share(const void* row, const LogprobPa
     w.terms(one, p.k2);
   };
   if (slice == 0 && wave == 0 && rs.head > 0) edge(0, rs.head);
-  for (int64_t v0 = begin + wave * 64; v0 < end; v0 += 4 * 64 * kAhead) {
-    uint4 x[kAhead];
+  uint4 x[kAhead];
+  int64_t v = begin + wave * 64 + lane;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) x[u] = row_vector<T>(rs.body, v0 + u * 256 + lane, end);
-    if (first) {
-      float most = -INFINITY;
+  for (int u = 0; u < kAhead; ++u) x[u] = row_vector<T>(rs.body, v + u * kLogprobThreads, end);
+  {
+    float most = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        float z[E];
-        unpack<T>(x[u], z);
-        most = fmaxf(most, largest_of(z));
-      }
-      const float all = wave_max_f32(fmaxf(most, w.c));
-      if (all > w.c) w.refer(all, p.k2);
-      w.list.above = top > 0 ? fmaxf(w.list.above, reached_by(most, top)) : w.c;
-      first = false;
+    for (int u = 0; u < kAhead; ++u) {
+      float z[E];
+      unpack<T>(x[u], z);
+      most = fmaxf(most, largest_of(z));
     }
+    const float all = wave_max_f32(fmaxf(most, w.c));
+    if (all > w.c) w.refer(all, p.k2);
+    w.list.above = top > 0 ? fmaxf(w.list.above, reached_by(most, top)) : w.c;
+  }
+  int round = 0, together = 1;
+  for (int64_t v0 = begin; v0 < end; v0 += kRound, v += kRound) {
+    uint4 next[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) take<T>(w, x[u], rs.head + (v0 + u * 256 + lane) * E, p.k2, top);
+    for (int u = 0; u < kAhead; ++u) next[u] = row_vector<T>(rs.body, v + kRound + u * kLogprobThreads, end);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) take<T>(w, x[u], rs.head + (v + u * kLogprobThreads) * E, p.k2, top);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) x[u] = next[u];
+    if (top > 0 && ++round == together && v0 + 2 * kRound < end) {
+      put_together(w.list, top, sh);
+      // (what does not pass the threshold is not held against the reference)
+      if (w.list.above > w.c) w.refer(w.list.above, p.k2);
+      together = 2 * round;
+    }
   }
   if (slice == p.slices - 1 && wave == 0 && rs.tail > 0) edge(rs.head, rs.head + rs.tail);
-  const double S = wave_sum_f64(double(w.S)), Es = wave_sum_f64(double(w.E));
-  if (top > 0) cut(w.list, top);
+  double sum[2] = {double(w.S), double(w.E)};
+  wave_sums_f64<2>(sum);
   if (lane == 0) {
-    // (the terms' common factor 2^rho goes here, so that sums of different references can be joined)
-    const double rho = w.far || w.c == -INFINITY ? 0.0 : double(p.k2) * double(w.c) - double(w.kc), f = exp2(-rho);
-    sh.S[wave] = f * S;
-    sh.E[wave] = f * (Es - rho * S);
+    sh.rho[wave] = w.far || w.c == -INFINITY ? 0.0 : double(p.k2) * double(w.c) - double(w.kc);
+    sh.S[wave] = sum[0];
+    sh.E[wave] = sum[1];
     sh.c[wave] = w.c;
-    sh.n[wave] = w.list.n;
   }
-  __syncthreads();
+  list = w.list;
+  if (top > 0) put_together(list, top, sh);
+  else __syncthreads();
 }
 
+// The first wave: the sums of all.
 __device__ __forceinline__ RowSums all_waves(const LogprobShared& sh, double k2) {
-  RowSums r{sh.c[0], sh.S[0], sh.E[0]};
-#pragma unroll
-  for (int w = 1; w < 4; ++w) r = join(r, RowSums{sh.c[w], sh.S[w], sh.E[w]}, k2);
-  return r;
+  const int w = min(lane_id(), kLogprobWaves - 1);
+  RowSums mine{sh.c[w], sh.rho[w], sh.S[w], sh.E[w]};
+  if (lane_id() >= kLogprobWaves) mine = RowSums{-INFINITY, 0.0, 0.0, 0.0};
+  return join(mine, k2);
 }
 
-// The results of an entry, from its row's sums and the waves' lists.
-template <typename T> __device__ void finish(const LogprobParams& p, int64_t entry, const void* row, const RowSums& sums, int status, LogprobShared& sh) {
-  const int tid = threadIdx.x, top = p.top;
+// The first wave: the results of an entry, from its row's sums and the list.
+__device__ __forceinline__ void finish(const LogprobParams& p, int64_t entry, int32_t token, float z, const RowSums& sums, int status, const List& list) {
+  const int lane = lane_id(), top = p.top;
   status |= sums.S != sums.S || sums.c == INFINITY ? 1 : sums.c == -INFINITY ? 2 : 0;
+  const bool usable = (status & 3) == 0, there = token >= 0 && token < p.V;
   // (log probabilities from differences to the reference: of logits near fp32's largest the normaliser has no room for ln S)
-  const double rT = p.rT, c = sums.c, ln_S = log(sums.S), lse = c * rT + ln_S;
-  if (tid == 0) {
-    const int32_t token = p.tokens ? as_global(p.tokens)[entry] : -1;
-    const bool there = token >= 0 && token < p.V;
-    double logp = NAN;
-    if (there && (status & 3) == 0) logp = (double(load_elem<T>(row, token)) - c) * rT - ln_S;
-    if (!there && token != -1) status |= kBadIndex;
-    const bool usable = (status & 3) == 0;
-    if (p.logp) p.logp[entry] = float(logp);
+  const double rT = p.rT, c = sums.c, ln_S = log(sums.S);
+  if (!there && token != -1) status |= kBadIndex;
+  if (lane == 0) {
+    if (p.logp) p.logp[entry] = there && usable ? float((double(z) - c) * rT - ln_S) : NAN;
     if (p.entropy) p.entropy[entry] = usable ? float(fmax(ln_S - 0.69314718055994530942 * sums.E / sums.S, 0.0)) : NAN;
-    if (p.lse) p.lse[entry] = usable ? float(lse) : status & 1 ? NAN : -INFINITY;
+    if (p.lse) p.lse[entry] = usable ? float(c * rT + ln_S) : status & 1 ? NAN : -INFINITY;
     if (p.status) p.status[entry] = status;
   }
   if (top == 0) return;
-  // the lists of four waves: a record's place is how many are larger
-  uint64_t mine = 0;
+  // a record's place is how many are larger
+  const int n = usable ? list.n : 0;
+  const uint64_t mine = lane < n ? list.at[lane] : 0;
   int place = 0;
-  if ((status & 3) == 0 && tid < 4 * top) {
-    const int w = tid / top, i = tid - w * top;
-    if (i < sh.n[w]) mine = sh.list[w][i];
+  for (int i = 0; i < n; ++i) {
+    const uint64_t other = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(mine >> 32), i))) << 32 | uint32_t(__builtin_amdgcn_readlane(int(mine), i));
+    place += other > mine ? 1 : 0;
   }
-  int total = 0;
-  for (int w = 0; w < 4; ++w) {
-    const int n = sh.n[w];
-    total += n;
-    for (int i = 0; i < n; ++i) place += sh.list[w][i] > mine ? 1 : 0;
-  }
-  if ((status & 3) != 0) total = 0;
-  if (mine != 0 && place < top) {
+  if (lane < n) {
     p.top_idx[entry * top + place] = int32_t(cand_index(mine));
     p.top_logp[entry * top + place] = float((double(cand_value(mine)) - c) * rT - ln_S);
-  }
-  if (tid < top && tid >= total) {
-    p.top_idx[entry * top + tid] = -1;
-    p.top_logp[entry * top + tid] = -INFINITY;
+  } else if (lane < top) {
+    p.top_idx[entry * top + lane] = -1;
+    p.top_logp[entry * top + lane] = -INFINITY;
   }
 }
 
@@ -308,89 +365,80 @@ __device__ __forceinline__ void refuse(const LogprobParams& p, int64_t entry, in
 }
 
 template <typename T>
-__global__ __launch_bounds__(kBlock) void logprob_kernel(const LogprobParams p) {
+__global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(const LogprobParams p) {
   __shared__ LogprobShared sh;
   const int tid = threadIdx.x, wave = wave_id(), lane = lane_id();
   const uint32_t entry = blockIdx.x / uint32_t(p.slices);
   const int slice = int(blockIdx.x - entry * uint32_t(p.slices));
   const uint32_t b = entry / uint32_t(p.m);
   const int j = int(entry - b * uint32_t(p.m));
+  // (asked for together)
+  const int named = p.count ? as_global(p.count)[b] : p.m, at = p.index ? as_global(p.index)[entry] : j;
+  const int32_t token = p.tokens ? as_global(p.tokens)[entry] : -1;
+  const int count = min(max(named, 0), p.m);
   // (a count that does not fit is told in the status of the sequence's first entry, also where that one does not count)
-  const int odd = j == 0 && p.count && as_global(p.count)[b] != counted(p.count, b, p.m) ? kBadIndex : 0;
-  if (j >= counted(p.count, b, p.m)) {
+  const int odd = j == 0 && named != count ? kBadIndex : 0;
+  if (j >= count) {
     if (odd && slice == 0 && tid == 0 && p.status) p.status[entry] = odd;
     return;
   }
-  const int at = p.index ? as_global(p.index)[entry] : j;
   if (at < 0 || at >= p.n) {
     if (slice == 0) refuse(p, entry, kBadIndex);
     return;
   }
   const void* row = reinterpret_cast<const char*>(p.logits) + (int64_t(b) * p.seq_stride + at * p.row_stride) * ElemTraits<T>::kBytes;
-  row_share<T>(row, p, slice, sh);
-  RowSums sums = all_waves(sh, p.k2);
-  if (p.slices > 1) {
-    const int size = 3 + p.top;
-    uint64_t* words = p.words + int64_t(entry) * p.slices;
-    uint64_t* part = p.part + int64_t(entry) * p.slices * size;
+  const float z = token >= 0 && token < p.V ? load_elem<T>(row, token) : 0.0f;
+  List list;
+  row_share<T>(row, p, slice, sh, list);
+  if (p.slices == 1) {
+    if (wave == 0) finish(p, entry, token, z, all_waves(sh, p.k2), odd, list);
+    return;
+  }
+  const int size = 4 + p.top;
+  uint64_t* words = p.words + int64_t(entry) * p.slices;
+  uint64_t* part = p.part + int64_t(entry) * p.slices * size;
+  if (wave == 0) {
+    const RowSums sums = all_waves(sh, p.k2);
     uint64_t* own = part + slice * size;
-    // this slice's list: the largest of its waves' (0 behind them, which is less than any record)
-    if (p.top > 0) {
-      uint64_t mine = 0;
-      int place = 0, total = 0;
-      if (tid < 4 * p.top) {
-        const int w = tid / p.top, i = tid - w * p.top;
-        if (i < sh.n[w]) mine = sh.list[w][i];
-      }
-      for (int w = 0; w < 4; ++w) {
-        total += sh.n[w];
-        for (int i = 0; i < sh.n[w]; ++i) place += sh.list[w][i] > mine ? 1 : 0;
-      }
-      if (mine != 0 && place < p.top) store_through(own + 3 + place, mine);
-      if (tid < p.top && tid >= total) store_through(own + 3 + tid, 0);
-    }
-    if (tid == 0) {
+    if (lane < p.top) store_through(own + 4 + lane, lane < list.n ? list.at[lane] : 0);
+    if (lane == 0) {
       store_through(own, as_u32(sums.c));
       store_through(own + 1, __builtin_bit_cast(uint64_t, sums.S));
       store_through(own + 2, __builtin_bit_cast(uint64_t, sums.E));
+      store_through(own + 3, list.least);
     }
-    if (!all_arrived(words, slice, p.slices, p.tag, sh.told)) return;
-    if (wave == 0) {
-      const bool mine = claimed(words, p.slices, p.tag);
-      if (lane == 0) sh.mine = mine;
-    }
-    __syncthreads();
-    if (!sh.mine) return;
-    // A lane has a slice's sums.  The lists lie in the order of the row: of equal numbers the first are met first, so that the threshold from before
-    // 64 records holds for all of them.
-    if (wave == 0) {
-      const uint64_t* from = part + min(lane, p.slices - 1) * size;
-      RowSums got{as_f32(uint32_t(load_through(from))), __builtin_bit_cast(double, load_through(from + 1)), __builtin_bit_cast(double, load_through(from + 2))};
-      if (lane >= p.slices) got = RowSums{-INFINITY, 0.0, 0.0};
-      const RowSums all = join(got, RowSums{wave_max_f32(got.c), 0.0, 0.0}, p.k2);
-      const double S = wave_sum_f64(all.S), Es = wave_sum_f64(all.E);
-      if (lane < 4) { sh.c[lane] = all.c; sh.S[lane] = lane == 0 ? S : 0.0; sh.E[lane] = lane == 0 ? Es : 0.0; }
-    }
-    List list{sh.list[wave], 0, -INFINITY};
-    if (p.top > 0) {
-      const int records = p.slices * p.top, each = (records + 3) / 4, from = wave * each, to = min(from + each, records);
-      for (int r0 = from; r0 < to; r0 += 64 * kAhead) {
-        uint64_t r[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          const int i = r0 + 64 * u + lane, s = min(i, records - 1) / p.top;
-          r[u] = i < to ? load_through(part + s * size + 3 + (i - s * p.top)) : 0;
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) offer(list, r[u] != 0 && cand_value(r[u]) > list.above, r[u], p.top);
-      }
-      cut(list, p.top);
-    }
-    if (lane == 0) sh.n[wave] = list.n;
-    __syncthreads();
-    sums = all_waves(sh, p.k2);
   }
-  finish<T>(p, entry, row, sums, odd, sh);
+  if (!all_arrived(words, slice, p.slices, p.tag, sh.told)) return;
+  if (wave == 0) {
+    const bool mine = claimed(words, p.slices, p.tag);
+    if (lane == 0) sh.mine = mine;
+  }
+  __syncthreads();
+  if (!sh.mine) return;
+  // A lane has a slice's sums.  Where a slice has `top` records, nothing below the least of them is among the row's.
+  const uint64_t* from = part + min(lane, p.slices - 1) * size;
+  const uint64_t c = load_through(from), S = load_through(from + 1), Es = load_through(from + 2), least = p.top > 0 ? load_through(from + 3) : 0;
+  RowSums got{as_f32(uint32_t(c)), 0.0, __builtin_bit_cast(double, S), __builtin_bit_cast(double, Es)};
+  if (lane >= p.slices) got = RowSums{-INFINITY, 0.0, 0.0, 0.0};
+  if (p.top > 0) {
+    const uint32_t hi = wave_max_u32(uint32_t(least >> 32));
+    const uint64_t reach = uint64_t(hi) << 32 | wave_max_u32(uint32_t(least >> 32) == hi ? uint32_t(least) : 0);
+    list = List{sh.list[wave], 0, -INFINITY, 0};
+    const int records = p.slices * p.top, each = (records + kLogprobWaves - 1) / kLogprobWaves, begin = wave * each, end = min(begin + each, records);
+    constexpr int kTogether = 8;
+    for (int r0 = begin; r0 < end; r0 += 64 * kTogether) {
+      uint64_t r[kTogether];
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) {
+        const int i = r0 + 64 * u + lane, s = min(i, records - 1) / p.top;
+        r[u] = i < end ? load_through(part + s * size + 4 + (i - s * p.top)) : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) offer(list, r[u] != 0 && r[u] >= reach && r[u] >= list.least, r[u], p.top);
+    }
+    put_together(list, p.top, sh);
+  }
+  if (wave == 0) finish(p, entry, token, z, join(got, p.k2), odd, list);
 }
 
 // ---- the gradient of the logits ---------------------------------------------------------------------------------

@@ -14,7 +14,7 @@ int shares(int64_t entries, int64_t V, int bytes) {
   return int(std::max<int64_t>(1, std::min<int64_t>(most, fill / std::max<int64_t>(entries, 1))));
 }
 size_t word_bytes(int64_t entries, int slices) { return (size_t(entries) * slices * 8 + 255) / 256 * 256; }
-size_t shared_bytes(int64_t entries, int slices, int top) { return slices == 1 ? 0 : word_bytes(entries, slices) + size_t(entries) * slices * (3 + top) * 8; }
+size_t shared_bytes(int64_t entries, int slices, int top) { return slices == 1 ? 0 : word_bytes(entries, slices) + size_t(entries) * slices * (4 + top) * 8; }
 
 int check_logits(const char* who, tslt_dtype dt, int64_t B, int32_t n, int64_t V, float temperature, int32_t top) {
   if (!valid_dtype(dt)) return fail(TSLT_ERR_INVALID_ARG, "%s: unknown dtype %d", who, int(dt));
@@ -66,7 +66,7 @@ int tslt_logprob(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_
   int code;
   if (!grid_fits(who, entries * p.slices, code)) return code;
   const auto kernel = dt == TSLT_F32 ? tslt::logprob_kernel<float> : dt == TSLT_BF16 ? tslt::logprob_kernel<tslt::Bf16> : tslt::logprob_kernel<tslt::F16>;
-  hipLaunchKernelGGL(kernel, dim3(unsigned(entries * p.slices)), dim3(tslt::kBlock), 0, reinterpret_cast<hipStream_t>(stream), p);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(entries * p.slices)), dim3(tslt::kLogprobThreads), 0, reinterpret_cast<hipStream_t>(stream), p);
   return launched("tslt_logprob launch");
 }
 
