@@ -6,11 +6,12 @@
 // and H = ln S - ln 2 E / S.  A wave whose logits pass its reference takes the larger one: S 2^d and 2^d (E + d S), d < 0 the difference.
 //
 // The `top` largest: each wave keeps a list in LDS of the logits above a threshold that `top` of the row's logits are known to reach.  At first that are the largest
-// logits of its lanes in the first loads: `top` of those 64 numbers are reached by as many logits.  Then the waves put their lists together, cut what they have to `top`, and
-// take the least of them as threshold: after the first loads, and again whenever twice as much of the row has been met, so that between two
-// of these about `top` logits are listed.  A logit costs no more than its share of a comparison a load, which the reference needs as well.
+// logits of the workgroup's lanes in the first loads: `top` of those 256 numbers are reached by as many logits, and by few more.  Whenever twice as much of the row has been
+// met the waves put their lists together, cut what they have to `top`, and take the least of them as threshold, so that between two of these
+// about `top` logits are listed.  A logit costs no more than its share of a comparison a load, which the reference needs as well.
 //
-// Few rows: several workgroups to a row, whose sums and lists the last of them to end joins (handover.h).
+// Few rows: several workgroups to a row, whose sums and lists the last of them to end joins (handover.h).  What it joins goes by a threshold from the waves' largest
+// logits again.
 #pragma once
 #include "handover.h"
 #include "rows.h"
@@ -20,6 +21,7 @@ namespace tslt {
 constexpr int kMaxTop = 32;
 constexpr int kListRoom = 128;           // records of a wave's list
 constexpr int kLogprobWaves = 4, kLogprobThreads = 64 * kLogprobWaves;
+constexpr int kPartHead = 4 + kLogprobWaves / 2, kPartWords = kPartHead + 64;
 
 struct LogprobParams {
   const void* logits;
@@ -32,7 +34,7 @@ struct LogprobParams {
   int32_t *top_idx, *status;
   int slices;                            // workgroups of a row, 64 at most
   uint64_t* words;                       // [entries][slices]
-  uint64_t* part;                        // [entries][slices][4 + top]: reference, S, E, the least record of a full list (else 0), the list
+  uint64_t* part;                        // [entries][slices][kPartWords]: reference, S, E, length of the list, the waves' largest logits, the list
   Tag tag;
 };
 
@@ -112,14 +114,21 @@ __device__ __forceinline__ void offer(List& l, bool mine, uint64_t record, int t
   l.n += __popcll(who);
   if (l.n > kListRoom - 64) cut(l, top);
 }
-// A first threshold from the largest of every lane: `top` of them reach it.
-__device__ __forceinline__ float reached_by(float largest, int top) {
-  const uint32_t key = mono_key(largest + 0.0f);
+// A threshold from N numbers a lane: `top` of them are greater.  (-inf if there are not so many; 16 bits of it, so that it is some 1 % low.)
+template <int N> __device__ __forceinline__ float reached_by(const float (&largest)[N], int top) {
+  uint32_t key[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) key[i] = mono_key(largest[i] + 0.0f) >> 16;
   uint32_t least = 0;
-  for (int bit = 31; bit >= 16; --bit) {
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
     const uint32_t trial = least | 1u << bit;
-    if (__popcll(ballot(key >= trial)) >= top) least = trial;
+    int reach = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) reach += __popcll(ballot(key[i] >= trial));
+    if (reach >= top) least = trial;
   }
+  least <<= 16;
   // the number before it (before both zeros, which are equal)
   return least > kKeyNegInf ? key_to_f32(least == 0x80000000u ? least - 2 : least - 1) : -INFINITY;
 }
@@ -180,13 +189,14 @@ struct LogprobShared {
   uint64_t list[kLogprobWaves][kListRoom];
   double rho[kLogprobWaves], S[kLogprobWaves], E[kLogprobWaves];
   float c[kLogprobWaves];
+  float largest[kLogprobThreads];
   int n[kLogprobWaves];
   uint64_t least;
   int told, mine;
 };
 
-// The waves' lists put together and cut down to `top` records, which the first wave's list then has.  All threads.
-__device__ __forceinline__ void put_together(List& l, int top, LogprobShared& sh) {
+// The waves' lists put together and cut down to `top` records, or to 64 at most if they need not be the least; the first wave's list then has them.  All threads.
+template <bool kLast> __device__ __forceinline__ void put_together(List& l, int top, LogprobShared& sh) {
   const int wave = wave_id(), lane = lane_id();
   if (l.n > 64) cut(l, top);
   if (lane == 0) sh.n[wave] = l.n;
@@ -201,14 +211,16 @@ __device__ __forceinline__ void put_together(List& l, int top, LogprobShared& sh
       total += n;
     }
     uint64_t least = 0;
-    if (total > top) least = least_of_top(r, top);
+    if (total > (kLast ? 64 : top)) least = least_of_top(r, top);
     wave_sync();
     l.n = keep_from(r, least, l.at);
+    if constexpr (kLast) return;
     if (total >= top) least = least_record(r, least);
     if (lane == 0) sh.least = least;
   } else {
     l.n = 0;
   }
+  if constexpr (kLast) return;
   __syncthreads();
   l.least = sh.least;
   if (l.least != 0) l.above = fmaxf(l.above, cand_value(l.least));
@@ -232,7 +244,7 @@ template <typename T> __device__ __forceinline__ void take(RowWave& w, const uin
   float z[E];
   unpack<T>(x, z);
   const float most = largest_of(z), above = w.list.above;
-  if (ballot(most > above) != 0) {
+  if (ballot(most > fminf(above, w.c)) != 0) {
     if (ballot(most > w.c) != 0) w.refer(wave_max_f32(fmaxf(most, w.c)), k2);
     if (top == 0) w.list.above = w.c;
     else
@@ -277,9 +289,18 @@ template <typename T> __device__ void row_share(const void* row, const LogprobPa
     }
     const float all = wave_max_f32(fmaxf(most, w.c));
     if (all > w.c) w.refer(all, p.k2);
-    w.list.above = top > 0 ? fmaxf(w.list.above, reached_by(most, top)) : w.c;
+    if (top == 0) {
+      w.list.above = w.c;
+    } else {
+      sh.largest[threadIdx.x] = most;
+      __syncthreads();
+      float largest[kLogprobWaves];
+#pragma unroll
+      for (int i = 0; i < kLogprobWaves; ++i) largest[i] = sh.largest[64 * i + lane];
+      w.list.above = fmaxf(w.list.above, reached_by(largest, top));
+    }
   }
-  int round = 0, together = 1;
+  int round = 0, together = 2;
   for (int64_t v0 = begin; v0 < end; v0 += kRound, v += kRound) {
     uint4 next[kAhead];
 #pragma unroll
@@ -289,9 +310,7 @@ template <typename T> __device__ void row_share(const void* row, const LogprobPa
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) x[u] = next[u];
     if (top > 0 && ++round == together && v0 + 2 * kRound < end) {
-      put_together(w.list, top, sh);
-      // (what does not pass the threshold is not held against the reference)
-      if (w.list.above > w.c) w.refer(w.list.above, p.k2);
+      put_together<false>(w.list, top, sh);
       together = 2 * round;
     }
   }
@@ -305,7 +324,7 @@ template <typename T> __device__ void row_share(const void* row, const LogprobPa
     sh.c[wave] = w.c;
   }
   list = w.list;
-  if (top > 0) put_together(list, top, sh);
+  if (top > 0) put_together<true>(list, top, sh);
   else __syncthreads();
 }
 
@@ -340,10 +359,11 @@ __device__ __forceinline__ void finish(const LogprobParams& p, int64_t entry, in
     const uint64_t other = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(mine >> 32), i))) << 32 | uint32_t(__builtin_amdgcn_readlane(int(mine), i));
     place += other > mine ? 1 : 0;
   }
-  if (lane < n) {
+  if (lane < n && place < top) {
     p.top_idx[entry * top + place] = int32_t(cand_index(mine));
     p.top_logp[entry * top + place] = float((double(cand_value(mine)) - c) * rT - ln_S);
-  } else if (lane < top) {
+  }
+  if (lane >= n && lane < top) {
     p.top_idx[entry * top + lane] = -1;
     p.top_logp[entry * top + lane] = -INFINITY;
   }
@@ -394,18 +414,18 @@ __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(const LogprobP
     if (wave == 0) finish(p, entry, token, z, all_waves(sh, p.k2), odd, list);
     return;
   }
-  const int size = 4 + p.top;
   uint64_t* words = p.words + int64_t(entry) * p.slices;
-  uint64_t* part = p.part + int64_t(entry) * p.slices * size;
+  uint64_t* part = p.part + int64_t(entry) * p.slices * kPartWords;
   if (wave == 0) {
     const RowSums sums = all_waves(sh, p.k2);
-    uint64_t* own = part + slice * size;
-    if (lane < p.top) store_through(own + 4 + lane, lane < list.n ? list.at[lane] : 0);
+    uint64_t* own = part + slice * kPartWords;
+    if (p.top > 0 && lane < list.n) store_through(own + kPartHead + lane, list.at[lane]);
+    if (lane < kLogprobWaves / 2) store_through(own + 4 + lane, uint64_t(as_u32(sh.c[2 * lane + 1])) << 32 | as_u32(sh.c[2 * lane]));
     if (lane == 0) {
       store_through(own, as_u32(sums.c));
       store_through(own + 1, __builtin_bit_cast(uint64_t, sums.S));
       store_through(own + 2, __builtin_bit_cast(uint64_t, sums.E));
-      store_through(own + 3, list.least);
+      store_through(own + 3, uint64_t(list.n));
     }
   }
   if (!all_arrived(words, slice, p.slices, p.tag, sh.told)) return;
@@ -415,28 +435,33 @@ __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(const LogprobP
   }
   __syncthreads();
   if (!sh.mine) return;
-  // A lane has a slice's sums.  Where a slice has `top` records, nothing below the least of them is among the row's.
-  const uint64_t* from = part + min(lane, p.slices - 1) * size;
-  const uint64_t c = load_through(from), S = load_through(from + 1), Es = load_through(from + 2), least = p.top > 0 ? load_through(from + 3) : 0;
-  RowSums got{as_f32(uint32_t(c)), 0.0, __builtin_bit_cast(double, S), __builtin_bit_cast(double, Es)};
+  // a lane has a slice's sums
+  const uint64_t* from = part + min(lane, p.slices - 1) * kPartWords;
+  uint64_t head[kPartHead];
+#pragma unroll
+  for (int i = 0; i < kPartHead; ++i) head[i] = i < 3 || p.top > 0 ? load_through(from + i) : 0;
+  RowSums got{as_f32(uint32_t(head[0])), 0.0, __builtin_bit_cast(double, head[1]), __builtin_bit_cast(double, head[2])};
   if (lane >= p.slices) got = RowSums{-INFINITY, 0.0, 0.0, 0.0};
   if (p.top > 0) {
-    const uint32_t hi = wave_max_u32(uint32_t(least >> 32));
-    const uint64_t reach = uint64_t(hi) << 32 | wave_max_u32(uint32_t(least >> 32) == hi ? uint32_t(least) : 0);
+    float largest[kLogprobWaves];
+#pragma unroll
+    for (int i = 0; i < kLogprobWaves; ++i) largest[i] = lane < p.slices ? as_f32(uint32_t(head[4 + i / 2] >> (32 * (i & 1)))) : -INFINITY;
+    const float above = reached_by(largest, p.top);
+    const int length = lane < p.slices ? int(head[3]) : 0;
     list = List{sh.list[wave], 0, -INFINITY, 0};
-    const int records = p.slices * p.top, each = (records + kLogprobWaves - 1) / kLogprobWaves, begin = wave * each, end = min(begin + each, records);
     constexpr int kTogether = 8;
-    for (int r0 = begin; r0 < end; r0 += 64 * kTogether) {
+    for (int s0 = wave; s0 < p.slices; s0 += kLogprobWaves * kTogether) {
       uint64_t r[kTogether];
 #pragma unroll
       for (int u = 0; u < kTogether; ++u) {
-        const int i = r0 + 64 * u + lane, s = min(i, records - 1) / p.top;
-        r[u] = i < end ? load_through(part + s * size + 4 + (i - s * p.top)) : 0;
+        const int s = min(s0 + u * kLogprobWaves, 63);
+        r[u] = lane < __builtin_amdgcn_readlane(length, s) ? load_through(part + s * kPartWords + kPartHead + lane) : 0;
       }
 #pragma unroll
-      for (int u = 0; u < kTogether; ++u) offer(list, r[u] != 0 && r[u] >= reach && r[u] >= list.least, r[u], p.top);
+      for (int u = 0; u < kTogether; ++u)
+        offer(list, s0 + u * kLogprobWaves < p.slices && r[u] != 0 && cand_value(r[u]) > above && r[u] >= list.least, r[u], p.top);
     }
-    put_together(list, p.top, sh);
+    put_together<true>(list, p.top, sh);
   }
   if (wave == 0) finish(p, entry, token, z, join(got, p.k2), odd, list);
 }

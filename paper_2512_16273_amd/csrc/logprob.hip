@@ -14,7 +14,7 @@ int shares(int64_t entries, int64_t V, int bytes) {
   return int(std::max<int64_t>(1, std::min<int64_t>(most, fill / std::max<int64_t>(entries, 1))));
 }
 size_t word_bytes(int64_t entries, int slices) { return (size_t(entries) * slices * 8 + 255) / 256 * 256; }
-size_t shared_bytes(int64_t entries, int slices, int top) { return slices == 1 ? 0 : word_bytes(entries, slices) + size_t(entries) * slices * (4 + top) * 8; }
+size_t shared_bytes(int64_t entries, int slices) { return slices == 1 ? 0 : word_bytes(entries, slices) + size_t(entries) * slices * tslt::kPartWords * 8; }
 
 int check_logits(const char* who, tslt_dtype dt, int64_t B, int32_t n, int64_t V, float temperature, int32_t top) {
   if (!valid_dtype(dt)) return fail(TSLT_ERR_INVALID_ARG, "%s: unknown dtype %d", who, int(dt));
@@ -34,7 +34,7 @@ extern "C" {
 
 size_t tslt_logprob_workspace_bytes(int64_t B, int32_t m, int64_t V, int32_t top) {
   if (B < 1 || m < 1 || V < 1 || top < 0 || top > TSLT_MAX_TOP || B > 0x7FFFFFFF / m) return 0;
-  return std::max(shared_bytes(B * m, shares(B * m, V, 2), top), shared_bytes(B * m, shares(B * m, V, 4), top));
+  return std::max(shared_bytes(B * m, shares(B * m, V, 2)), shared_bytes(B * m, shares(B * m, V, 4)));
 }
 
 int tslt_logprob(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_t V, int64_t seq_stride, int64_t row_stride, float temperature,
@@ -55,7 +55,7 @@ int tslt_logprob(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_
   p.logp = out_logp; p.entropy = out_entropy; p.lse = out_lse; p.top_idx = out_top_idx; p.top_logp = out_top_logp; p.status = status;
   const int64_t entries = B * m;
   p.slices = shares(entries, V, elem_bytes(dt));
-  const size_t need = shared_bytes(entries, p.slices, top);
+  const size_t need = shared_bytes(entries, p.slices);
   if (need > 0) {
     if (!ws || !aligned(ws, 256) || ws_bytes < need)
       return fail(TSLT_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu are needed, 256-byte aligned", who, ws ? ws_bytes : size_t(0), need);
