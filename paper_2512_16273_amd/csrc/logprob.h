@@ -110,9 +110,9 @@ __device__ __forceinline__ void cut(List& l, int top) {
 __device__ __forceinline__ void offer(List& l, bool mine, uint64_t record, int top) {
   const uint64_t who = ballot(mine);
   if (who == 0) return;
+  if (l.n > kListRoom - 64) cut(l, top);
   if (mine) l.at[l.n + lanes_below(who)] = record;
   l.n += __popcll(who);
-  if (l.n > kListRoom - 64) cut(l, top);
 }
 // A threshold from N numbers a lane: `top` of them are greater.  (-inf if there are not so many; 16 bits of it, so that it is some 1 % low.)
 template <int N> __device__ __forceinline__ float reached_by(const float (&largest)[N], int top) {
@@ -155,10 +155,14 @@ struct RowWave {
   List list;
   // A vector's terms, added up by themselves first; nothing of what is -inf.
   template <int N> __device__ __forceinline__ void terms(const float (&z)[N], float k2) {
+    if (same_in_wave(far)) add<N, true>(z, k2);
+    else add<N, false>(z, k2);
+  }
+  template <int N, bool kFar> __device__ __forceinline__ void add(const float (&z)[N], float k2) {
     float s[N], t[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const float d = far ? (z[e] - c) * k2 : fmaf(z[e], k2, -kc);
+      const float d = kFar ? (z[e] - c) * k2 : fmaf(z[e], k2, -kc);
       s[e] = fast_exp2(d);
       const float u = fmaxf(d, -200.0f);                 // (2^-200 is 0, and 0 times a number is 0)
       t[e] = e < N / 2 || N == 1 ? s[e] * u : fmaf(s[e], u, t[e - N / 2]);
@@ -237,6 +241,33 @@ template <int E> __device__ __forceinline__ float largest_of(const float (&z)[E]
   else return max3f(max3f(most, z[3], z[4]), max3f(z[5], z[6], z[7]), most);
 }
 
+// Those of a vector's numbers that are greater than `above`.
+template <int E> __device__ __forceinline__ void list_vector(List& l, const float (&z)[E], float above, uint32_t first, int top) {
+  uint64_t who[E];
+  int all = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    who[e] = ballot(z[e] > above);
+    all += __popcll(who[e]);
+  }
+  if (l.n + all <= kListRoom) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (who[e] != 0) {
+        if (z[e] > above) l.at[l.n + lanes_below(who[e])] = make_cand(z[e], first + e);
+        l.n += __popcll(who[e]);
+      }
+    return;
+  }
+#pragma unroll 1
+  for (int i = 0; i < E; ++i) {                          // (rare: one place in the code for all of them)
+    float x = z[0];
+#pragma unroll
+    for (int e = 1; e < E; ++e) x = i == e ? z[e] : x;
+    offer(l, x > above, make_cand(x, first + i), top);
+  }
+}
+
 // All lanes of a wave: their vector's numbers, of indices first .. first + E - 1.  (A vector's numbers are not met in their order: what is offered
 // goes by the threshold from before it, which all of those behind its numbers have reached with lower indices.)
 template <typename T> __device__ __forceinline__ void take(RowWave& w, const uint4& x, int64_t first, float k2, int top) {
@@ -247,9 +278,7 @@ template <typename T> __device__ __forceinline__ void take(RowWave& w, const uin
   if (ballot(most > fminf(above, w.c)) != 0) {
     if (ballot(most > w.c) != 0) w.refer(wave_max_f32(fmaxf(most, w.c)), k2);
     if (top == 0) w.list.above = w.c;
-    else
-#pragma unroll
-      for (int e = 0; e < E; ++e) offer(w.list, z[e] > above, make_cand(z[e], uint32_t(first + e)), top);
+    else list_vector(w.list, z, above, uint32_t(first), top);
   }
   w.terms(z, k2);
 }
@@ -556,10 +585,8 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
   const float f = float(exp2(-rho) * double(p.rT)), a0 = f * float(c0 - c1 * rho), a1 = f * float(c1), k2 = p.k2, none = there ? NAN : 0.0f;
   const bool fill = !there || !known;
   // (a p of 0 gives 0, whatever its logarithm)
-  const auto gradient = [&](float z) {
-    const float d = far ? (z - far_c) * k2 : fmaf(z, k2, -hi);
-    return fill ? none : fast_exp2(d) * fmaf(a1, fmaxf(d, -200.0f), a0);
-  };
+  const auto of = [&](float d) { return fast_exp2(d) * fmaf(a1, fmaxf(d, -200.0f), a0); };
+  const auto gradient = [&](float z) { return fill ? none : of(far ? (z - far_c) * k2 : fmaf(z, k2, -hi)); };
   __syncthreads();
   // the given places in this share: their numbers, before the logits are written over (by this share alone)
   if (!fill && tid <= p.top) {
@@ -590,8 +617,13 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
         for (int e = 0; e < E; ++e) z[e] = none;
       } else {
         unpack<T>(x[u], z);
+        if (same_in_wave(far)) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) z[e] = gradient(z[e]);
+          for (int e = 0; e < E; ++e) z[e] = of((z[e] - far_c) * k2);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) z[e] = of(fmaf(z[e], k2, -hi));
+        }
       }
       body[v0 + u * kBlock] = Vector16<T>::pack(z);
     }
