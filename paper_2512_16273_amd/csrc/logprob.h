@@ -625,7 +625,7 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
           for (int e = 0; e < E; ++e) z[e] = of(fmaf(z[e], k2, -hi));
         }
       }
-      body[v0 + u * kBlock] = Vector16<T>::pack(z);
+      __builtin_nontemporal_store(Vector16<T>::pack(z), body + v0 + u * kBlock);
     }
   }
   if (fill) return;

@@ -13,6 +13,12 @@ int shares(int64_t entries, int64_t V, int bytes) {
   const int64_t fill = 2 * int64_t(tslt::compute_units()), most = std::min<int64_t>(64, V * bytes / 8192);
   return int(std::max<int64_t>(1, std::min<int64_t>(most, fill / std::max<int64_t>(entries, 1))));
 }
+// Of the gradient, which leaves nothing to join, more: rows that do not count are only filled, so that shares take unequal times (8 x 256 rows of 128256, two thirds
+// of which count, with 2 / 8 / 16 / 32 / 64 workgroups a compute unit 173 / 173 / 151 / 147 / 148 us, all counting 217 / 214 / 209 / 203 / 204).
+int shares_back(int64_t entries, int64_t V, int bytes) {
+  const int64_t fill = 32 * int64_t(tslt::compute_units()), most = std::min<int64_t>(64, V * bytes / 16384);
+  return int(std::max<int64_t>(1, std::min<int64_t>(most, (fill + entries - 1) / std::max<int64_t>(entries, 1))));
+}
 size_t word_bytes(int64_t entries, int slices) { return (size_t(entries) * slices * 8 + 255) / 256 * 256; }
 size_t shared_bytes(int64_t entries, int slices) { return slices == 1 ? 0 : word_bytes(entries, slices) + size_t(entries) * slices * tslt::kPartWords * 8; }
 
@@ -89,7 +95,7 @@ int tslt_logprob_backward(const void* logits, tslt_dtype dt, int64_t B, int32_t 
   p.V = V; p.rT = 1.0f / temperature; p.k2 = exponent_scale(p.rT); p.n = n; p.top = grad_top ? top : 0;
   p.count = count; p.tokens = tokens; p.top_idx = top_idx; p.lse = lse; p.entropy = entropy;
   p.grad_logp = grad_logp; p.grad_entropy = grad_entropy; p.grad_lse = grad_lse; p.grad_top = grad_top;
-  p.slices = shares(B * n, V, elem_bytes(dt));
+  p.slices = shares_back(B * n, V, elem_bytes(dt));
   int code;
   if (!grid_fits(who, B * n * p.slices, code)) return code;
   const auto kernel = dt == TSLT_F32 ? tslt::logprob_backward_kernel<float> : dt == TSLT_BF16 ? tslt::logprob_backward_kernel<tslt::Bf16> : tslt::logprob_backward_kernel<tslt::F16>;
