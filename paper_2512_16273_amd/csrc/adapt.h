@@ -1,13 +1,13 @@
 // tslt_adapt: out = base + scale (x A^T) B^T, of every sequence its own A and B, in two launches.
 //
 // The first makes h = x A^T.  A workgroup has 16 tokens of one sequence, whose four waves share the channels, or 64, 16 a wave; where that makes few workgroups the
-// channels are cut too, and each cut leaves its sums.  The second adds those up, and has of 16 or 64 tokens 256 channels of the result, 64 a wave.
+// channels are cut too, and each cut leaves its sums.  The second adds those up, and has of 16 or 64 tokens runs of 256 channels of the result.
 //
 // Tokens are the columns of the matrix instructions and what is learned the rows, 16 bytes a lane straight from memory: a lane has of the first one's results
 // four ranks in a row, and of the second one's eight (four of fp32) channels in a row, as the rows of the second are dealt out to two instructions so.
 //
 // h enters the second in two terms of the rows' type, as if it were twice as many ranks: 16 bits of it for bfloat16, 22 for binary16 (whose range it is
-// brought to by a power of two a token), where the result keeps 8 and 11.  So the products of 16 ranks are one instruction of 32.
+// brought to by a power of two a token), where the result keeps 8 and 11.
 #pragma once
 #include "rows.h"
 
@@ -21,9 +21,10 @@ struct AdaptParams {
   const int32_t *adapter, *rank, *count;
   const float* scale;
   int32_t* status;
-  int tiles;                             // of a sequence's tokens
-  int chunks;                            // of the ranks (first launch), of the result's channels (second)
+  int tiles, up_tiles;                   // of a sequence's tokens, in the first launch and the second
+  int chunks;                            // of the ranks
   int cuts;                              // of the channels of x
+  int splits;                            // workgroups that share the result's channels
   float* h;                              // [cuts][B * n][R]
   bool copy;                             // out is not base
 };
@@ -64,62 +65,122 @@ __device__ __forceinline__ int adapter_of(const AdaptParams& p, int64_t b, int& 
   return a;
 }
 
-// h of kTokenTiles * 16 tokens and kRankTiles * 16 ranks.
-template <typename T, int kTokenTiles, int kRankTiles>
-__global__ __launch_bounds__(kBlock) void adapt_down_kernel(const AdaptParams p) {
+// Where a workgroup of the first launch stands: its cut of the channels, its ranks, its tokens.
+struct DownBlock {
+  int cut, rank0, rank, a, tile, tokens;
+  uint32_t b;
+  __device__ __forceinline__ DownBlock(const AdaptParams& p, int rank_tiles) {
+    uint32_t block = blockIdx.x;
+    cut = int(block % uint32_t(p.cuts));
+    block /= uint32_t(p.cuts);
+    rank0 = int(block % uint32_t(p.chunks)) * (16 * rank_tiles);
+    block /= uint32_t(p.chunks);
+    b = block / uint32_t(p.tiles);
+    tile = int(block - b * uint32_t(p.tiles));
+    tokens = counted(p.count, b, p.n);
+    bool odd;
+    a = adapter_of(p, b, rank, odd);
+  }
+};
+
+// h of 16 tokens and kRankTiles * 16 ranks: the four waves share the channels.
+template <typename T, int kRankTiles>
+__global__ __launch_bounds__(kBlock) void adapt_down_few_kernel(const AdaptParams p) {
   constexpr int kBytes = ElemTraits<T>::kBytes, kLane = 16 / kBytes, kStep = Product<T>::kChannels;
-  constexpr bool kShare = kTokenTiles == 1;              // the waves share the channels
-  __shared__ f32x4 part[kShare ? 3 : 1][kShare ? kRankTiles : 1][64];
-  const int wave = wave_id(), lane = lane_id(), r = lane & 15, g = lane >> 4;
-  uint32_t block = blockIdx.x;
-  const int cut = int(block % uint32_t(p.cuts));
-  block /= uint32_t(p.cuts);
-  const int chunk = int(block % uint32_t(p.chunks));
-  block /= uint32_t(p.chunks);
-  const uint32_t b = block / uint32_t(p.tiles);
-  const int tile = int(block - b * uint32_t(p.tiles)), tokens = counted(p.count, b, p.n);
-  const int t0 = tile * (16 * kTokenTiles) + (kShare ? 0 : 16 * wave), rank0 = chunk * (16 * kRankTiles);
-  int rank;
-  bool odd;
-  const int a = adapter_of(p, b, rank, odd);
-  if (tile * (16 * kTokenTiles) >= tokens || rank0 >= rank) return;
-  const int tiles = min((rank - rank0 + 15) / 16, kRankTiles);
-  // this cut's steps, and the wave's of them
-  const int steps = (p.K + kStep - 1) / kStep, each = (steps + p.cuts - 1) / p.cuts, begin = cut * each, end = min(begin + each, steps);
-  const char* x = reinterpret_cast<const char*>(p.x.data) + (int64_t(b) * p.x.seq + min(t0 + r, tokens - 1) * p.x.token) * kBytes;
-  const char* rows = reinterpret_cast<const char*>(p.a) + ((int64_t(a) * p.R + rank0 + r) * p.K) * kBytes;
+  __shared__ f32x4 part[3][kRankTiles][64];
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, g = lane >> 4;
+  const DownBlock at(p, kRankTiles);
+  const int t0 = at.tile * 16, rank0 = at.rank0;
+  if (t0 >= at.tokens || rank0 >= at.rank) return;
+  const int tiles = min((at.rank - rank0 + 15) / 16, kRankTiles);
+  const int steps = (p.K + kStep - 1) / kStep, each = (steps + p.cuts - 1) / p.cuts, begin = at.cut * each, end = min(begin + each, steps);
+  const char* x = reinterpret_cast<const char*>(p.x.data) + (int64_t(at.b) * p.x.seq + min(t0 + r, at.tokens - 1) * p.x.token) * kBytes;
+  const char* rows = reinterpret_cast<const char*>(p.a) + ((int64_t(at.a) * p.R + rank0 + r) * p.K) * kBytes;
   f32x4 sum[kRankTiles];
 #pragma unroll
   for (int j = 0; j < kRankTiles; ++j) sum[j] = f32x4{0, 0, 0, 0};
-  constexpr int kAheadSteps = 4, kEvery = kShare ? 4 : 1;
-  for (int s0 = begin + (kShare ? wave : 0); s0 < end; s0 += kEvery * kAheadSteps) {
-    u32x4 xs[kAheadSteps], as[kAheadSteps][kRankTiles];
+  constexpr int kSteps = 4;
+  for (int s0 = begin + wave; s0 < end; s0 += 4 * kSteps) {
+    u32x4 xs[kSteps], as[kSteps][kRankTiles];
 #pragma unroll
-    for (int u = 0; u < kAheadSteps; ++u) {
-      const int s = s0 + u * kEvery, k = s * kStep + g * kLane;
+    for (int u = 0; u < kSteps; ++u) {
+      const int s = s0 + u * 4, k = s * kStep + g * kLane;
       const bool there = s < end && k < p.K;             // (K is a multiple of a lane's channels)
       xs[u] = there ? load16(x + int64_t(k) * kBytes) : u32x4{0, 0, 0, 0};
 #pragma unroll
       for (int j = 0; j < kRankTiles; ++j) as[u][j] = there && j < tiles ? load16(rows + (int64_t(16 * j) * p.K + k) * kBytes) : u32x4{0, 0, 0, 0};
     }
 #pragma unroll
-    for (int u = 0; u < kAheadSteps; ++u)
+    for (int u = 0; u < kSteps; ++u)
 #pragma unroll
       for (int j = 0; j < kRankTiles; ++j) sum[j] = Product<T>::add(as[u][j], xs[u], sum[j]);
   }
-  if constexpr (kShare) {
-    if (wave > 0)
+  if (wave > 0)
 #pragma unroll
-      for (int j = 0; j < kRankTiles; ++j) part[wave - 1][j][lane] = sum[j];
-    __syncthreads();
-    if (wave > 0) return;
+    for (int j = 0; j < kRankTiles; ++j) part[wave - 1][j][lane] = sum[j];
+  __syncthreads();
+  if (wave > 0 || t0 + r >= at.tokens) return;
+  float* to = p.h + ((int64_t(at.cut) * p.B + at.b) * p.n + t0 + r) * p.R + rank0 + 4 * g;
 #pragma unroll
-    for (int j = 0; j < kRankTiles; ++j)
+  for (int j = 0; j < kRankTiles; ++j) {
 #pragma unroll
-      for (int w = 0; w < 3; ++w) sum[j] += part[w][j][lane];
+    for (int w = 0; w < 3; ++w) sum[j] += part[w][j][lane];
+    if (j < tiles) *reinterpret_cast<f32x4*>(to + 16 * j) = sum[j];
   }
-  if (t0 + r >= tokens) return;
-  float* to = p.h + ((int64_t(cut) * p.B + b) * p.n + t0 + r) * p.R + rank0 + 4 * g;
+}
+
+// h of 64 tokens, 16 a wave: A goes through LDS, 128 bytes of each rank at a time, as all four waves take it.  Its 16-byte pieces are dealt out there so that
+// the 16 ranks of an operand lie in different banks.
+template <typename T, int kRankTiles>
+__global__ __launch_bounds__(kBlock) void adapt_down_many_kernel(const AdaptParams p) {
+  constexpr int kBytes = ElemTraits<T>::kBytes, kLane = 16 / kBytes, kRound = 128 / kBytes;      // channels of a lane, of a round
+  constexpr int kPieces = kRankTiles * 16 * 8, kMine = (kPieces + kBlock - 1) / kBlock;
+  __shared__ u32x4 piece[2][kPieces];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, g = lane >> 4;
+  const DownBlock at(p, kRankTiles);
+  const int t0 = at.tile * 64 + 16 * wave, rank0 = at.rank0;
+  if (at.tile * 64 >= at.tokens || rank0 >= at.rank) return;
+  const int tiles = min((at.rank - rank0 + 15) / 16, kRankTiles);
+  const int rounds = (p.K + kRound - 1) / kRound, each = (rounds + p.cuts - 1) / p.cuts, begin = at.cut * each, end = min(begin + each, rounds);
+  const char* x = reinterpret_cast<const char*>(p.x.data) + (int64_t(at.b) * p.x.seq + min(t0 + r, at.tokens - 1) * p.x.token) * kBytes;
+  const char* rows = reinterpret_cast<const char*>(p.a) + ((int64_t(at.a) * p.R + rank0) * p.K) * kBytes;
+  f32x4 sum[kRankTiles];
+#pragma unroll
+  for (int j = 0; j < kRankTiles; ++j) sum[j] = f32x4{0, 0, 0, 0};
+  u32x4 xs[2], as[kMine];
+  const auto ask = [&](int round) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int q = tid + i * kBlock, k = round * kRound + (q & 7) * kLane;
+      as[i] = round < end && q < 128 * tiles && k < p.K ? load16(rows + (int64_t(q >> 3) * p.K + k) * kBytes) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int k = round * kRound + (4 * u + g) * kLane;
+      xs[u] = round < end && k < p.K ? load16(x + int64_t(k) * kBytes) : u32x4{0, 0, 0, 0};
+    }
+  };
+  ask(begin);
+  for (int round = begin; round < end; ++round) {
+    u32x4* now = piece[round & 1];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int q = tid + i * kBlock, row = q >> 3;
+      if (kPieces % kBlock == 0 || q < kPieces) now[row * 8 + ((q & 7) ^ (row >> 1 & 7))] = as[i];
+    }
+    const u32x4 xn[2] = {xs[0], xs[1]};
+    ask(round + 1);
+    __syncthreads();                                     // (what is read below is written again behind the next one)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < kRankTiles; ++j) {
+        const int row = 16 * j + r;
+        sum[j] = Product<T>::add(now[row * 8 + ((4 * u + g) ^ (row >> 1 & 7))], xn[u], sum[j]);
+      }
+  }
+  if (t0 + r >= at.tokens) return;
+  float* to = p.h + ((int64_t(at.cut) * p.B + at.b) * p.n + t0 + r) * p.R + rank0 + 4 * g;
 #pragma unroll
   for (int j = 0; j < kRankTiles; ++j)
     if (j < tiles) *reinterpret_cast<f32x4*>(to + 16 * j) = sum[j];
@@ -130,21 +191,20 @@ template <typename T> struct Terms;
 template <> struct Terms<Bf16> { typedef __bf16 E; };
 template <> struct Terms<F16> { typedef _Float16 E; };
 
-constexpr int kRanksTogether = 64;       // of h in LDS
-
-template <typename T, int kTokenTiles> struct AdaptShared {
-  // 16-bit rows: of each 16 ranks [g][token][8], g = 0, 1 the first terms of ranks 8 g .., g = 2, 3 the second of ranks 8 (g - 2) ..; fp32: [g][token][4]
-  u32x4 h[kRanksTogether / 16][4][16 * kTokenTiles];
-  float factor[16 * kTokenTiles];
+// How h lies in LDS and meets B.  A set is the ranks of 16 bytes of four lanes, 32 of 16-bit rows and 16 of fp32 ones: one instruction (of fp32, four) for each
+// term.  Of 16 ranks in all (kPacked), both terms are one instruction of 32: g = 0, 1 the first terms of ranks 8 g .. 8 g + 7, g = 2, 3 the second ones of ranks 8 (g - 2) ..
+template <typename T, bool kPacked> struct Sets {
+  static constexpr int kTerms = sizeof(T) == 4 || kPacked ? 1 : 2, kRanks = sizeof(T) == 4 || kPacked ? 16 : 32;
 };
+// [set][term][g][token] 16 bytes; two sets are taken together.
+constexpr int adapt_lds_bytes(int ranks, int token_tiles, bool packed) { return (packed ? 16 : (ranks + 31) / 32 * 32) * 4 * 16 * token_tiles; }
 
-// Ranks rank0 .. rank0 + 63 of the tokens' h into LDS; behind a barrier on both sides.
-template <typename T, int kTokenTiles>
-__device__ __forceinline__ void adapt_place(const AdaptParams& p, const float* h, int64_t cut_stride, int tokens, int rank0, int rank, AdaptShared<T, kTokenTiles>& sh) {
-  const int q = threadIdx.x & 15;                        // four ranks: 4 q ..
-#pragma unroll
-  for (int it = 0; it < kTokenTiles; ++it) {
-    const int token = it * 16 + (threadIdx.x >> 4), at = rank0 + 4 * q;
+// Behind a barrier on both sides.  Sixteen lanes have a token.
+template <typename T, int kTokenTiles, bool kPacked>
+__device__ __forceinline__ void adapt_place(const AdaptParams& p, const float* h, int64_t cut_stride, int tokens, int rank, u32x4* to, float* factor) {
+  constexpr int kTokens = 16 * kTokenTiles;
+  const int q = threadIdx.x & 15;                        // four ranks of 64: 4 q ..
+  const auto load = [&](int token, int at) {
     f32x4 v{0, 0, 0, 0};
     if (token < tokens && at < rank) {
       const float* from = h + int64_t(token) * p.R + at;
@@ -153,46 +213,52 @@ __device__ __forceinline__ void adapt_place(const AdaptParams& p, const float* h
       for (int i = 0; i < 4; ++i)
         if (at + i >= rank) v[i] = 0.0f;
     }
-    if constexpr (sizeof(T) == 4) {
-      sh.h[q >> 2][q & 3][token] = __builtin_bit_cast(u32x4, v);
-    } else {
-      typedef typename Terms<T>::E E;
-      typedef E E4 __attribute__((ext_vector_type(4)));
-      E4 first, second;
-      const float up = sizeof(E) == 2 && __is_same(E, _Float16) ? sh.factor[token] : 1.0f;
+    return v;
+  };
+  f32x4 first[kTokenTiles];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float w = v[i] * up;
-        first[i] = E(w);
-        second[i] = E(w - float(first[i]));
-      }
-      uint64_t* to = reinterpret_cast<uint64_t*>(&sh.h[q >> 2][(q & 3) >> 1][token]) + (q & 1);
-      *to = __builtin_bit_cast(uint64_t, first);
-      reinterpret_cast<uint64_t*>(&sh.h[q >> 2][2 + ((q & 3) >> 1)][token])[q & 1] = __builtin_bit_cast(uint64_t, second);
-    }
-  }
-}
-
-// A power of two for each token that brings its largest h to 2^13 .. 2^14 (binary16 rows).
-template <int kTokenTiles>
-__device__ __forceinline__ void adapt_range(const AdaptParams& p, const float* h, int64_t cut_stride, int tokens, int rank, float* factor) {
-  const int q = threadIdx.x & 15;
+  for (int it = 0; it < kTokenTiles; ++it) first[it] = load(it * 16 + (threadIdx.x >> 4), 4 * q);
 #pragma unroll
   for (int it = 0; it < kTokenTiles; ++it) {
     const int token = it * 16 + (threadIdx.x >> 4);
-    uint32_t most = 0;                                   // magnitudes as whole numbers: NaN is the largest
-    for (int at = 4 * q; at < rank; at += 64) {
-      if (token >= tokens) break;
-      f32x4 v{0, 0, 0, 0};
-      for (int c = 0; c < p.cuts; ++c) v += *(const f32x4 __attribute__((address_space(1)))*)(h + int64_t(token) * p.R + at + c * cut_stride);
+    float up = 1.0f;
+    if constexpr (__is_same(T, F16)) {
+      // a power of two that brings the token's largest h to 2^13 .. 2^14 (magnitudes as whole numbers: NaN is the largest)
+      uint32_t most = 0;
+      for (int at = 4 * q; at < rank; at += 64) {
+        const f32x4 v = at < 64 ? first[it] : load(token, at);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (at + i < rank) most = max(most, as_u32(v[i]) & 0x7FFFFFFFu);
+        for (int i = 0; i < 4; ++i) most = max(most, as_u32(v[i]) & 0x7FFFFFFFu);
+      }
+#pragma unroll
+      for (int w = 1; w < 16; w *= 2) most = max(most, uint32_t(__shfl_xor(int(most), w, 16)));
+      const int e = int(most >> 23) - 127;               // 2^e <= largest
+      up = as_f32(uint32_t(127 + min(max(13 - e, -126), 100)) << 23);
+      if (q == 0) factor[token] = up;
     }
+    // (zeros up to a whole set)
+    constexpr int kRanks = Sets<T, kPacked>::kRanks, kTerms = Sets<T, kPacked>::kTerms;
+    for (int at = 4 * q; at < (rank + kRanks - 1) / kRanks * kRanks; at += 64) {
+      const f32x4 v = at < 64 ? first[it] : load(token, at);
+      u32x4* set = to + at / kRanks * (4 * kTerms * kTokens) + token;
+      const int within = at % kRanks;
+      if constexpr (sizeof(T) == 4) {
+        set[(within >> 2) * kTokens] = __builtin_bit_cast(u32x4, v);
+      } else {
+        typedef typename Terms<T>::E E;
+        typedef E E4 __attribute__((ext_vector_type(4)));
+        E4 term[2];
 #pragma unroll
-    for (int w = 1; w < 16; w *= 2) most = max(most, uint32_t(__shfl_xor(int(most), w, 16)));
-    const int e = int(most >> 23) - 127;                 // 2^e <= largest
-    if (q == 0) factor[token] = as_f32(uint32_t(127 + min(max(13 - e, -126), 100)) << 23);
+        for (int i = 0; i < 4; ++i) {
+          const float w = v[i] * up;
+          term[0][i] = E(w);
+          term[1][i] = E(w - float(term[0][i]));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          reinterpret_cast<uint64_t*>(set + ((kPacked ? 2 : 4) * i + (within >> 3)) * kTokens)[within >> 2 & 1] = __builtin_bit_cast(uint64_t, term[i]);
+      }
+    }
   }
 }
 
@@ -230,105 +296,152 @@ template <typename T> __device__ __forceinline__ u32x4 mask_ranks(u32x4 v, int f
   return v;
 }
 
-template <typename T, int kTokenTiles>
-__global__ __launch_bounds__(kBlock) void adapt_up_kernel(const AdaptParams p) {
+constexpr int kUpWaves = 2;
+
+// A workgroup has 16 or 64 tokens and every p.splits-th run of 256 channels of the result, 64 a wave.  Two sets of ranks at a time; B of the next ones, and then the next run's base, are asked
+// for before the present ones' products (in that order: loads come back in the order in which they were asked for, and B is nearer).
+template <typename T, int kTokenTiles, bool kPacked>
+__global__ __launch_bounds__(kBlock, kUpWaves) void adapt_up_kernel(const AdaptParams p) {
   constexpr int kBytes = ElemTraits<T>::kBytes, kLane = 16 / kBytes;       // kLane: a lane's channels in a row
-  constexpr int kSets = kLane / 4, kGroups = 4 / kSets;                      // instructions that make those, groups of them: 64 channels
-  __shared__ AdaptShared<T, kTokenTiles> sh;
-  const int wave = wave_id(), lane = lane_id(), r = lane & 15, g = lane >> 4;
+  constexpr int kRows = kLane / 4, kGroups = 4 / kRows;                      // instructions that make those, groups of them: 64 channels
+  constexpr int kTokens = 16 * kTokenTiles, kRanks = Sets<T, kPacked>::kRanks, kTerms = Sets<T, kPacked>::kTerms, kTogether = kPacked ? 1 : 2;
+  extern __shared__ u32x4 placed[];
+  __shared__ float factor[kTokens];
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, g = lane >> 4;
   uint32_t block = blockIdx.x;
-  const int chunk = int(block % uint32_t(p.chunks));
-  block /= uint32_t(p.chunks);
-  const uint32_t b = block / uint32_t(p.tiles);
-  const int tile = int(block - b * uint32_t(p.tiles)), t0 = tile * (16 * kTokenTiles), tokens = counted(p.count, b, p.n) - t0;
+  const int split = int(block % uint32_t(p.splits));
+  block /= uint32_t(p.splits);
+  const uint32_t b = block / uint32_t(p.up_tiles);
+  const int tile = int(block - b * uint32_t(p.up_tiles)), t0 = tile * kTokens;
   int rank;
   bool odd;
-  const int a = adapter_of(p, b, rank, odd);
-  if (tile == 0 && chunk == 0 && threadIdx.x == 0 && p.status)
+  const int a = adapter_of(p, b, rank, odd), tokens = counted(p.count, b, p.n) - t0;
+  if (tile == 0 && split == 0 && threadIdx.x == 0 && p.status)
     p.status[b] = odd || (p.count && as_global(p.count)[b] != counted(p.count, b, p.n)) ? kBadIndex : 0;
   if (tokens <= 0) return;
-  const int n0 = chunk * 256 + wave * 64;                // the wave's first channel
-  const bool any = n0 < p.N;
   const char* base = reinterpret_cast<const char*>(p.base.data) + (int64_t(b) * p.base.seq + t0 * p.base.token) * kBytes;
   char* out = reinterpret_cast<char*>(const_cast<void*>(p.out.data)) + (int64_t(b) * p.out.seq + t0 * p.out.token) * kBytes;
+  const int first = split * 256 + wave * 64, stride = p.splits * 256;      // the wave's first channel of each run
   if (rank == 0) {                                       // nothing to add
-    if (!p.copy || !any) return;
-    for (int t = r; t < min(tokens, 16 * kTokenTiles); t += 16)
+    if (!p.copy) return;
+    for (int n0 = first; n0 < p.N; n0 += stride)
+      for (int t = r; t < min(tokens, kTokens); t += 16)
 #pragma unroll
-      for (int q = 0; q < kGroups; ++q) {
-        const int c = n0 + (q * 4 + g) * kLane;
-        if (c < p.N) store_part<T>(out + (t * p.out.token + c) * kBytes, load_part<T>(base + (t * p.base.token + c) * kBytes, p.N - c), p.N - c);
-      }
+        for (int q = 0; q < kGroups; ++q) {
+          const int c = n0 + (q * 4 + g) * kLane;
+          if (c < p.N) store_part<T>(out + (t * p.out.token + c) * kBytes, load_part<T>(base + (t * p.base.token + c) * kBytes, p.N - c), p.N - c);
+        }
     return;
   }
-  const float* h = p.h + (int64_t(b) * p.n + t0) * p.R;
-  const int64_t cut_stride = p.B * p.n * int64_t(p.R);
-  u32x4 held[kTokenTiles][kGroups];                      // base
+  // A lane's place in the rows of base and out, and in those of B: row r of instruction j is a channel of the lane's run, so that its results lie in a row.  What is the
+  // same for all lanes is added in scalar registers.
+  const char* lane_base[kTokenTiles];                    // (lanes behind the last token read that one's)
 #pragma unroll
-  for (int t = 0; t < kTokenTiles; ++t)
-#pragma unroll
-    for (int q = 0; q < kGroups; ++q) {
-      const int c = n0 + (q * 4 + g) * kLane, token = 16 * t + r;
-      held[t][q] = c < p.N && token < tokens ? load_part<T>(base + (token * p.base.token + c) * kBytes, p.N - c) : u32x4{0, 0, 0, 0};
-    }
-  if constexpr (__is_same(T, F16)) {
-    adapt_range<kTokenTiles>(p, h, cut_stride, tokens, rank, sh.factor);
-    __syncthreads();
-  }
-  f32x4 sum[kTokenTiles][4];
-#pragma unroll
-  for (int t = 0; t < kTokenTiles; ++t)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum[t][j] = f32x4{0, 0, 0, 0};
-  // Row r of instruction j: channel of the lane's run 4 j' + i, so that a lane's results lie in a row.
+  for (int t = 0; t < kTokenTiles; ++t) lane_base[t] = base + (min(16 * t + r, tokens - 1) * p.base.token + g * kLane) * kBytes;
+  char* lane_out = out + (r * p.out.token + g * kLane) * kBytes;
   const char* rows = reinterpret_cast<const char*>(p.b) + int64_t(a) * p.N * p.R * kBytes;
-  for (int rank0 = 0; rank0 < rank; rank0 += kRanksTogether) {
-    if (rank0 > 0) __syncthreads();
-    adapt_place<T, kTokenTiles>(p, h, cut_stride, tokens, rank0, rank, sh);
-    __syncthreads();
-    if (!any) continue;
-    for (int s = 0; s < kRanksTogether / 16 && rank0 + 16 * s < rank; ++s) {
-      const int from = rank0 + 16 * s + (sizeof(T) == 4 ? 4 * g : 8 * (g & 1));
-      u32x4 w[4];
+  const int lane_rank = kLane * (kPacked && sizeof(T) == 2 ? g & 1 : g), lane_channel = (r >> 2) * kLane + (r & 3);
+  const uint32_t lane_row = uint32_t((lane_channel * p.R + lane_rank) * kBytes);
+  u32x4 next[kTokenTiles][kGroups];                      // base
+  const auto ask = [&](int n0) {
+#pragma unroll
+    for (int t = 0; t < kTokenTiles; ++t)
+#pragma unroll
+      for (int q = 0; q < kGroups; ++q) {
+        const char* at = lane_base[t] + n0 * kBytes + q * 64;
+        const int c = n0 + (q * 4 + g) * kLane;
+        if (n0 + 64 <= p.N) next[t][q] = load16_any(at);
+        else next[t][q] = c < p.N ? load_part<T>(at, p.N - c) : u32x4{0, 0, 0, 0};
+      }
+  };
+  u32x4 w[kTogether][4];
+  const auto ask_rows = [&](int n0, int rank0) {
+    if (n0 + 64 <= p.N && rank0 + kTogether * kRanks <= rank) {
+#pragma unroll
+      for (int s = 0; s < kTogether; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[s][j] = load16(rows + (int64_t(n0 + (j / kRows) * (4 * kLane) + 4 * (j % kRows)) * p.R + rank0 + s * kRanks) * kBytes + lane_row);
+      return;
+    }
+#pragma unroll
+    for (int s = 0; s < kTogether; ++s)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int c = n0 + (j / kSets) * (4 * kLane) + (r >> 2) * kLane + 4 * (j % kSets) + (r & 3);
-        w[j] = c < p.N && from < rank ? load16(rows + (int64_t(c) * p.R + from) * kBytes) : u32x4{0, 0, 0, 0};
-        if (from + kLane > rank) w[j] = mask_ranks<T>(w[j], from, rank);
+        const int c = n0 + (j / kRows) * (4 * kLane) + lane_channel + 4 * (j % kRows), from = rank0 + s * kRanks + lane_rank;
+        w[s][j] = c < p.N && from < rank ? load16(rows + (int64_t(c) * p.R + from) * kBytes) : u32x4{0, 0, 0, 0};
+      }
+  };
+  ask_rows(first, 0);
+  ask(first);
+  const float scale = p.scale ? as_global(p.scale)[a] : 1.0f;
+  adapt_place<T, kTokenTiles, kPacked>(p, p.h + (int64_t(b) * p.n + t0) * p.R, p.B * p.n * int64_t(p.R), tokens, rank, placed, factor);
+  __syncthreads();
+  for (int n0 = first; n0 < p.N; n0 += stride) {
+    u32x4 held[kTokenTiles][kGroups];
+    f32x4 sum[kTokenTiles][4];
+#pragma unroll
+    for (int t = 0; t < kTokenTiles; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[t][j] = f32x4{0, 0, 0, 0};
+    for (int rank0 = 0; rank0 < rank; rank0 += kTogether * kRanks) {
+      u32x4 v[kTogether][4];
+#pragma unroll
+      for (int s = 0; s < kTogether; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[s][j] = w[s][j];
+      if (rank0 + kTogether * kRanks > rank)             // (not where they are asked for: that would wait for them)
+#pragma unroll
+        for (int s = 0; s < kTogether; ++s)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[s][j] = mask_ranks<T>(v[s][j], rank0 + s * kRanks + lane_rank, rank);
+      const bool last = rank0 + kTogether * kRanks >= rank;
+      ask_rows(last ? n0 + stride : n0, last ? 0 : rank0 + kTogether * kRanks);
+      if (last) {
+#pragma unroll
+        for (int t = 0; t < kTokenTiles; ++t)
+#pragma unroll
+          for (int q = 0; q < kGroups; ++q) held[t][q] = next[t][q];
+        ask(n0 + stride);
       }
 #pragma unroll
-      for (int t = 0; t < kTokenTiles; ++t) {
-        const u32x4 hs = sh.h[s][g][16 * t + r];
+      for (int s = 0; s < kTogether; ++s) {
+        if (s > 0 && rank0 + s * kRanks >= rank) continue;
+        const u32x4* set = placed + (rank0 / kRanks + s) * (4 * kTerms * kTokens);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[t][j] = Product<T>::add(w[j], hs, sum[t][j]);
+        for (int e = 0; e < kTerms; ++e)
+#pragma unroll
+          for (int t = 0; t < kTokenTiles; ++t) {
+            const u32x4 hs = set[(e * 4 + g) * kTokens + 16 * t + r];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[t][j] = Product<T>::add(v[s][j], hs, sum[t][j]);
+          }
       }
     }
-  }
-  if (!any) return;
-  const float scale = p.scale ? as_global(p.scale)[a] : 1.0f;
 #pragma unroll
-  for (int t = 0; t < kTokenTiles; ++t) {
-    const int token = 16 * t + r;
-    if (token >= tokens) continue;
-    const float f = __is_same(T, F16) ? scale / sh.factor[token] : scale;
+    for (int t = 0; t < kTokenTiles; ++t) {
+      if (16 * t + r >= tokens) continue;
+      const float f = __is_same(T, F16) ? scale / factor[16 * t + r] : scale;
+      char* to = lane_out + (16 * t * p.out.token + n0) * kBytes;
 #pragma unroll
-    for (int q = 0; q < kGroups; ++q) {
-      const int c = n0 + (q * 4 + g) * kLane;
-      if (c >= p.N) continue;
-      u32x4 made;
-      if constexpr (sizeof(T) == 4) {
+      for (int q = 0; q < kGroups; ++q) {
+        u32x4 made;
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) made[i] = as_u32(fmaf(sum[t][q][i], f, as_f32(held[t][q][i])));
-      } else {
-        float v[8];
-        unpack<T>(make_uint4(held[t][q][0], held[t][q][1], held[t][q][2], held[t][q][3]), v);
+          for (int i = 0; i < 4; ++i) made[i] = as_u32(fmaf(sum[t][q][i], f, as_f32(held[t][q][i])));
+        } else {
+          float x[8];
+          unpack<T>(make_uint4(held[t][q][0], held[t][q][1], held[t][q][2], held[t][q][3]), x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaf(sum[t][2 * q + (i >> 2)][i & 3], f, v[i]);
-        Eight<T> e;
-        e.set(v);
-        made = e.w;
+          for (int i = 0; i < 8; ++i) x[i] = fmaf(sum[t][2 * q + (i >> 2)][i & 3], f, x[i]);
+          Eight<T> e;
+          e.set(x);
+          made = e.w;
+        }
+        const int c = n0 + (q * 4 + g) * kLane;
+        if (n0 + 64 <= p.N) store16_any(to + q * 64, made);
+        else if (c < p.N) store_part<T>(to + q * 64, made, p.N - c);
       }
-      store_part<T>(out + (token * p.out.token + c) * kBytes, made, p.N - c);
     }
   }
 }

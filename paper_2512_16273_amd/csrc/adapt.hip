@@ -8,33 +8,53 @@
 
 namespace {
 
-// Workgroups' tokens and how many cuts x's channels are in: twice as many workgroups as compute units, of 512 channels or more.
-struct Plan { int token_tiles, rank_tiles, tiles, chunks, cuts; };
-Plan plan_down(int64_t B, int32_t n, int32_t K, int32_t R) {
+// How a call is cut: tokens of a workgroup in both launches (in sixteens), ranks of one in the first (in sixteens), how many cuts x's channels are in, and how
+// many workgroups share the channels of the result.
+//   Cuts fill the GPU twice, but every workgroup of the second launch adds their sums up: 512 channels each at least, and fewer of high ranks (2 x 1000 tokens of rank 128, 4
+//   / 8 cuts 35.6 / 37.0 us; 500 of rank 256, 1 / 2 / 8 cuts 53 / 39 / 43).
+//   The second launch takes 64 tokens where that makes workgroups for half of the compute units at least (4 x 2001 tokens of rank 64, 32 / 64: 96 / 89 us; 16 x 85 of rank 16 19.8 /
+//   25.6), and the channels in as many shares as there is room for at once (2 x 1000 fp32 tokens, two workgroups fit a compute unit, for 2 / 3 / 4 of them 38 / 46 / 44 us; 16 x 85
+//   bfloat16 ones, three fit, 21.1 / 19.8 / 19.8; 256 x 9, five fit, for 4 / 5 / 8 25.5 / 24.6 / 25.7).
+struct Plan { int token_tiles, rank_tiles, tiles, chunks, cuts, up_token_tiles, up_tiles, splits; };
+Plan plan_adapt(tslt_dtype dt, int64_t B, int32_t n, int32_t K, int32_t N, int32_t R) {
   Plan p;
+  const int64_t cus = tslt::compute_units(), sequences = std::min<int64_t>(B, 1 << 20);
+  const auto between = [](int64_t least, int64_t x, int64_t most) { return int(std::max(least, std::min(x, most))); };
   p.token_tiles = n > 16 ? 4 : 1;
   p.rank_tiles = R == 16 ? 1 : R == 32 ? 2 : 4;
   p.tiles = (n + 16 * p.token_tiles - 1) / (16 * p.token_tiles);
   p.chunks = (R / 16 + p.rank_tiles - 1) / p.rank_tiles;
-  const int64_t blocks = std::min<int64_t>(B, 1 << 20) * p.tiles * p.chunks, most = std::min<int64_t>(8, K / 512);
-  p.cuts = int(std::max<int64_t>(1, std::min<int64_t>(most, 2 * int64_t(tslt::compute_units()) / blocks)));
+  p.cuts = between(1, std::min<int64_t>(512 / R, K / 512), 8);
+  p.cuts = between(1, 2 * cus / (sequences * p.tiles * p.chunks), p.cuts);
+  p.up_token_tiles = n <= 16 ? 1 : dt == TSLT_F32 || sequences * ((n + 63) / 64) < cus / 2 ? 2 : 4;
+  p.up_tiles = (n + 16 * p.up_token_tiles - 1) / (16 * p.up_token_tiles);
+  const int64_t fill = (n <= 16 ? 5 : p.up_token_tiles == 2 && dt != TSLT_F32 ? 3 : 2) * cus;
+  p.splits = between(1, fill / (sequences * p.up_tiles), (int64_t(N) + 255) / 256);
   return p;
 }
-
-template <typename T, int kTokenTiles> void launch_down(const tslt::AdaptParams& p, int rank_tiles, unsigned blocks, hipStream_t s) {
-  if (rank_tiles == 1) hipLaunchKernelGGL((tslt::adapt_down_kernel<T, kTokenTiles, 1>), dim3(blocks), dim3(tslt::kBlock), 0, s, p);
-  else if (rank_tiles == 2) hipLaunchKernelGGL((tslt::adapt_down_kernel<T, kTokenTiles, 2>), dim3(blocks), dim3(tslt::kBlock), 0, s, p);
-  else hipLaunchKernelGGL((tslt::adapt_down_kernel<T, kTokenTiles, 4>), dim3(blocks), dim3(tslt::kBlock), 0, s, p);
+template <typename T, int kRankTiles> void launch_down(const tslt::AdaptParams& p, int token_tiles, hipStream_t s) {
+  const dim3 blocks(unsigned(p.B * p.tiles * p.chunks * p.cuts)), threads(tslt::kBlock);
+  if (token_tiles == 1) hipLaunchKernelGGL((tslt::adapt_down_few_kernel<T, kRankTiles>), blocks, threads, 0, s, p);
+  else hipLaunchKernelGGL((tslt::adapt_down_many_kernel<T, kRankTiles>), blocks, threads, 0, s, p);
 }
-template <typename T> void launch_adapt(tslt::AdaptParams p, const Plan& plan, hipStream_t s) {
-  p.tiles = plan.tiles; p.chunks = plan.chunks; p.cuts = plan.cuts;
-  const unsigned down = unsigned(p.B * p.tiles * p.chunks * p.cuts);
-  if (plan.token_tiles == 1) launch_down<T, 1>(p, plan.rank_tiles, down, s);
-  else launch_down<T, 4>(p, plan.rank_tiles, down, s);
-  p.chunks = (p.N + 255) / 256;
-  const unsigned up = unsigned(p.B * p.tiles * p.chunks);
-  if (plan.token_tiles == 1) hipLaunchKernelGGL((tslt::adapt_up_kernel<T, 1>), dim3(up), dim3(tslt::kBlock), 0, s, p);
-  else hipLaunchKernelGGL((tslt::adapt_up_kernel<T, 4>), dim3(up), dim3(tslt::kBlock), 0, s, p);
+template <typename T, int kTokenTiles, bool kPacked> hipError_t launch_up(const tslt::AdaptParams& p, hipStream_t s) {
+  const int lds = tslt::adapt_lds_bytes(p.R, kTokenTiles, kPacked);         // (64 KB of 64 tokens and 256 ranks)
+  if (lds > 48 * 1024) {
+    const hipError_t e = tslt::allow_dynamic_lds<&tslt::adapt_up_kernel<T, kTokenTiles, kPacked>>(64 * 1024);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((tslt::adapt_up_kernel<T, kTokenTiles, kPacked>), dim3(unsigned(p.B * p.up_tiles * p.splits)), dim3(tslt::kBlock), lds, s, p);
+  return hipSuccess;
+}
+template <typename T> hipError_t launch_adapt(tslt::AdaptParams p, const Plan& plan, hipStream_t s) {
+  p.tiles = plan.tiles; p.chunks = plan.chunks; p.cuts = plan.cuts; p.splits = plan.splits; p.up_tiles = plan.up_tiles;
+  if (plan.rank_tiles == 1) launch_down<T, 1>(p, plan.token_tiles, s);
+  else if (plan.rank_tiles == 2) launch_down<T, 2>(p, plan.token_tiles, s);
+  else launch_down<T, 4>(p, plan.token_tiles, s);
+  if (plan.up_token_tiles == 1) return p.R == 16 ? launch_up<T, 1, true>(p, s) : launch_up<T, 1, false>(p, s);
+  if constexpr (sizeof(T) == 2)
+    if (plan.up_token_tiles == 4) return p.R == 16 ? launch_up<T, 4, true>(p, s) : launch_up<T, 4, false>(p, s);
+  return p.R == 16 ? launch_up<T, 2, true>(p, s) : launch_up<T, 2, false>(p, s);
 }
 bool sizes_fit(int64_t B, int32_t n, int32_t K, int32_t N, int32_t R) {
   return B >= 1 && n >= 1 && K >= 1 && N >= 1 && R >= 16 && R <= TSLT_MAX_ADAPTER_RANK && R % 16 == 0 && B <= 0x7FFFFFFF / n;
@@ -46,7 +66,7 @@ extern "C" {
 
 size_t tslt_adapt_workspace_bytes(int64_t B, int32_t n, int32_t K, int32_t N, int32_t R) {
   if (!sizes_fit(B, n, K, N, R)) return 0;
-  return (size_t(plan_down(B, n, K, R).cuts) * size_t(B) * n * R * 4 + 255) / 256 * 256;
+  return (size_t(plan_adapt(TSLT_F32, B, n, K, N, R).cuts) * size_t(B) * n * R * 4 + 255) / 256 * 256;
 }
 
 int tslt_adapt(const tslt_rows* x, int32_t K, const tslt_rows* base, const tslt_rows* out, int32_t N, tslt_dtype dt, int64_t B, int32_t n,
@@ -70,20 +90,19 @@ int tslt_adapt(const tslt_rows* x, int32_t K, const tslt_rows* base, const tslt_
     return fail(TSLT_ERR_INVALID_ARG, "%s: rows that are added to in place must have the same strides", who);
   if (!a || !b || !adapter) return fail(TSLT_ERR_INVALID_ARG, "%s: null pointer", who);
   if (!aligned(a, 16) || !aligned(b, 16)) return fail(TSLT_ERR_INVALID_ARG, "%s: adapters not aligned to 16 bytes", who);
-  const Plan plan = plan_down(B, n, K, R);
+  const Plan plan = plan_adapt(dt, B, n, K, N, R);
   const size_t need = tslt_adapt_workspace_bytes(B, n, K, N, R);
   if (!ws || !aligned(ws, 256) || ws_bytes < need)
     return fail(TSLT_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu are needed, 256-byte aligned", who, ws ? ws_bytes : size_t(0), need);
   int code;
-  if (!grid_fits(who, B * plan.tiles * std::max<int64_t>(int64_t(plan.chunks) * plan.cuts, (int64_t(N) + 255) / 256), code)) return code;
+  if (!grid_fits(who, B * std::max<int64_t>(int64_t(plan.tiles) * plan.chunks * plan.cuts, int64_t(plan.up_tiles) * plan.splits), code)) return code;
   tslt::AdaptParams p{};
   p.x = view(&rx); p.base = view(&rb); p.out = view(&ro);
   p.K = K; p.N = N; p.R = R; p.n = n; p.B = B; p.n_adapters = n_adapters; p.a = a; p.b = b; p.adapter = adapter; p.rank = rank; p.count = count;
   p.scale = scale; p.status = status; p.h = reinterpret_cast<float*>(ws); p.copy = rb.data != ro.data;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (dt == TSLT_F32) launch_adapt<float>(p, plan, s);
-  else if (dt == TSLT_BF16) launch_adapt<tslt::Bf16>(p, plan, s);
-  else launch_adapt<tslt::F16>(p, plan, s);
+  const hipError_t e = dt == TSLT_F32 ? launch_adapt<float>(p, plan, s) : dt == TSLT_BF16 ? launch_adapt<tslt::Bf16>(p, plan, s) : launch_adapt<tslt::F16>(p, plan, s);
+  if (e != hipSuccess) return tslt::hip_fail(e, "hipFuncSetAttribute");
   return launched("tslt_adapt launch");
 }
 
