@@ -287,18 +287,18 @@ __global__ __launch_bounds__(kBlock) void rotate_backward_kernel(const RotatePar
   }
 }
 
-// The workgroups' shares together: 32 of the 2 D channels to a workgroup, eight of its lanes to each.
+// The workgroups' shares together: eight of the 2 D channels to a workgroup, 32 of its lanes to each.
 template <int D> __global__ __launch_bounds__(kBlock) void rotate_weights_kernel(const RotateParams p) {
-  __shared__ double share[8][32];
-  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, channel = blockIdx.x * 32 + lane;
+  __shared__ double share[32][8];
+  const int lane = threadIdx.x & 7, group = threadIdx.x >> 3, channel = blockIdx.x * 8 + lane;
   double all = 0.0;
 #pragma unroll 8
-  for (int i = group; i < p.parts; i += 8) all += as_global(p.part)[int64_t(i) * (2 * D) + channel];
+  for (int i = group; i < p.parts; i += 32) all += as_global(p.part)[int64_t(i) * (2 * D) + channel];
   share[group][lane] = all;
   __syncthreads();
   if (group > 0) return;
 #pragma unroll
-  for (int g = 1; g < 8; ++g) all += share[g][lane];
+  for (int g = 1; g < 32; ++g) all += share[g][lane];
   float* out = channel < D ? p.out_q_weight : p.out_k_weight;
   if (out) out[channel < D ? channel : channel - D] = float(all);
 }

@@ -9,19 +9,29 @@
 
 namespace {
 
-constexpr int kTokensEach = 4;
+// Tokens of a workgroup: more of them have more angles to compute at once, fewer make more workgroups (64 x 21 tokens of 40 heads of 128, four / two 11.2 / 9.6 us).
+int tokens_each(int64_t tokens) { return tokens <= int64_t(tslt::compute_units()) ? 1 : tokens <= 16 * int64_t(tslt::compute_units()) ? 2 : 4; }
+// Backwards, where each goes on to others and keeps its share of the weights' gradients, three fit a compute unit (8 x 2048 tokens, 2 / 3 / 6 of them 130 / 108 / 115 us).
+int tokens_back(int64_t tokens) { return tokens <= 4 * int64_t(tslt::compute_units()) ? 1 : 4; }
+int64_t backward_blocks(int64_t tokens) {
+  const int each = tokens_back(tokens);
+  return std::min<int64_t>((tokens + each - 1) / each, 3 * int64_t(tslt::compute_units()));
+}
 
-// Calls of few tokens: one to a workgroup.
-bool few(int64_t tokens) { return tokens <= int64_t(tslt::compute_units()); }
-int64_t backward_blocks(int64_t tokens) { return std::min<int64_t>((tokens + kTokensEach - 1) / kTokensEach, 2 * int64_t(tslt::compute_units())); }
-
+template <typename T, int D, int kTokens> void launch_rotate_of(const tslt::RotateParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((tslt::rotate_kernel<T, D, kTokens>), dim3(unsigned((p.tokens + kTokens - 1) / kTokens)), dim3(tslt::kBlock), 0, s, p);
+}
 template <typename T, int D> void launch_rotate(const tslt::RotateParams& p, hipStream_t s) {
-  if (few(p.tokens)) hipLaunchKernelGGL((tslt::rotate_kernel<T, D, 1>), dim3(unsigned(p.tokens)), dim3(tslt::kBlock), 0, s, p);
-  else hipLaunchKernelGGL((tslt::rotate_kernel<T, D, kTokensEach>), dim3(unsigned((p.tokens + kTokensEach - 1) / kTokensEach)), dim3(tslt::kBlock), 0, s, p);
+  const int each = tokens_each(p.tokens);
+  each == 1 ? launch_rotate_of<T, D, 1>(p, s) : each == 2 ? launch_rotate_of<T, D, 2>(p, s) : launch_rotate_of<T, D, 4>(p, s);
+}
+template <int D> void launch_rotate_weights(const tslt::RotateParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((tslt::rotate_weights_kernel<D>), dim3(2 * D / 8), dim3(tslt::kBlock), 0, s, p);
 }
 template <typename T, int D> void launch_rotate_backward(const tslt::RotateParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((tslt::rotate_backward_kernel<T, D, kTokensEach>), dim3(unsigned(p.parts)), dim3(tslt::kBlock), 0, s, p);
-  if (p.part) hipLaunchKernelGGL((tslt::rotate_weights_kernel<D>), dim3(2 * D / 32), dim3(tslt::kBlock), 0, s, p);
+  if (tokens_back(p.tokens) == 1) hipLaunchKernelGGL((tslt::rotate_backward_kernel<T, D, 1>), dim3(unsigned(p.parts)), dim3(tslt::kBlock), 0, s, p);
+  else hipLaunchKernelGGL((tslt::rotate_backward_kernel<T, D, 4>), dim3(unsigned(p.parts)), dim3(tslt::kBlock), 0, s, p);
+  if (p.part) launch_rotate_weights<D>(p, s);
 }
 
 int check_rotation(const char* who, tslt_dtype dt, int64_t B, int32_t n, int32_t heads_q, int32_t heads, bool keys, int32_t D, const tslt_rotation* how) {
@@ -129,9 +139,7 @@ int tslt_rotate_backward(const tslt_rows* grad_q, const tslt_rows* grad_k, const
     }
     TSLT_BY_TYPE_AND_D(launch_rotate_backward, dt, head_dim, p, s);
   } else if (weights) {                    // no sequences: gradients of nothing
-    const unsigned blocks = unsigned(2 * head_dim / 32);
-    const auto join = head_dim == 64 ? tslt::rotate_weights_kernel<64> : head_dim == 128 ? tslt::rotate_weights_kernel<128> : tslt::rotate_weights_kernel<256>;
-    hipLaunchKernelGGL(join, dim3(blocks), dim3(tslt::kBlock), 0, s, p);
+    head_dim == 64 ? launch_rotate_weights<64>(p, s) : head_dim == 128 ? launch_rotate_weights<128>(p, s) : launch_rotate_weights<256>(p, s);
   }
   return launched("tslt_rotate_backward launch");
 }
