@@ -56,8 +56,9 @@ template <typename T> hipError_t launch_adapt(tslt::AdaptParams p, const Plan& p
     if (plan.up_token_tiles == 4) return p.R == 16 ? launch_up<T, 4, true>(p, s) : launch_up<T, 4, false>(p, s);
   return p.R == 16 ? launch_up<T, 2, true>(p, s) : launch_up<T, 2, false>(p, s);
 }
+constexpr int32_t kMostChannels = 1 << 28;                                 // (a row's bytes are counted in 32 bits)
 bool sizes_fit(int64_t B, int32_t n, int32_t K, int32_t N, int32_t R) {
-  return B >= 1 && n >= 1 && K >= 1 && N >= 1 && R >= 16 && R <= TSLT_MAX_ADAPTER_RANK && R % 16 == 0 && B <= 0x7FFFFFFF / n;
+  return B >= 1 && n >= 1 && K >= 1 && N >= 1 && K <= kMostChannels && N <= kMostChannels && R >= 16 && R <= TSLT_MAX_ADAPTER_RANK && R % 16 == 0 && B <= 0x7FFFFFFF / n;
 }
 
 }  // namespace
@@ -79,6 +80,7 @@ int tslt_adapt(const tslt_rows* x, int32_t K, const tslt_rows* base, const tslt_
   if (R < 16 || R > TSLT_MAX_ADAPTER_RANK || R % 16)
     return fail(TSLT_ERR_UNSUPPORTED, "%s: R must be a multiple of 16 up to %d (got %d)", who, TSLT_MAX_ADAPTER_RANK, int(R));
   if (K % (16 / elem_bytes(dt))) return fail(TSLT_ERR_UNSUPPORTED, "%s: rows of K=%d elements are no multiple of 16 bytes", who, int(K));
+  if (K > kMostChannels || N > kMostChannels) return fail(TSLT_ERR_UNSUPPORTED, "%s: rows of K=%d, N=%d elements, %d at most", who, int(K), int(N), int(kMostChannels));
   if (n_adapters > 0x7FFFFFFF || B > 0x7FFFFFFF / n) return fail(TSLT_ERR_UNSUPPORTED, "%s: adapters and tokens must fit 31 bits", who);
   if (B == 0) return TSLT_OK;
   tslt_rows rx = x ? *x : tslt_rows{}, rb = base ? *base : tslt_rows{}, ro = out ? *out : tslt_rows{};

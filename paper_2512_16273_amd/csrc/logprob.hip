@@ -27,7 +27,7 @@ int check_logits(const char* who, tslt_dtype dt, int64_t B, int32_t n, int64_t V
   if (B < 0 || n < 1 || V < 1) return fail(TSLT_ERR_INVALID_ARG, "%s: bad shape B=%lld n=%d V=%lld", who, (long long)B, int(n), (long long)V);
   if (V > 0x7FFFFFFF || V * elem_bytes(dt) >= (int64_t(1) << 32)) return fail(TSLT_ERR_UNSUPPORTED, "%s: a row must be shorter than 4 GiB", who);
   if (B > 0x7FFFFFFF / n) return fail(TSLT_ERR_UNSUPPORTED, "%s: the rows of a call must fit 31 bits", who);
-  if (!(temperature > 0.0f) || !(1.0f / temperature > 0.0f) || !(1.0f / temperature < 3.0e38f))
+  if (!(temperature > 0.0f) || !(1.0f / temperature > 0.0f) || !(1.0f / temperature < 1.0e38f))
     return fail(TSLT_ERR_INVALID_ARG, "%s: temperature must be > 0", who);
   if (top < 0 || top > TSLT_MAX_TOP) return fail(TSLT_ERR_UNSUPPORTED, "%s: top must be 0 to %d (got %d)", who, TSLT_MAX_TOP, int(top));
   return TSLT_OK;

@@ -80,7 +80,7 @@ def test_logprob(lib):
         return lib.tslt_logprob(z, dt, B, n, V, n * V, V, T, index, m, None, tokens, top, None, None, None, idx, logp, None, ws, ws_bytes, None)
     assert call(dt=9) == -1 and call(B=-1) == -1 and call(n=0) == -1 and call(V=0) == -1 and call(z=None) == -1
     assert call(V=1 << 31) == -2 and call(dt=0, V=1 << 30) == -2 and call(B=1 << 31) == -2 and call(index=FAKE, m=1 << 30, B=4) == -2
-    for T in (0.0, -1.0, NAN, INF, 1e-39):
+    for T in (0.0, -1.0, NAN, INF, 1e-39, 5e-39, 9e-39):
         assert call(T=T) == -1 and "temperature" in message(lib)
     assert call(m=2) == -1 and call(index=FAKE, m=0) == -1 and "index" in message(lib)
     assert call(top=33) == -2 and call(top=-1) == -2 and call(top=4) == -1 and call(top=4, idx=FAKE) == -1
@@ -122,7 +122,7 @@ def test_adapt(lib):
     for R in (0, 8, 24, 272, -16):
         assert call(R=R) == -2 and "R must be" in message(lib)
     assert call(K=60) == -2 and call(K=6, dt=0) == -2 and call(K=4) == -2 and "16 bytes" in message(lib)
-    assert call(B=1 << 31) == -2 and call(adapters=1 << 31) == -2 and call(N=1 << 30, B=1 << 20) == -2
+    assert call(B=1 << 31) == -2 and call(adapters=1 << 31) == -2 and call(N=1 << 29) == -2 and call(K=1 << 29) == -2
     assert call(x=None) == -1 and call(base=rows(data=None)) == -1 and call(out=rows(FAKE * 3 + 1)) == -1 and call(x=rows(token=12)) == -1
     assert call(a=None) == -1 and call(b=None) == -1 and call(adapter=None) == -1 and call(a=FAKE + 8) == -1 and call(b=FAKE + 2) == -1
     assert call(out=rows(FAKE * 2, token=513)) == -1 and "in place" in message(lib)
