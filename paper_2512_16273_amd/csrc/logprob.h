@@ -20,7 +20,7 @@ namespace tslt {
 
 constexpr int kMaxTop = 32;
 constexpr int kListRoom = 128;           // records of a wave's list
-constexpr int kLogprobWaves = 4, kLogprobThreads = 64 * kLogprobWaves;
+constexpr int kLogprobWaves = 4;         // of a workgroup; short rows have one
 constexpr int kPartHead = 4 + kLogprobWaves / 2, kPartWords = kPartHead + 64;
 
 struct LogprobParams {
@@ -189,27 +189,27 @@ struct RowWave {
   }
 };
 
-struct LogprobShared {
-  uint64_t list[kLogprobWaves][kListRoom];
-  double rho[kLogprobWaves], S[kLogprobWaves], E[kLogprobWaves];
-  float c[kLogprobWaves];
-  float largest[kLogprobThreads];
-  int n[kLogprobWaves];
+template <int W> struct LogprobShared {
+  uint64_t list[W][kListRoom];
+  double rho[W], S[W], E[W];
+  float c[W];
+  float largest[64 * W];
+  int n[W];
   uint64_t least;
   int told, mine;
 };
 
 // The waves' lists put together and cut down to `top` records, or to 64 at most if they need not be the least; the first wave's list then has them.  All threads.
-template <bool kLast> __device__ __forceinline__ void put_together(List& l, int top, LogprobShared& sh) {
+template <bool kLast, int W> __device__ __forceinline__ void put_together(List& l, int top, LogprobShared<W>& sh) {
   const int wave = wave_id(), lane = lane_id();
   if (l.n > 64) cut(l, top);
   if (lane == 0) sh.n[wave] = l.n;
   __syncthreads();
   if (wave == 0) {
-    uint64_t r[kLogprobWaves];
+    uint64_t r[W];
     int total = 0;
 #pragma unroll
-    for (int w = 0; w < kLogprobWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const int n = sh.n[w];
       r[w] = lane < n ? sh.list[w][lane] : 0;
       total += n;
@@ -286,8 +286,8 @@ template <typename T> __device__ __forceinline__ void take(RowWave& w, const uin
 constexpr int kAhead = 4;                // vectors of a lane that are asked for together
 
 // A workgroup's share of a row: its waves' sums in LDS, and the likeliest in the first wave's list.
-template <typename T> __device__ void row_share(const void* row, const LogprobParams& p, int slice, LogprobShared& sh, List& list) {
-  constexpr int E = ElemTraits<T>::kPerVec, kRound = kLogprobThreads * kAhead;
+template <typename T, int W> __device__ void row_share(const void* row, const LogprobParams& p, int slice, LogprobShared<W>& sh, List& list) {
+  constexpr int E = ElemTraits<T>::kPerVec, kThreads = 64 * W, kRound = kThreads * kAhead;
   const int wave = wave_id(), lane = lane_id(), top = p.top;
   const RowSplit rs = split_row<T>(row, p.V);
   const int64_t each = (rs.nvec + p.slices - 1) / p.slices, begin = min(each * slice, rs.nvec), end = min(begin + each, rs.nvec);
@@ -307,7 +307,7 @@ template <typename T> __device__ void row_share(const void* row, const LogprobPa
   uint4 x[kAhead];
   int64_t v = begin + wave * 64 + lane;
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u) x[u] = row_vector<T>(rs.body, v + u * kLogprobThreads, end);
+  for (int u = 0; u < kAhead; ++u) x[u] = row_vector<T>(rs.body, v + u * kThreads, end);
   {
     float most = -INFINITY;
 #pragma unroll
@@ -323,9 +323,9 @@ template <typename T> __device__ void row_share(const void* row, const LogprobPa
     } else {
       sh.largest[threadIdx.x] = most;
       __syncthreads();
-      float largest[kLogprobWaves];
+      float largest[W];
 #pragma unroll
-      for (int i = 0; i < kLogprobWaves; ++i) largest[i] = sh.largest[64 * i + lane];
+      for (int i = 0; i < W; ++i) largest[i] = sh.largest[64 * i + lane];
       w.list.above = fmaxf(w.list.above, reached_by(largest, top));
     }
   }
@@ -333,13 +333,13 @@ template <typename T> __device__ void row_share(const void* row, const LogprobPa
   for (int64_t v0 = begin; v0 < end; v0 += kRound, v += kRound) {
     uint4 next[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) next[u] = row_vector<T>(rs.body, v + kRound + u * kLogprobThreads, end);
+    for (int u = 0; u < kAhead; ++u) next[u] = row_vector<T>(rs.body, v + kRound + u * kThreads, end);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) take<T>(w, x[u], rs.head + (v + u * kLogprobThreads) * E, p.k2, top);
+    for (int u = 0; u < kAhead; ++u) take<T>(w, x[u], rs.head + (v + u * kThreads) * E, p.k2, top);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) x[u] = next[u];
     if (top > 0 && ++round == together && v0 + 2 * kRound < end) {
-      put_together<false>(w.list, top, sh);
+      put_together<false, W>(w.list, top, sh);
       together = 4 * round;
     }
   }
@@ -353,15 +353,15 @@ template <typename T> __device__ void row_share(const void* row, const LogprobPa
     sh.c[wave] = w.c;
   }
   list = w.list;
-  if (top > 0) put_together<true>(list, top, sh);
+  if (top > 0) put_together<true, W>(list, top, sh);
   else __syncthreads();
 }
 
 // The first wave: the sums of all.
-__device__ __forceinline__ RowSums all_waves(const LogprobShared& sh, double k2) {
-  const int w = min(lane_id(), kLogprobWaves - 1);
+template <int W> __device__ __forceinline__ RowSums all_waves(const LogprobShared<W>& sh, double k2) {
+  const int w = min(lane_id(), W - 1);
   RowSums mine{sh.c[w], sh.rho[w], sh.S[w], sh.E[w]};
-  if (lane_id() >= kLogprobWaves) mine = RowSums{-INFINITY, 0.0, 0.0, 0.0};
+  if (lane_id() >= W) mine = RowSums{-INFINITY, 0.0, 0.0, 0.0};
   return join(mine, k2);
 }
 
@@ -413,9 +413,9 @@ __device__ __forceinline__ void refuse(const LogprobParams& p, int64_t entry, in
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(const LogprobParams p) {
-  __shared__ LogprobShared sh;
+template <typename T, int W>
+__global__ __launch_bounds__(64 * W) void logprob_kernel(const LogprobParams p) {
+  __shared__ LogprobShared<W> sh;
   const int tid = threadIdx.x, wave = wave_id(), lane = lane_id();
   const uint32_t entry = blockIdx.x / uint32_t(p.slices);
   const int slice = int(blockIdx.x - entry * uint32_t(p.slices));
@@ -438,61 +438,63 @@ __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(const LogprobP
   const void* row = reinterpret_cast<const char*>(p.logits) + (int64_t(b) * p.seq_stride + at * p.row_stride) * ElemTraits<T>::kBytes;
   const float z = token >= 0 && token < p.V ? load_elem<T>(row, token) : 0.0f;
   List list;
-  row_share<T>(row, p, slice, sh, list);
-  if (p.slices == 1) {
+  row_share<T, W>(row, p, slice, sh, list);
+  if (W == 1 || p.slices == 1) {
     if (wave == 0) finish(p, entry, token, z, all_waves(sh, p.k2), odd, list);
     return;
   }
-  uint64_t* words = p.words + int64_t(entry) * p.slices;
-  uint64_t* part = p.part + int64_t(entry) * p.slices * kPartWords;
-  if (wave == 0) {
-    const RowSums sums = all_waves(sh, p.k2);
-    uint64_t* own = part + slice * kPartWords;
-    if (p.top > 0 && lane < list.n) store_through(own + kPartHead + lane, list.at[lane]);
-    if (lane < kLogprobWaves / 2) store_through(own + 4 + lane, uint64_t(as_u32(sh.c[2 * lane + 1])) << 32 | as_u32(sh.c[2 * lane]));
-    if (lane == 0) {
-      store_through(own, as_u32(sums.c));
-      store_through(own + 1, __builtin_bit_cast(uint64_t, sums.S));
-      store_through(own + 2, __builtin_bit_cast(uint64_t, sums.E));
-      store_through(own + 3, uint64_t(list.n));
-    }
-  }
-  if (!all_arrived(words, slice, p.slices, p.tag, sh.told)) return;
-  if (wave == 0) {
-    const bool mine = claimed(words, p.slices, p.tag);
-    if (lane == 0) sh.mine = mine;
-  }
-  __syncthreads();
-  if (!sh.mine) return;
-  // a lane has a slice's sums
-  const uint64_t* from = part + min(lane, p.slices - 1) * kPartWords;
-  uint64_t head[kPartHead];
-#pragma unroll
-  for (int i = 0; i < kPartHead; ++i) head[i] = i < 3 || p.top > 0 ? load_through(from + i) : 0;
-  RowSums got{as_f32(uint32_t(head[0])), 0.0, __builtin_bit_cast(double, head[1]), __builtin_bit_cast(double, head[2])};
-  if (lane >= p.slices) got = RowSums{-INFINITY, 0.0, 0.0, 0.0};
-  if (p.top > 0) {
-    float largest[kLogprobWaves];
-#pragma unroll
-    for (int i = 0; i < kLogprobWaves; ++i) largest[i] = lane < p.slices ? as_f32(uint32_t(head[4 + i / 2] >> (32 * (i & 1)))) : -INFINITY;
-    const float above = reached_by(largest, p.top);
-    const int length = lane < p.slices ? int(head[3]) : 0;
-    list = List{sh.list[wave], 0, -INFINITY, 0};
-    constexpr int kTogether = 8;
-    for (int s0 = wave; s0 < p.slices; s0 += kLogprobWaves * kTogether) {
-      uint64_t r[kTogether];
-#pragma unroll
-      for (int u = 0; u < kTogether; ++u) {
-        const int s = min(s0 + u * kLogprobWaves, 63);
-        r[u] = lane < __builtin_amdgcn_readlane(length, s) ? load_through(part + s * kPartWords + kPartHead + lane) : 0;
+  if constexpr (W == kLogprobWaves) {
+    uint64_t* words = p.words + int64_t(entry) * p.slices;
+    uint64_t* part = p.part + int64_t(entry) * p.slices * kPartWords;
+    if (wave == 0) {
+      const RowSums sums = all_waves(sh, p.k2);
+      uint64_t* own = part + slice * kPartWords;
+      if (p.top > 0 && lane < list.n) store_through(own + kPartHead + lane, list.at[lane]);
+      if (lane < kLogprobWaves / 2) store_through(own + 4 + lane, uint64_t(as_u32(sh.c[2 * lane + 1])) << 32 | as_u32(sh.c[2 * lane]));
+      if (lane == 0) {
+        store_through(own, as_u32(sums.c));
+        store_through(own + 1, __builtin_bit_cast(uint64_t, sums.S));
+        store_through(own + 2, __builtin_bit_cast(uint64_t, sums.E));
+        store_through(own + 3, uint64_t(list.n));
       }
-#pragma unroll
-      for (int u = 0; u < kTogether; ++u)
-        offer(list, s0 + u * kLogprobWaves < p.slices && r[u] != 0 && cand_value(r[u]) > above && r[u] >= list.least, r[u], p.top);
     }
-    put_together<true>(list, p.top, sh);
+    if (!all_arrived(words, slice, p.slices, p.tag, sh.told)) return;
+    if (wave == 0) {
+      const bool mine = claimed(words, p.slices, p.tag);
+      if (lane == 0) sh.mine = mine;
+    }
+    __syncthreads();
+    if (!sh.mine) return;
+    // a lane has a slice's sums
+    const uint64_t* from = part + min(lane, p.slices - 1) * kPartWords;
+    uint64_t head[kPartHead];
+#pragma unroll
+    for (int i = 0; i < kPartHead; ++i) head[i] = i < 3 || p.top > 0 ? load_through(from + i) : 0;
+    RowSums got{as_f32(uint32_t(head[0])), 0.0, __builtin_bit_cast(double, head[1]), __builtin_bit_cast(double, head[2])};
+    if (lane >= p.slices) got = RowSums{-INFINITY, 0.0, 0.0, 0.0};
+    if (p.top > 0) {
+      float largest[kLogprobWaves];
+#pragma unroll
+      for (int i = 0; i < kLogprobWaves; ++i) largest[i] = lane < p.slices ? as_f32(uint32_t(head[4 + i / 2] >> (32 * (i & 1)))) : -INFINITY;
+      const float above = reached_by(largest, p.top);
+      const int length = lane < p.slices ? int(head[3]) : 0;
+      list = List{sh.list[wave], 0, -INFINITY, 0};
+      constexpr int kTogether = 8;
+      for (int s0 = wave; s0 < p.slices; s0 += kLogprobWaves * kTogether) {
+        uint64_t r[kTogether];
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+          const int s = min(s0 + u * kLogprobWaves, 63);
+          r[u] = lane < __builtin_amdgcn_readlane(length, s) ? load_through(part + s * kPartWords + kPartHead + lane) : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u)
+          offer(list, s0 + u * kLogprobWaves < p.slices && r[u] != 0 && cand_value(r[u]) > above && r[u] >= list.least, r[u], p.top);
+      }
+      put_together<true, W>(list, p.top, sh);
+    }
+    if (wave == 0) finish(p, entry, token, z, join(got, p.k2), odd, list);
   }
-  if (wave == 0) finish(p, entry, token, z, join(got, p.k2), odd, list);
 }
 
 // ---- the gradient of the logits ---------------------------------------------------------------------------------
@@ -530,8 +532,6 @@ template <typename T> struct Vector16 {
 template <typename T>
 __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobBackwardParams p) {
   constexpr int E = ElemTraits<T>::kPerVec, kBytes = ElemTraits<T>::kBytes;
-  __shared__ int64_t place[kMaxTop + 1];
-  __shared__ float given[kMaxTop + 1], put[kMaxTop + 1];
   const int tid = threadIdx.x, lane = lane_id();
   const uint32_t entry = blockIdx.x / uint32_t(p.slices);
   const int slice = int(blockIdx.x - entry * uint32_t(p.slices));
@@ -552,6 +552,8 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
   double c0 = 0.0, c1 = 0.0, rho = 0.0;
   float far_c = 0.0f, hi = 0.0f;
   bool known = true, far = false;
+  int place = -1;                        // of lane 0 the token, of those behind it the likeliest ones; -1: none
+  float given = 0.0f;
   if (there) {
     const float lse = as_global(p.lse)[entry];
     known = fabsf(lse) < INFINITY;
@@ -566,38 +568,29 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
       c0 -= g * as_global(p.entropy)[entry];
       c1 = -g * 0.69314718055994530942;
     }
-    int64_t j = -1;
-    float g = 0.0f;
     if (lane == 0 && p.grad_logp) {
-      j = as_global(p.tokens)[entry];
-      g = as_global(p.grad_logp)[entry];
+      place = as_global(p.tokens)[entry];
+      given = as_global(p.grad_logp)[entry];
     } else if (lane > 0 && lane <= p.top) {
-      j = as_global(p.top_idx)[int64_t(entry) * p.top + lane - 1];
-      g = as_global(p.grad_top)[int64_t(entry) * p.top + lane - 1];
+      place = as_global(p.top_idx)[int64_t(entry) * p.top + lane - 1];
+      given = as_global(p.grad_top)[int64_t(entry) * p.top + lane - 1];
     }
-    const bool counts = j >= 0 && j < p.V;
-    c0 -= wave_sum_f64(counts ? double(g) : 0.0);
-    if (tid <= p.top) {
-      place[tid] = counts ? j : -1;
-      given[tid] = g;
-    }
+    if (place < 0 || place >= p.V) { place = -1; given = 0.0f; }
+    c0 -= wave_sum_f64(double(given));
   }
   const float f = float(exp2(-rho) * double(p.rT)), a0 = f * float(c0 - c1 * rho), a1 = f * float(c1), k2 = p.k2, none = there ? NAN : 0.0f;
   const bool fill = !there || !known;
   // (a p of 0 gives 0, whatever its logarithm)
   const auto of = [&](float d) { return fast_exp2(d) * fmaf(a1, fmaxf(d, -200.0f), a0); };
   const auto gradient = [&](float z) { return fill ? none : of(far ? (z - far_c) * k2 : fmaf(z, k2, -hi)); };
-  __syncthreads();
-  // the given places in this share: their numbers, before the logits are written over (by this share alone)
-  if (!fill && tid <= p.top) {
-    const int64_t j = place[tid];
-    float sum = 0.0f;
-    for (int k = 0; k <= p.top; ++k) sum += place[k] == j ? given[k] : 0.0f;
-    const int64_t lo = first ? 0 : rs.head + begin * E, hi_at = last ? p.V : rs.head + end * E;
-    if (j >= lo && j < hi_at) put[tid] = fmaf(p.rT, sum, gradient(load_elem<T>(row, j)));
-    else if (j >= 0) place[tid] = -1;
+  // the first wave: the numbers at the given places in this share, before they are written over where the results lie on the logits (by this share alone)
+  const int64_t lo = first ? 0 : rs.head + begin * E, hi_at = last ? p.V : rs.head + end * E;
+  const bool some = !fill && (p.grad_logp || p.top > 0), mine = some && tid <= p.top && place >= lo && place < hi_at;
+  const float z_there = mine ? load_elem<T>(row, place) : 0.0f;
+  if (p.out == p.logits && some) {
+    stores_arrived();                                    // (and loads)
+    __syncthreads();
   }
-  __syncthreads();
   if (tid < edges) store_elem<T>(out, edge_at, gradient(fill ? 0.0f : load_elem<T>(row, edge_at)));
   constexpr int kAheadBack = 4;
   for (int64_t v0 = begin + tid; v0 < end; v0 += kBlock * kAheadBack) {
@@ -628,15 +621,17 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
       __builtin_nontemporal_store(Vector16<T>::pack(z), body + v0 + u * kBlock);
     }
   }
-  if (fill) return;
-  // whoever has written there
+  if (!some) return;
+  // the given places, behind everything that was written there
+  stores_arrived();
+  __syncthreads();
+  if (wave_id() > 0) return;
+  float sum = 0.0f;
   for (int k = 0; k <= p.top; ++k) {
-    const int64_t j = place[k];
-    if (j < 0) continue;
-    const int64_t in_body = j - rs.head, v = in_body / E;
-    const bool edge = in_body < 0 || v >= rs.nvec;
-    if (edge ? tid < edges && edge_at == j : tid == int((v - begin) % kBlock)) store_elem<T>(out, j, put[k]);
+    const int other = __builtin_amdgcn_readlane(place, k);
+    sum += other == place ? as_f32(__builtin_amdgcn_readlane(as_u32(given), k)) : 0.0f;
   }
+  if (mine) store_elem<T>(out, place, fmaf(p.rT, sum, gradient(z_there)));
 }
 
 }  // namespace tslt

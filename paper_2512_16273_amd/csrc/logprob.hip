@@ -8,9 +8,10 @@
 
 namespace {
 
-// Workgroups of a row: where rows are fewer than fill the GPU, shares of 8 KB and more.
+// Workgroups of a row: where rows are fewer than fill the GPU, shares of 8 KB and more.  Twice as many where there are rows for half of the compute units (5 likeliest of
+// 16 x 9 rows of 128256 for 2 / 4 / 8 workgroups a unit 28.2 / 22.9 / 28.6 us, of 4 x 9 rows, whose join they delay, 15.9 / 17.5 / 18.4).
 int shares(int64_t entries, int64_t V, int bytes) {
-  const int64_t fill = 2 * int64_t(tslt::compute_units()), most = std::min<int64_t>(64, V * bytes / 8192);
+  const int64_t cus = tslt::compute_units(), fill = (2 * entries >= cus ? 4 : 2) * cus, most = std::min<int64_t>(64, V * bytes / 8192);
   return int(std::max<int64_t>(1, std::min<int64_t>(most, fill / std::max<int64_t>(entries, 1))));
 }
 // Of the gradient, which leaves nothing to join, more: rows that do not count are only filled, so that shares take unequal times (8 x 256 rows of 128256, two thirds
@@ -31,6 +32,16 @@ int check_logits(const char* who, tslt_dtype dt, int64_t B, int32_t n, int64_t V
     return fail(TSLT_ERR_INVALID_ARG, "%s: temperature must be > 0", who);
   if (top < 0 || top > TSLT_MAX_TOP) return fail(TSLT_ERR_UNSUPPORTED, "%s: top must be 0 to %d (got %d)", who, TSLT_MAX_TOP, int(top));
   return TSLT_OK;
+}
+// Many short rows: a wave to each, with nothing to wait for between waves (us with four waves / one, binary16 rows with 5 likeliest: 25000 rows of 2200 logits 144 / 60, 6000 of
+// 8000 39 / 33, 6000 of 16000 66 / 54, of 32000 87 / 86; fewer rows leave too few waves: 1500 of 2200 13.1 / 9.7, of 8000 13.9 / 19.1, 2304 of 32000 41 / 52).
+bool one_wave(int64_t entries, int64_t bytes) {
+  const int64_t cus = tslt::compute_units();
+  return (entries >= 8 * cus && bytes <= 32768) || (entries >= 4 * cus && bytes <= 8192);
+}
+template <typename T> void launch_logprob(const tslt::LogprobParams& p, bool one, unsigned blocks, hipStream_t s) {
+  if (one) hipLaunchKernelGGL((tslt::logprob_kernel<T, 1>), dim3(blocks), dim3(64), 0, s, p);
+  else hipLaunchKernelGGL((tslt::logprob_kernel<T, tslt::kLogprobWaves>), dim3(blocks), dim3(64 * tslt::kLogprobWaves), 0, s, p);
 }
 float exponent_scale(float rT) { return float(double(rT) * 1.4426950408889634074); }
 
@@ -71,8 +82,10 @@ int tslt_logprob(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_
   }
   int code;
   if (!grid_fits(who, entries * p.slices, code)) return code;
-  const auto kernel = dt == TSLT_F32 ? tslt::logprob_kernel<float> : dt == TSLT_BF16 ? tslt::logprob_kernel<tslt::Bf16> : tslt::logprob_kernel<tslt::F16>;
-  hipLaunchKernelGGL(kernel, dim3(unsigned(entries * p.slices)), dim3(tslt::kLogprobThreads), 0, reinterpret_cast<hipStream_t>(stream), p);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const unsigned blocks = unsigned(entries * p.slices);
+  const bool one = one_wave(entries, V * elem_bytes(dt));
+  dt == TSLT_F32 ? launch_logprob<float>(p, one, blocks, s) : dt == TSLT_BF16 ? launch_logprob<tslt::Bf16>(p, one, blocks, s) : launch_logprob<tslt::F16>(p, one, blocks, s);
   return launched("tslt_logprob launch");
 }
 
