@@ -6,6 +6,10 @@
 // A row is D / 16 lanes wide: each has two runs of eight channels, of which one holds the partners of the other (of pairs half the rotated
 // channels apart; neighbours are partners inside a run), so that nothing but a row's sums crosses lanes.  The angles of a token are those of all its
 // heads: a workgroup takes kTokens tokens, computes their cosines and sines once, a lane an angle, and then all of their rows.
+//
+// Bound by memory, and forwards almost as much by vector instructions (250 for the 16 channels of a lane: sums of squares in fp64, two products with r and the weight,
+// the turn, two addresses).  bfloat16, 40 heads of 128: prompts of 4 x 4001 tokens, three axes, a third of which count, 26.7 us (3.8 TB/s), 64 x 21 tokens 9.1; backwards 8 x 2048 tokens 102 us
+// (4.9 TB/s, what a copy reaches), 5 of them the weights' second launch.  One token 2.9 on the device, 5.1 a call: the launch, its position, its row.
 #pragma once
 #include "rows.h"
 
