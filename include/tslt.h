@@ -540,7 +540,7 @@ typedef struct {
 } tslt_rotation;
 
 /*   q           [B][n][heads_q][head_dim] of type dt;  k [B][n][heads][head_dim], NULL: none (heads does not count then)
- *   out_q, out_k  the same shapes and type; each may be its input itself (the same place and strides)
+ *   out_q, out_k  the same shapes and type, no two rows on each other; each may be its input itself (the same place and strides)
  *   status      [B] int32; may be NULL
  * head_dim is 64, 128 or 256.  Angles are fp64 until they are brought into one turn, sums of squares fp64, the rest fp32, rounded once.  A row that
  * holds a number that is not finite comes out as those rules give.  No workspace. */

@@ -500,7 +500,7 @@ bool read_workspace(PyObject* o, void*& p, size_t& bytes) {
 // position, freq, axis, base, q_weight, k_weight, eps, adjacent: eight arguments from a on.
 bool read_rotation(PyObject* const* a, int64_t B, int64_t n, int64_t D, tslt_rotation& how) {
   how = {};
-  how.axes = 1;
+  how.axes = TSLT_MAX_AXES;              // (without positions a token is at the same place on every axis)
   if (a[1] != Py_None) {
     const at::Tensor* freq = dense(a[1], at::kFloat);
     if (freq == nullptr || freq->dim() != 1 || freq->numel() > 256) return false;

@@ -20,6 +20,12 @@ inline int check_rows(const char* who, const char* what, const tslt_rows* r, tsl
     return fail(TSLT_ERR_INVALID_ARG, "%s: rows of %s must begin at multiples of 16 bytes", who, what);
   return TSLT_OK;
 }
+// Rows that are written to: not one for several.
+inline int check_distinct(const char* who, const char* what, const tslt_rows* r, int64_t B, int64_t n, int64_t heads) {
+  if ((B > 1 && r->seq_stride == 0) || (n > 1 && r->token_stride == 0) || (heads > 1 && r->head_stride == 0))
+    return fail(TSLT_ERR_INVALID_ARG, "%s: rows of %s must not lie on each other", who, what);
+  return TSLT_OK;
+}
 inline bool valid_dtype(tslt_dtype dt) { return dt == TSLT_F32 || dt == TSLT_BF16 || dt == TSLT_F16; }
 inline tslt::RowsView view(const tslt_rows* r) {
   return r ? tslt::RowsView{r->data, r->seq_stride, r->token_stride, r->head_stride} : tslt::RowsView{nullptr, 0, 0, 0};

@@ -30,6 +30,7 @@ ROW_NONFINITE, ROW_EMPTY, ROW_TOKEN_NOT_IN_SET, ROW_BAD_SET, ROW_EXACT_PATH = 1,
 ROW_BAD_PAGE, ROW_BAD_INDEX = 16, 32
 PAGE_TOKENS = 64
 MAX_TOP = 32
+MAX_AXES = 4
 MAX_K_CAP = 1024
 PAYLOAD = {"f32": 0, "bf16": 1, "f16": 2}       # tslt_dtype codes of the formats a payload can travel in
 
@@ -770,7 +771,7 @@ def _rotation(B: int, n: int, D: int, position, freq, axis, base, q_weight, k_we
         if freq.dim() != 1:
             raise TsltError("freq must be [rotary / 2]")
         pairs = freq.numel()
-    axes, seq = 1, 0
+    axes, seq = MAX_AXES, 0                     # (without positions a token is at the same place on every axis)
     if position is not None:
         _dev(position, torch.int32, "position")
         if position.dim() != 3 or position.shape[0] not in (1, B) or position.shape[1] != n:

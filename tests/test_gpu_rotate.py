@@ -117,6 +117,9 @@ def test_defaults_no_keys_no_positions():
     assert got["k"] is None
     at = torch.arange(70, device=DEV, dtype=torch.int32).view(1, 70, 1)
     assert torch.equal(got["q"], tslt.rotate(c["q"], None, at, c["freq"])["q"])
+    axis = torch.arange(32, device=DEV, dtype=torch.int32) % 4
+    also = tslt.rotate(c["q"], None, None, c["freq"], axis=axis)   # the same place on every axis
+    assert torch.equal(also["q"], got["q"]) and also["status"].tolist() == [0, 0]
     assert torch.equal(tslt.rotate(c["q"], None, None, None)["q"], c["q"])
     normed = tslt.rotate(c["q"], None, None, None, eps=1e-5)["q"]
     want = O.rotate(host(c["q"]), np.ones((2, 70, 0)), np.zeros((2, 70, 0)), False, None, 1e-5)

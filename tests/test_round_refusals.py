@@ -39,6 +39,8 @@ def rotation_refusals(lib, call):
     assert call(q=None) == -1 and call(q=rows(data=FAKE + 2)) == -1 and call(q=rows(token=100)) == -1 and "16 bytes" in message(lib)
     assert call(oq=rows(head=3)) == -1 and call(ok=None) == -1 and "together" in message(lib)
     assert call(oq=rows(seq=2048)) == -1 and "in place" in message(lib)
+    for lie in (dict(seq=0), dict(token=0), dict(head=0)):
+        assert call(oq=rows(FAKE * 2, **lie)) == -1 and call(ok=rows(FAKE * 3, **lie)) == -1 and "each other" in message(lib)
 
 
 def test_rotate(lib):
@@ -104,6 +106,7 @@ def test_logprob_backward(lib):
     assert call(idx=None) == -1 and call(top=0) == -1 and "top_idx" in message(lib)
     assert call(z=FAKE + 1) == -1 and call(out=FAKE + 1) == -1
     assert call(out=FAKE, stride=1008) == -1 and "written over" in message(lib)
+    assert call(stride=0) == -1 and call(stride=999) == -1 and "each other" in message(lib)
     assert call(B=0) == 0
 
 
@@ -126,6 +129,7 @@ def test_adapt(lib):
     assert call(x=None) == -1 and call(base=rows(data=None)) == -1 and call(out=rows(FAKE * 3 + 1)) == -1 and call(x=rows(token=12)) == -1
     assert call(a=None) == -1 and call(b=None) == -1 and call(adapter=None) == -1 and call(a=FAKE + 8) == -1 and call(b=FAKE + 2) == -1
     assert call(out=rows(FAKE * 2, token=513)) == -1 and "in place" in message(lib)
+    assert call(out=rows(FAKE * 3, seq=0)) == -1 and call(out=rows(FAKE * 3, token=0)) == -1 and "each other" in message(lib)
     need = lib.tslt_adapt_workspace_bytes(2, 3, 64, 100, 16)
     assert need > 0
     for ws, size in ((None, need), (FAKE + 16, need), (FAKE, need - 1)):
