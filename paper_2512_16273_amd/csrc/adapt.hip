@@ -98,7 +98,7 @@ int tslt_adapt(const tslt_rows* x, int32_t K, const tslt_rows* base, const tslt_
   if (!ws || !aligned(ws, 256) || ws_bytes < need)
     return fail(TSLT_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu are needed, 256-byte aligned", who, ws ? ws_bytes : size_t(0), need);
   int code;
-  if (!grid_fits(who, B * std::max<int64_t>(int64_t(plan.tiles) * plan.chunks * plan.cuts, int64_t(plan.up_tiles) * plan.splits), code)) return code;
+  if (!grid_fits(who, B * std::max<int64_t>(int64_t(plan.tiles) * plan.chunks * plan.cuts, int64_t(plan.up_tiles) * plan.splits), code, tslt::kBlock)) return code;
   tslt::AdaptParams p{};
   p.x = view(&rx); p.base = view(&rb); p.out = view(&ro);
   p.K = K; p.N = N; p.R = R; p.n = n; p.B = B; p.n_adapters = n_adapters; p.a = a; p.b = b; p.adapter = adapter; p.rank = rank; p.count = count;

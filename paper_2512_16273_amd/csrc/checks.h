@@ -30,8 +30,9 @@ inline bool valid_dtype(tslt_dtype dt) { return dt == TSLT_F32 || dt == TSLT_BF1
 inline tslt::RowsView view(const tslt_rows* r) {
   return r ? tslt::RowsView{r->data, r->seq_stride, r->token_stride, r->head_stride} : tslt::RowsView{nullptr, 0, 0, 0};
 }
-inline bool grid_fits(const char* who, int64_t blocks, int& code) {
-  code = blocks > 0x7FFFFFFF ? fail(TSLT_ERR_UNSUPPORTED, "%s: too many workgroups for one launch", who) : 0;
+// A launch has fewer than 2^32 threads (`threads` a workgroup; the calls that leave it out are bounded by their own checks or by HIP).
+inline bool grid_fits(const char* who, int64_t blocks, int& code, int64_t threads = 1) {
+  code = blocks > (threads == 1 ? 0x7FFFFFFF : 0xFFFFFFFF / threads) ? fail(TSLT_ERR_UNSUPPORTED, "%s: too many workgroups for one launch", who) : 0;
   return code == 0;
 }
 inline int launched(const char* who) {

@@ -82,10 +82,10 @@ int tslt_logprob(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_
     p.tag = tslt::next_tag();
   }
   int code;
-  if (!grid_fits(who, entries * p.slices, code)) return code;
+  const bool one = one_wave(entries, V * elem_bytes(dt));
+  if (!grid_fits(who, entries * p.slices, code, one ? 64 : 64 * tslt::kLogprobWaves)) return code;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const unsigned blocks = unsigned(entries * p.slices);
-  const bool one = one_wave(entries, V * elem_bytes(dt));
   dt == TSLT_F32 ? launch_logprob<float>(p, one, blocks, s) : dt == TSLT_BF16 ? launch_logprob<tslt::Bf16>(p, one, blocks, s) : launch_logprob<tslt::F16>(p, one, blocks, s);
   return launched("tslt_logprob launch");
 }
@@ -112,7 +112,7 @@ int tslt_logprob_backward(const void* logits, tslt_dtype dt, int64_t B, int32_t 
   p.grad_logp = grad_logp; p.grad_entropy = grad_entropy; p.grad_lse = grad_lse; p.grad_top = grad_top;
   p.slices = shares_back(B * n, V, elem_bytes(dt));
   int code;
-  if (!grid_fits(who, B * n * p.slices, code)) return code;
+  if (!grid_fits(who, B * n * p.slices, code, tslt::kBlock)) return code;
   const auto kernel = dt == TSLT_F32 ? tslt::logprob_backward_kernel<float> : dt == TSLT_BF16 ? tslt::logprob_backward_kernel<tslt::Bf16> : tslt::logprob_backward_kernel<tslt::F16>;
   hipLaunchKernelGGL(kernel, dim3(unsigned(B * n * p.slices)), dim3(tslt::kBlock), 0, reinterpret_cast<hipStream_t>(stream), p);
   return launched("tslt_logprob_backward launch");

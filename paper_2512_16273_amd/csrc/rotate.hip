@@ -91,6 +91,8 @@ int tslt_rotate(const tslt_rows* q, const tslt_rows* k, tslt_dtype dt, int64_t B
   }
   if ((q->data == out_q->data && !same_rows(q, out_q)) || (k && k->data == out_k->data && !same_rows(k, out_k)))
     return fail(TSLT_ERR_INVALID_ARG, "%s: rows that are rotated in place must have the same strides", who);
+  int code;
+  if (!grid_fits(who, (B * n + tokens_each(B * n) - 1) / tokens_each(B * n), code, tslt::kBlock)) return code;
   tslt::RotateParams p = params(B, n, heads_q, heads, k != nullptr, how, count, status);
   p.q = view(q); p.k = view(k); p.out_q = view(out_q); p.out_k = view(out_k);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);

@@ -50,6 +50,7 @@ def test_rotate(lib):
         return lib.tslt_rotate(q, k, dt, B, n, hq, h, D, r, None, oq, ok, None, None)
     rotation_refusals(lib, call)
     assert call(k=None) == -1 and "together" in message(lib)
+    assert call(B=(1 << 26) + 4, n=1) == -2 and "workgroups" in message(lib)       # four tokens to each, 2^32 threads
     assert call(B=0) == 0
 
 
@@ -82,6 +83,8 @@ def test_logprob(lib):
         return lib.tslt_logprob(z, dt, B, n, V, n * V, V, T, index, m, None, tokens, top, None, None, None, idx, logp, None, ws, ws_bytes, None)
     assert call(dt=9) == -1 and call(B=-1) == -1 and call(n=0) == -1 and call(V=0) == -1 and call(z=None) == -1
     assert call(V=1 << 31) == -2 and call(dt=0, V=1 << 30) == -2 and call(B=1 << 31) == -2 and call(index=FAKE, m=1 << 30, B=4) == -2
+    for rows_, V in ((1 << 26, 1000), (1 << 24, 17000)):                           # a wave, four waves to each
+        assert call(B=rows_, n=1, m=1, V=V) == -2 and "workgroups" in message(lib)
     for T in (0.0, -1.0, NAN, INF, 1e-39, 5e-39, 9e-39):
         assert call(T=T) == -1 and "temperature" in message(lib)
     assert call(m=2) == -1 and call(index=FAKE, m=0) == -1 and "index" in message(lib)
@@ -101,6 +104,7 @@ def test_logprob_backward(lib):
         return lib.tslt_logprob_backward(z, dt, B, n, V, n * V, V, T, None, tokens, lse, entropy, idx, top, g, gh, None, gt, out, n * stride, stride, None)
     assert call(dt=9) == -1 and call(B=-1) == -1 and call(n=0) == -1 and call(V=0) == -1 and call(z=None) == -1 and call(out=None) == -1 and call(lse=None) == -1
     assert call(V=1 << 31) == -2 and call(B=1 << 31) == -2 and call(T=0.0) == -1 and call(top=33) == -2
+    assert call(B=1 << 24, n=1) == -2 and "workgroups" in message(lib)
     assert call(tokens=None) == -1 and "tokens" in message(lib)
     assert call(entropy=None) == -1 and "entropy" in message(lib)
     assert call(idx=None) == -1 and call(top=0) == -1 and "top_idx" in message(lib)
@@ -134,6 +138,7 @@ def test_adapt(lib):
     assert need > 0
     for ws, size in ((None, need), (FAKE + 16, need), (FAKE, need - 1)):
         assert call(ws=ws, ws_bytes=size) == -3 and "workspace" in message(lib)
+    assert call(B=1 << 24, n=1, ws_bytes=1 << 40) == -2 and "workgroups" in message(lib)
     assert call(B=0) == 0
     for bad in ((0, 3, 64, 100, 16), (2, 3, 64, 100, 24), (1 << 31, 3, 64, 100, 16)):
         assert lib.tslt_adapt_workspace_bytes(*bad) == 0
