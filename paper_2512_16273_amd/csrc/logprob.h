@@ -3,7 +3,7 @@
 //
 // With k = log2(e) / T and a reference c of the row's logits (the largest that a wave has met), a term is e_j = 2^(k z_j - fl(k c)), one multiply-add and
 // one exponential; S = sum e_j and E = sum e_j log2 e_j.  Then, with rho = k c - fl(k c) (taken back in fp64 where terms are added up), lse = c / T + ln S - rho ln 2
-// and H = ln S - ln 2 E / S.  A wave whose logits pass its reference takes the larger one: S 2^d and 2^d (E + d S), d < 0 the difference.
+// and H = ln S - ln 2 E / S.  A wave whose logits pass its reference takes the larger one: S 2^d and 2^d (E + d S), d < 0 the difference of the two fl(k c).
 //
 // The `top` largest: each wave keeps a list in LDS of the logits above a threshold that `top` of the row's logits are known to reach.  At first that are the largest
 // logits of the workgroup's lanes in the first loads: `top` of those 256 numbers are reached by as many logits, and by few more.  Whenever four times as much of the row has been
@@ -181,15 +181,21 @@ struct RowWave {
     S += s[0];
     E += t[N / 2];
   }
+  // A term is 2^(k z - k c + rho), rho = k c - fl(k c) of the reference that it met (0 where differences are taken first): what a new one changes is both.
   __device__ __forceinline__ void refer(float most, float k2) {
+#pragma clang fp contract(off)           // (kc - now is of the rounded products)
+    const float now = most * k2;
+    const bool now_far = !(fabsf(now) < 4194304.0f);
     if (c != -INFINITY) {
-      const float d = (c - most) * k2, f = fast_exp2(d);
+      float d = kc - now;
+      if (far || now_far) d = (c - most) * k2 + ((now_far ? 0.0f : fmaf(most, k2, -now)) - (far ? 0.0f : fmaf(c, k2, -kc)));
+      const float f = fast_exp2(d);
       E = f > 0.0f ? f * fmaf(d, S, E) : 0.0f;
       S = f * S;
     }
     c = most;
-    kc = c * k2;
-    far = !(fabsf(kc) < 4194304.0f);
+    kc = now;
+    far = now_far;
   }
 };
 
