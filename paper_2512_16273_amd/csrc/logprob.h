@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
     far = !(fabs(scaled) < 4194304.0);
     far_c = float(reference);
     hi = float(scaled);
-    rho = far ? 0.0 : scaled - double(hi);
+    rho = far ? (reference - double(far_c)) * double(p.k2) : scaled - double(hi);
     if (p.grad_lse) c0 += as_global(p.grad_lse)[entry];
     if (p.grad_entropy) {
       const double g = as_global(p.grad_entropy)[entry];
