@@ -590,7 +590,9 @@ int tslt_logprob(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_
  *               tokens with grad_logp, top_idx with grad_top.  A token or index outside 0..V-1 has no part
  *   grad_logp, grad_entropy, grad_lse  [B][n] fp32, grad_top [B][n][top] fp32; NULL: 0
  *   out         [B][n] rows like the logits', of their type, out_seq_stride and out_row_stride; may be the logits themselves (the same place and
- *               strides).  Rows that do not count get zeros; rows whose lse is not finite get NaN
+ *               strides).  Rows that do not count get zeros; rows that tslt_logprob could not use (lse NaN, or -inf of an empty row) get NaN
+ * p goes by the lse that is given: half a step of it, up to 2^-24 |lse|, is p's relative error beside its own roundings (2^-14 at 1000).  From |lse| = 2^23 on, where its steps
+ * are 1 and more and nothing of ln sum is left (rows of nothing but fp32's or bfloat16's lowest number; those whose lse is beyond fp32), the row is added up again instead, by one workgroup.
  * No workspace. */
 int tslt_logprob_backward(const void* logits, tslt_dtype dt, int64_t B, int32_t n, int64_t V, int64_t seq_stride, int64_t row_stride, float temperature,
                           const int32_t* count, const int32_t* tokens, const float* lse, const float* entropy, const int32_t* top_idx, int32_t top,

@@ -512,6 +512,7 @@ __global__ __launch_bounds__(64 * W) void logprob_kernel(const LogprobParams p) 
 // dz = (1 / T) (p (c0 + c1 log2 p) + what the token and the likeliest ones were given), p = 2^(k z - k T lse): elementwise, bound by
 // reading a row and writing one (8 x 256 bfloat16 rows of 128256, all of which count, 203 us, 5.2 TB/s; 42 % of which count, the others filled with zeros, 147).  The few
 // numbers of the second part are put in place by one wave at the end.  Stores go past the caches (173 us with them, then without 178).
+// A row whose lse holds nothing of ln S any more (|lse| from 2^23 on) is added up again, p = 2^(k z - k c) / S with c the largest, by one workgroup, which reads it three times.
 
 struct LogprobBackwardParams {
   const void* logits;
@@ -550,10 +551,15 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
   const int i = int(entry - b * uint32_t(p.n));
   const char* row = reinterpret_cast<const char*>(p.logits) + (int64_t(b) * p.seq_stride + i * p.row_stride) * kBytes;
   char* out = reinterpret_cast<char*>(p.out) + (int64_t(b) * p.out_seq_stride + i * p.out_row_stride) * kBytes;
+  const bool there = i < counted(p.count, b, p.n);
+  // Where fp32 has steps of 1 and more the lse says nothing of ln S (a row of nothing but the type's lowest number): one workgroup has the whole row then, and adds it up again.
+  const float lse = there ? as_global(p.lse)[entry] : 0.0f;
+  const bool again = fabsf(lse) >= 8388608.0f;
+  if (again && slice > 0) return;
   // the split goes by where the results lie; the logits may lie otherwise
   const RowSplit rs = split_row<T>(out, p.V);
-  const int64_t each = (rs.nvec + p.slices - 1) / p.slices, begin = min(each * slice, rs.nvec), end = min(begin + each, rs.nvec);
-  const bool first = slice == 0, last = slice == p.slices - 1, there = i < counted(p.count, b, p.n);
+  const int64_t each = (rs.nvec + p.slices - 1) / p.slices, begin = again ? 0 : min(each * slice, rs.nvec), end = again ? rs.nvec : min(begin + each, rs.nvec);
+  const bool first = slice == 0, last = again || slice == p.slices - 1;
   const int edges = (first ? rs.head : 0) + (last ? rs.tail : 0);
   const int64_t edge_at = tid < edges ? edge_index<T>(rs, first ? tid : rs.head + tid) : 0;
   u32x4* body = reinterpret_cast<u32x4*>(out + size_t(rs.head) * kBytes);
@@ -565,14 +571,48 @@ __global__ __launch_bounds__(kBlock) void logprob_backward_kernel(const LogprobB
   bool known = true, far = false;
   int place = -1;                        // of lane 0 the token, of those behind it the likeliest ones; -1: none
   float given = 0.0f;
-  if (there) {
-    const float lse = as_global(p.lse)[entry];
-    known = fabsf(lse) < INFINITY;
+  if (again) {
+    const auto all = [&](auto use) {
+      if (tid < edges) use(load_elem<T>(row, edge_at));
+#pragma unroll 1
+      for (int64_t v = tid; v < rs.nvec; v += kBlock) {
+        const u32x4 r = load16_any(from + v * 16);
+        float z[E];
+        unpack<T>(make_uint4(r[0], r[1], r[2], r[3]), z);
+#pragma unroll
+        for (int e = 0; e < E; ++e) use(z[e]);
+      }
+    };
+    __shared__ float most[kBlock / 64];
+    __shared__ double sums[kBlock / 64];
+    float c = -INFINITY;
+    all([&](float z) { c = fmaxf(c, z); });
+    c = wave_max_f32(c);
+    if (lane == 0) most[wave_id()] = c;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kBlock / 64; ++w) c = fmaxf(c, most[w]);
+    double S = 0.0;                      // NaN of a row that cannot be used
+    all([&](float z) { S += double(fast_exp2((z - c) * p.k2)); });
+    S = wave_sum_f64(S);
+    if (lane == 0) sums[wave_id()] = S;
+    __syncthreads();
+    S = 0.0;
+#pragma unroll
+    for (int w = 0; w < kBlock / 64; ++w) S += sums[w];
+    known = S == S;
+    far = true;
+    far_c = c;
+    rho = log2(S);
+  } else if (there) {
+    known = lse == lse;
     const double reference = double(lse) / double(p.rT), scaled = double(p.k2) * reference;
     far = !(fabs(scaled) < 4194304.0);
     far_c = float(reference);
     hi = float(scaled);
     rho = far ? (reference - double(far_c)) * double(p.k2) : scaled - double(hi);
+  }
+  if (there) {
     if (p.grad_lse) c0 += as_global(p.grad_lse)[entry];
     if (p.grad_entropy) {
       const double g = as_global(p.grad_entropy)[entry];
