@@ -188,7 +188,7 @@ struct RowWave {
     const bool now_far = !(fabsf(now) < 4194304.0f);
     if (c != -INFINITY) {
       float d = kc - now;
-      if (far || now_far) d = (c - most) * k2 + ((now_far ? 0.0f : fmaf(most, k2, -now)) - (far ? 0.0f : fmaf(c, k2, -kc)));
+      if (same_in_wave(far || now_far)) d = (c - most) * k2 + ((now_far ? 0.0f : fmaf(most, k2, -now)) - (far ? 0.0f : fmaf(c, k2, -kc)));
       const float f = fast_exp2(d);
       E = f > 0.0f ? f * fmaf(d, S, E) : 0.0f;
       S = f * S;
