@@ -490,6 +490,8 @@ int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t widt
  * what was accepted.  Rows of tokens are tslt_rows as above ([B][n][heads][D], or [B][n][width], whose head_stride does not count), also where
  * they are written to; `count` [B] int32 says how many of a sequence's n tokens (or entries) there are, the first ones: 0..n, another
  * counts as the nearest and sets TSLT_ROW_BAD_INDEX; NULL: all.  What belongs to the others is not read, and is left as it was.
+ * Rows that are written to lie apart: of sequences, tokens and heads, from the smallest stride to the largest, each steps over all that those before
+ * it span (any order of them, parts of wider rows); rows that do not are refused.
  * A call of more tokens (entries) than one launch has workgroups for, 2^24 and more, is refused. */
 
 /* Adapters of many requests: out_t = base_t + scale_a * (x_t A_a^T) B_a^T, a = adapter of the token's sequence.

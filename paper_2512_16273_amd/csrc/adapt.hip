@@ -88,9 +88,9 @@ int tslt_adapt(const tslt_rows* x, int32_t K, const tslt_rows* base, const tslt_
   if (int e = check_rows(who, "x", &rx, dt)) return e;
   if (!rb.data || !ro.data) return fail(TSLT_ERR_INVALID_ARG, "%s: null pointer", who);
   if (!aligned(rb.data, elem_bytes(dt)) || !aligned(ro.data, elem_bytes(dt))) return fail(TSLT_ERR_INVALID_ARG, "%s: rows not aligned to their type", who);
-  if (int e = check_distinct(who, "out", &ro, B, n, 1)) return e;
   if (rb.data == ro.data && (rb.seq_stride != ro.seq_stride || rb.token_stride != ro.token_stride))
     return fail(TSLT_ERR_INVALID_ARG, "%s: rows that are added to in place must have the same strides", who);
+  if (int e = check_distinct(who, "out", &ro, B, n, 1, N)) return e;
   if (!a || !b || !adapter) return fail(TSLT_ERR_INVALID_ARG, "%s: null pointer", who);
   if (!aligned(a, 16) || !aligned(b, 16)) return fail(TSLT_ERR_INVALID_ARG, "%s: adapters not aligned to 16 bytes", who);
   const Plan plan = plan_adapt(dt, B, n, K, N, R);

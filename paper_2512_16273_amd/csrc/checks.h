@@ -2,6 +2,8 @@
 #pragma once
 #include "tslt.h"
 
+#include <algorithm>
+
 #include "error.h"
 #include "rows.h"
 
@@ -20,10 +22,18 @@ inline int check_rows(const char* who, const char* what, const tslt_rows* r, tsl
     return fail(TSLT_ERR_INVALID_ARG, "%s: rows of %s must begin at multiples of 16 bytes", who, what);
   return TSLT_OK;
 }
-// Rows that are written to: not one for several.
-inline int check_distinct(const char* who, const char* what, const tslt_rows* r, int64_t B, int64_t n, int64_t heads) {
-  if ((B > 1 && r->seq_stride == 0) || (n > 1 && r->token_stride == 0) || (heads > 1 && r->head_stride == 0))
-    return fail(TSLT_ERR_INVALID_ARG, "%s: rows of %s must not lie on each other", who, what);
+// Rows of `width` elements that are written to lie apart: from the nearest of their dimensions to the farthest, each steps over all that those inside it span.
+inline int check_distinct(const char* who, const char* what, const tslt_rows* r, int64_t B, int64_t n, int64_t heads, int64_t width) {
+  typedef __int128 Wide;
+  struct Dim { Wide stride; int64_t size; } d[3] = {{r->seq_stride, B}, {r->token_stride, n}, {r->head_stride, heads}};
+  for (Dim& x : d) x.stride = x.size < 2 ? 0 : x.stride < 0 ? -x.stride : x.stride;
+  std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  Wide span = width;
+  for (const Dim& x : d) {
+    if (x.size < 2) continue;
+    if (x.stride < span) return fail(TSLT_ERR_INVALID_ARG, "%s: rows of %s must not lie on each other", who, what);
+    span += x.stride * (x.size - 1);
+  }
   return TSLT_OK;
 }
 inline bool valid_dtype(tslt_dtype dt) { return dt == TSLT_F32 || dt == TSLT_BF16 || dt == TSLT_F16; }

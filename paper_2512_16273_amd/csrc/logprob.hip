@@ -2,7 +2,6 @@
 #include "tslt.h"
 
 #include <algorithm>
-#include <cstdlib>
 
 #include "checks.h"
 #include "logprob.h"
@@ -102,7 +101,8 @@ int tslt_logprob_backward(const void* logits, tslt_dtype dt, int64_t B, int32_t 
   if (grad_logp && !tokens) return fail(TSLT_ERR_INVALID_ARG, "%s: grad_logp needs tokens", who);
   if (grad_entropy && !entropy) return fail(TSLT_ERR_INVALID_ARG, "%s: grad_entropy needs entropy", who);
   if (grad_top && (!top_idx || top < 1)) return fail(TSLT_ERR_INVALID_ARG, "%s: grad_top needs top_idx", who);
-  if ((n > 1 && std::abs(out_row_stride) < V) || (B > 1 && out_seq_stride == 0)) return fail(TSLT_ERR_INVALID_ARG, "%s: rows of out must not lie on each other", who);
+  const tslt_rows made{out, out_seq_stride, out_row_stride, 0};
+  if (int e = check_distinct(who, "out", &made, B, n, 1, V)) return e;
   if (out == logits && (seq_stride != out_seq_stride || row_stride != out_row_stride))
     return fail(TSLT_ERR_INVALID_ARG, "%s: logits that are written over must have the same strides", who);
   tslt::LogprobBackwardParams p{};

@@ -83,11 +83,11 @@ int tslt_rotate(const tslt_rows* q, const tslt_rows* k, tslt_dtype dt, int64_t B
   if (B == 0) return TSLT_OK;
   if (int e = check_rows(who, "q", q, dt)) return e;
   if (int e = check_rows(who, "out_q", out_q, dt)) return e;
-  if (int e = check_distinct(who, "out_q", out_q, B, n, heads_q)) return e;
+  if (int e = check_distinct(who, "out_q", out_q, B, n, heads_q, head_dim)) return e;
   if (k) {
     if (int e = check_rows(who, "k", k, dt)) return e;
     if (int e = check_rows(who, "out_k", out_k, dt)) return e;
-    if (int e = check_distinct(who, "out_k", out_k, B, n, heads)) return e;
+    if (int e = check_distinct(who, "out_k", out_k, B, n, heads, head_dim)) return e;
   }
   if ((q->data == out_q->data && !same_rows(q, out_q)) || (k && k->data == out_k->data && !same_rows(k, out_k)))
     return fail(TSLT_ERR_INVALID_ARG, "%s: rows that are rotated in place must have the same strides", who);
@@ -118,13 +118,13 @@ int tslt_rotate_backward(const tslt_rows* grad_q, const tslt_rows* grad_k, const
   if (B > 0) {
     if (int e = check_rows(who, "grad_q", grad_q, dt)) return e;
     if (int e = check_rows(who, "out_q", out_q, dt)) return e;
-    if (int e = check_distinct(who, "out_q", out_q, B, n, heads_q)) return e;
+    if (int e = check_distinct(who, "out_q", out_q, B, n, heads_q, head_dim)) return e;
     if (norm)
       if (int e = check_rows(who, "q", q, dt)) return e;
     if (grad_k) {
       if (int e = check_rows(who, "grad_k", grad_k, dt)) return e;
       if (int e = check_rows(who, "out_k", out_k, dt)) return e;
-      if (int e = check_distinct(who, "out_k", out_k, B, n, heads)) return e;
+      if (int e = check_distinct(who, "out_k", out_k, B, n, heads, head_dim)) return e;
       if (norm)
         if (int e = check_rows(who, "k", k, dt)) return e;
     }
