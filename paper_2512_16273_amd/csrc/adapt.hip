@@ -22,12 +22,12 @@ Plan plan_adapt(tslt_dtype dt, int64_t B, int32_t n, int32_t K, int32_t N, int32
   const auto between = [](int64_t least, int64_t x, int64_t most) { return int(std::max(least, std::min(x, most))); };
   p.token_tiles = n > 16 ? 4 : 1;
   p.rank_tiles = R == 16 ? 1 : R == 32 ? 2 : 4;
-  p.tiles = (n + 16 * p.token_tiles - 1) / (16 * p.token_tiles);
+  p.tiles = int((int64_t(n) + 16 * p.token_tiles - 1) / (16 * p.token_tiles));
   p.chunks = (R / 16 + p.rank_tiles - 1) / p.rank_tiles;
   p.cuts = between(1, std::min<int64_t>(512 / R, K / 512), 8);
   p.cuts = between(1, 2 * cus / (sequences * p.tiles * p.chunks), p.cuts);
-  p.up_token_tiles = n <= 16 ? 1 : dt == TSLT_F32 || sequences * ((n + 63) / 64) < cus / 2 ? 2 : 4;
-  p.up_tiles = (n + 16 * p.up_token_tiles - 1) / (16 * p.up_token_tiles);
+  p.up_token_tiles = n <= 16 ? 1 : dt == TSLT_F32 || sequences * ((int64_t(n) + 63) / 64) < cus / 2 ? 2 : 4;
+  p.up_tiles = int((int64_t(n) + 16 * p.up_token_tiles - 1) / (16 * p.up_token_tiles));
   const int64_t fill = (n <= 16 ? 5 : p.up_token_tiles == 2 && dt != TSLT_F32 ? 3 : 2) * cus;
   p.splits = between(1, fill / (sequences * p.up_tiles), (int64_t(N) + 255) / 256);
   return p;
