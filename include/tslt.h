@@ -492,7 +492,8 @@ int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t widt
  * counts as the nearest and sets TSLT_ROW_BAD_INDEX; NULL: all.  What belongs to the others is not read, and is left as it was.
  * Rows that are written to lie apart: of sequences, tokens and heads, from the smallest stride to the largest, each steps over all that those before
  * it span (any order of them, parts of wider rows); rows that do not are refused.
- * A call of more tokens (entries) than one launch has workgroups for, 2^24 and more, is refused. */
+ * Tokens (entries) of a call fit 31 bits, and a call whose work is more than one launch takes, 2^32 threads, is refused (TSLT_ERR_UNSUPPORTED): tslt_rotate of
+ * some 2^26 tokens, tslt_logprob of 2^24 rows (2^26 short ones), tslt_logprob_backward of 2^24 rows, tslt_adapt of 2^24 tiles of 16 or 64 tokens of a sequence, or fewer for ranks above 64. */
 
 /* Adapters of many requests: out_t = base_t + scale_a * (x_t A_a^T) B_a^T, a = adapter of the token's sequence.
  *
