@@ -464,8 +464,13 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return result(code);
 }
 
-// ---- around attention and verification: `device` is the current one, on which the call's tensors live ----
+// ---- around attention and verification: `device` is the current one, on which all of a call's tensors have to live ----
 bool on(const at::Tensor* t, long long device) { return t != nullptr && t->device().index() == device; }
+// The same of those that are tensors among a call's arguments, and of those of its results that are named.
+bool all_on(long long device, std::initializer_list<PyObject*> given, PyObject* made, std::initializer_list<PyObject*> names) {
+  const auto fine = [&](PyObject* o) { return o == nullptr || !THPVariable_Check(o) || THPVariable_Unpack(o).device().index() == device; };
+  return std::all_of(given.begin(), given.end(), fine) && std::all_of(names.begin(), names.end(), [&](PyObject* name) { return fine(PyDict_GetItem(made, name)); });
+}
 bool fits(std::initializer_list<int64_t> sizes) { return std::max(sizes) <= 0x7FFFFFFF; }
 // [B][n][heads][D] like the sizes given, dense along D.
 bool read_heads(PyObject* o, at::IntArrayRef sizes, at::ScalarType type, tslt_rows& rows) {
@@ -550,7 +555,7 @@ PyObject* py_rotate(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (!read_rotation(a + 2, B, n, D, how) || !read_ints(a[10], B, count)) Py_RETURN_NONE;
   bool there = true;
   int32_t* status = sized<int32_t>(a[11], k_status, at::kInt, B, true, there);
-  if (!there) Py_RETURN_NONE;
+  if (!there || !all_on(device, {a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[10]}, a[11], {k_q, k_status}) || (k && !all_on(device, {}, a[11], {k_k}))) Py_RETURN_NONE;
   int code;
   Py_BEGIN_ALLOW_THREADS
   code = lib.rotate(&qr, k ? &kr : nullptr, tslt_dtype(dt), B, int32_t(n), int32_t(heads_q), int32_t(heads), int32_t(D), &how, count, &oq, k ? &ok : nullptr, status, stream);
@@ -584,7 +589,9 @@ PyObject* py_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   float* dq = sized<float>(a[13], k_q_weight, at::kFloat, D, true, there);
   float* dk = sized<float>(a[13], k_k_weight, at::kFloat, D, true, there);
   int32_t* status = sized<int32_t>(a[13], k_status, at::kInt, B, true, there);
-  if (!there) Py_RETURN_NONE;
+  if (!there || !all_on(device, {a[1], a[4], a[5], a[6], a[7], a[8], a[9], a[12], a[14]}, a[13], {k_q, k_q_weight, k_k_weight, k_status}) ||
+      (keys && !all_on(device, {}, a[13], {k_k})) || (norm && !all_on(device, {a[2], keys ? a[3] : nullptr}, a[13], {})))
+    Py_RETURN_NONE;
   int code;
   Py_BEGIN_ALLOW_THREADS
   code = lib.rotate_backward(&gqr, keys ? &gkr : nullptr, norm ? &qr : nullptr, norm && keys ? &kr : nullptr, tslt_dtype(dt), B, int32_t(n), int32_t(heads_q), int32_t(heads),
@@ -618,7 +625,7 @@ PyObject* py_logprob(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   int32_t* top_idx = top ? sized<int32_t>(a[6], k_top_idx, at::kInt, B * m * top, false, there) : nullptr;
   float* top_logp = top ? sized<float>(a[6], k_top_logp, at::kFloat, B * m * top, false, there) : nullptr;
   int32_t* status = sized<int32_t>(a[6], k_status, at::kInt, B * m, true, there);
-  if (!there) Py_RETURN_NONE;
+  if (!there || !all_on(device, {a[2], a[4], a[5], a[7]}, a[6], {k_logp, k_entropy, k_lse, k_status}) || (top && !all_on(device, {}, a[6], {k_top_idx, k_top_logp}))) Py_RETURN_NONE;
   int code;
   Py_BEGIN_ALLOW_THREADS
   code = lib.logprob(z->data_ptr(), tslt_dtype(dt), B, int32_t(n), V, stride[0], stride[1], float(T), rows, int32_t(m), count, tokens, int32_t(top), logp, entropy, lse, top_idx,
@@ -647,7 +654,7 @@ PyObject* py_logprob_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) 
   const float *lse, *entropy, *g_logp, *g_entropy, *g_lse, *g_top;
   if (!read_ints(a[2], B * n, tokens) || !read_floats(a[3], {B, n}, lse) || !read_floats(a[4], {B, n}, entropy) || !read_floats(a[5], {B, n}, g_logp) ||
       !read_floats(a[6], {B, n}, g_entropy) || !read_floats(a[7], {B, n}, g_lse) || !read_floats(a[9], {B, n, top}, g_top) || (top && !read_ints(a[8], B * n * top, top_idx)) ||
-      !read_ints(a[10], B, count) || lse == nullptr)
+      !read_ints(a[10], B, count) || lse == nullptr || !all_on(device, {a[2], a[3], a[4], a[5], a[6], a[7], top ? a[8] : nullptr, a[9], a[10]}, a[11], {k_logits}))
     Py_RETURN_NONE;
   int code;
   Py_BEGIN_ALLOW_THREADS
@@ -686,7 +693,7 @@ PyObject* py_adapt(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     Py_RETURN_NONE;
   bool there = true;
   int32_t* status = sized<int32_t>(a[8], k_status, at::kInt, B, true, there);
-  if (!there) Py_RETURN_NONE;
+  if (!there || !all_on(device, {a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[9]}, a[8], {k_out, k_status})) Py_RETURN_NONE;
   const tslt_rows xr{x->data_ptr(), xs[0], xs[1], 0}, br{base->data_ptr(), bs[0], bs[1], 0}, orows{out->data_ptr(), os[0], os[1], 0};
   int code;
   Py_BEGIN_ALLOW_THREADS

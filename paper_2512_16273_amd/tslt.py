@@ -729,11 +729,12 @@ def cache_evict(cache: dict, pages: torch.Tensor, length: torch.Tensor, weight: 
 
 # ---- around attention and verification ---------------------------------------------------------------------------
 
-def _here(t: torch.Tensor, name: str) -> int:
-    """The current stream; t, a tensor of the call, has to live on its device."""
+def _here(made: dict, names, **given) -> int:
+    """The current stream; the tensors of the call, those of `made` that are named among them, have to live on its device."""
     device = torch.cuda.current_device()
-    if t.device.index != device:
-        raise TsltError(f"{name} lives on {t.device}, the current device is cuda:{device}")
+    for name, t in (*given.items(), *((f"out {name}", made.get(name)) for name in names)):
+        if t is not None and t.device.index != device:
+            raise TsltError(f"{name} lives on {t.device}, the current device is cuda:{device}")
     return torch._C._cuda_getCurrentRawStream(device)
 
 
@@ -817,7 +818,9 @@ def rotate(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[torch.
     _check(lib.tslt_rotate(qr, kr, _dtype_code(q), B, n, heads_q, heads, D, how, _counted(count, "count", B),
                            _rows_of(_given(out, "q"), "out q", q.shape, q.dtype),
                            None if k is None else _rows_of(_given(out, "k"), "out k", k.shape, q.dtype),
-                           _sized(out, "status", torch.int32, B, optional=True), _here(q, "q")))
+                           _sized(out, "status", torch.int32, B, optional=True),
+                           _here(out, ("q", "status") if k is None else ("q", "k", "status"), q=q, k=k, position=position, freq=freq, axis=axis, base=base,
+                                 q_weight=q_weight, k_weight=k_weight, count=count)))
     return out
 
 
@@ -869,7 +872,9 @@ def rotate_backward(grad_q: torch.Tensor, grad_k: Optional[torch.Tensor], q: Opt
                                     _rows_of(_given(out, "q"), "out q", grad_q.shape, dtype),
                                     None if grad_k is None else _rows_of(_given(out, "k"), "out k", grad_k.shape, dtype), dq, dk,
                                     _sized(out, "status", torch.int32, B, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
-                                    _here(grad_q, "grad_q")))
+                                    _here(out, ("q", "q_weight", "k_weight", "status") if grad_k is None else ("q", "k", "q_weight", "k_weight", "status"),
+                                          grad_q=grad_q, grad_k=grad_k, q=q if qr else None, k=k if kr else None, position=position, freq=freq, axis=axis, base=base,
+                                          q_weight=q_weight, k_weight=k_weight, count=count, workspace=ws)))
     return out
 
 
@@ -924,7 +929,8 @@ def logprob(logits: torch.Tensor, temperature: float, tokens: Optional[torch.Ten
                             _sized(out, "top_idx", torch.int32, B * m * top) if top > 0 else None,
                             _sized(out, "top_logp", torch.float32, B * m * top) if top > 0 else None,
                             _sized(out, "status", torch.int32, B * m, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
-                            _here(logits, "logits")))
+                            _here(out, ("logp", "entropy", "lse", "status", "top_idx", "top_logp")[:6 if top > 0 else 4], logits=logits, tokens=tokens, index=index,
+                                  count=count, workspace=ws)))
     return out
 
 
@@ -967,7 +973,8 @@ def logprob_backward(logits: torch.Tensor, temperature: float, tokens: Optional[
                                      _counted(top_idx, "top_idx", B * n * top) if top else None, top, given(grad_logp, "grad_logp"),
                                      given(grad_entropy, "grad_entropy"), given(grad_lse, "grad_lse"),
                                      _optional(grad_top, "grad_top", torch.float32, (B, n, top)), made.data_ptr(), out_seq, out_row,
-                                     _here(logits, "logits")))
+                                     _here(out, ("logits",), logits=logits, tokens=tokens, lse=lse, entropy=entropy, grad_logp=grad_logp, grad_entropy=grad_entropy,
+                                           grad_lse=grad_lse, top_idx=top_idx if top else None, grad_top=grad_top, count=count)))
     return out
 
 
@@ -1013,5 +1020,5 @@ def adapt(x: torch.Tensor, base: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
                           _optional(a, "a", x.dtype, (adapters, R, K)), _optional(b, "b", x.dtype, (adapters, N, R)), adapters, R,
                           _counted(adapter, "adapter", B), _optional(scale, "scale", torch.float32, (adapters,)), _counted(rank, "rank", adapters),
                           _counted(count, "count", B), _sized(out, "status", torch.int32, B, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
-                          _here(x, "x")))
+                          _here(out, ("out", "status"), x=x, base=base, a=a, b=b, adapter=adapter, scale=scale, rank=rank, count=count, workspace=ws)))
     return out
