@@ -468,10 +468,20 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 bool on(const at::Tensor* t, long long device) { return t != nullptr && t->device().index() == device; }
 // The same of those that are tensors among a call's arguments, and of those of its results that are named.
 bool all_on(long long device, std::initializer_list<PyObject*> given, PyObject* made, std::initializer_list<PyObject*> names) {
-  const auto fine = [&](PyObject* o) { return o == nullptr || !THPVariable_Check(o) || THPVariable_Unpack(o).device().index() == device; };
+  const auto fine = [&](PyObject* o) { return o == nullptr || !THPVariable_CheckExact(o) || THPVariable_Unpack(o).device().index() == device; };
   return std::all_of(given.begin(), given.end(), fine) && std::all_of(names.begin(), names.end(), [&](PyObject* name) { return fine(PyDict_GetItem(made, name)); });
 }
 bool fits(std::initializer_list<int64_t> sizes) { return std::max(sizes) <= 0x7FFFFFFF; }
+// Torch is told of results that the call has written to (tensors of inference mode have no versions); what the call returns.
+PyObject* told(int code, PyObject* made, std::initializer_list<PyObject*> names) {
+  for (PyObject* name : names) {
+    PyObject* o = code == TSLT_OK && name ? PyDict_GetItem(made, name) : nullptr;
+    if (o == nullptr || !THPVariable_CheckExact(o)) continue;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  }
+  return result(code);
+}
 // [B][n][heads][D] like the sizes given, dense along D.
 bool read_heads(PyObject* o, at::IntArrayRef sizes, at::ScalarType type, tslt_rows& rows) {
   const at::Tensor* t = plain(o);
@@ -560,7 +570,7 @@ PyObject* py_rotate(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   Py_BEGIN_ALLOW_THREADS
   code = lib.rotate(&qr, k ? &kr : nullptr, tslt_dtype(dt), B, int32_t(n), int32_t(heads_q), int32_t(heads), int32_t(D), &how, count, &oq, k ? &ok : nullptr, status, stream);
   Py_END_ALLOW_THREADS
-  return result(code);
+  return told(code, a[11], {k_q, k ? k_k : nullptr, k_status});
 }
 
 // rotate_backward(grad_q, grad_k, q, k, position, freq, axis, base, q_weight, k_weight, eps, adjacent, count, out, workspace, device, stream)
@@ -597,7 +607,7 @@ PyObject* py_rotate_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   code = lib.rotate_backward(&gqr, keys ? &gkr : nullptr, norm ? &qr : nullptr, norm && keys ? &kr : nullptr, tslt_dtype(dt), B, int32_t(n), int32_t(heads_q), int32_t(heads),
                              int32_t(D), &how, count, &oq, keys ? &ok : nullptr, dq, dk, status, ws, ws_bytes, stream);
   Py_END_ALLOW_THREADS
-  return result(code);
+  return told(code, a[13], {k_q, keys ? k_k : nullptr, k_q_weight, k_k_weight, k_status});
 }
 
 // logprob(logits, temperature, tokens, top, index, count, out, workspace, device, stream)
@@ -631,7 +641,7 @@ PyObject* py_logprob(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   code = lib.logprob(z->data_ptr(), tslt_dtype(dt), B, int32_t(n), V, stride[0], stride[1], float(T), rows, int32_t(m), count, tokens, int32_t(top), logp, entropy, lse, top_idx,
                      top_logp, status, ws, ws_bytes, stream);
   Py_END_ALLOW_THREADS
-  return result(code);
+  return told(code, a[6], {k_logp, k_entropy, k_lse, k_status, top ? k_top_idx : nullptr, top ? k_top_logp : nullptr});
 }
 
 // logprob_backward(logits, temperature, tokens, lse, entropy, grad_logp, grad_entropy, grad_lse, top_idx, grad_top, count, out, device, stream)
@@ -661,7 +671,7 @@ PyObject* py_logprob_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) 
   code = lib.logprob_backward(z->data_ptr(), tslt_dtype(dt), B, int32_t(n), V, stride[0], stride[1], float(T), count, tokens, lse, entropy, top_idx, int32_t(top), g_logp, g_entropy,
                               g_lse, g_top, out->data_ptr(), out_stride[0], out_stride[1], stream);
   Py_END_ALLOW_THREADS
-  return result(code);
+  return told(code, a[11], {k_logits});
 }
 
 // adapt(x, base, a, b, adapter, scale, rank, count, out, workspace, device, stream)
@@ -700,7 +710,7 @@ PyObject* py_adapt(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   code = lib.adapt(&xr, int32_t(K), &br, &orows, int32_t(N), tslt_dtype(dt), B, int32_t(n), down->data_ptr(), up->data_ptr(), adapters, int32_t(R), adapter, scale, rank, count,
                    status, ws, ws_bytes, stream);
   Py_END_ALLOW_THREADS
-  return result(code);
+  return told(code, a[8], {k_out, k_status});
 }
 
 // What a call into torch throws (no memory left, say) becomes a Python exception, as from torch itself.

@@ -728,6 +728,8 @@ def cache_evict(cache: dict, pages: torch.Tensor, length: torch.Tensor, weight: 
 
 
 # ---- around attention and verification ---------------------------------------------------------------------------
+#
+# Results are no part of a graph of autograd's, also of tensors that ask for a gradient: the gradients are the calls rotate_backward and logprob_backward.
 
 def _here(made: dict, names, **given) -> int:
     """The current stream; the tensors of the call, those of `made` that are named among them, have to live on its device."""
@@ -736,6 +738,12 @@ def _here(made: dict, names, **given) -> int:
         if t is not None and t.device.index != device:
             raise TsltError(f"{name} lives on {t.device}, the current device is cuda:{device}")
     return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _told(out: dict, *names: str) -> dict:
+    """out, with torch told that those of its tensors were written to (one that a gradient needs as it was is an error then)."""
+    torch.autograd.graph.increment_version([t for t in map(out.get, names) if t is not None])
+    return out
 
 
 def _current():
@@ -821,7 +829,7 @@ def rotate(q: torch.Tensor, k: Optional[torch.Tensor], position: Optional[torch.
                            _sized(out, "status", torch.int32, B, optional=True),
                            _here(out, ("q", "status") if k is None else ("q", "k", "status"), q=q, k=k, position=position, freq=freq, axis=axis, base=base,
                                  q_weight=q_weight, k_weight=k_weight, count=count)))
-    return out
+    return _told(out, "q", "status") if k is None else _told(out, "q", "k", "status")
 
 
 def rotate_backward_workspace_bytes(B: int, n: int, heads_q: int, heads: int, head_dim: int) -> int:
@@ -875,7 +883,7 @@ def rotate_backward(grad_q: torch.Tensor, grad_k: Optional[torch.Tensor], q: Opt
                                     _here(out, ("q", "q_weight", "k_weight", "status") if grad_k is None else ("q", "k", "q_weight", "k_weight", "status"),
                                           grad_q=grad_q, grad_k=grad_k, q=q if qr else None, k=k if kr else None, position=position, freq=freq, axis=axis, base=base,
                                           q_weight=q_weight, k_weight=k_weight, count=count, workspace=ws)))
-    return out
+    return _told(out, *(("q",) if grad_k is None else ("q", "k")), "q_weight", "k_weight", "status")
 
 
 def _logits(t: torch.Tensor, name: str):
@@ -931,7 +939,7 @@ def logprob(logits: torch.Tensor, temperature: float, tokens: Optional[torch.Ten
                             _sized(out, "status", torch.int32, B * m, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
                             _here(out, ("logp", "entropy", "lse", "status", "top_idx", "top_logp")[:6 if top > 0 else 4], logits=logits, tokens=tokens, index=index,
                                   count=count, workspace=ws)))
-    return out
+    return _told(out, "logp", "entropy", "lse", "status", *(("top_idx", "top_logp") if top > 0 else ()))
 
 
 def logprob_backward(logits: torch.Tensor, temperature: float, tokens: Optional[torch.Tensor], lse: torch.Tensor, entropy: Optional[torch.Tensor] = None,
@@ -975,7 +983,7 @@ def logprob_backward(logits: torch.Tensor, temperature: float, tokens: Optional[
                                      _optional(grad_top, "grad_top", torch.float32, (B, n, top)), made.data_ptr(), out_seq, out_row,
                                      _here(out, ("logits",), logits=logits, tokens=tokens, lse=lse, entropy=entropy, grad_logp=grad_logp, grad_entropy=grad_entropy,
                                            grad_lse=grad_lse, top_idx=top_idx if top else None, grad_top=grad_top, count=count)))
-    return out
+    return _told(out, "logits")
 
 
 def _token_rows(t: torch.Tensor, name: str, shape, dtype) -> _Rows:
@@ -1021,4 +1029,4 @@ def adapt(x: torch.Tensor, base: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
                           _counted(adapter, "adapter", B), _optional(scale, "scale", torch.float32, (adapters,)), _counted(rank, "rank", adapters),
                           _counted(count, "count", B), _sized(out, "status", torch.int32, B, optional=True), _ptr(ws), ws.numel() if ws is not None else 0,
                           _here(out, ("out", "status"), x=x, base=base, a=a, b=b, adapter=adapter, scale=scale, rank=rank, count=count, workspace=ws)))
-    return out
+    return _told(out, "out", "status")
