@@ -88,7 +88,7 @@ template <int D, int kTokens> __device__ __forceinline__ void rotate_turns(const
   const int tid = threadIdx.x;
   bool bad = false;
   for (int e = tid; e < kTokens * max(p.pairs, 1); e += kBlock) {
-    const int tok = p.pairs ? e / p.pairs : e, j = e - tok * p.pairs;
+    const int tok = p.pairs ? e / p.pairs : e, j = p.pairs ? e - tok * p.pairs : 0;      // (without a rotation an entry is a token)
     const int64_t t = t0 + tok;
     const uint32_t seq = uint32_t(t < p.tokens ? t : 0) / uint32_t(p.n);
     const int i = int(uint32_t(t < p.tokens ? t : 0) - seq * uint32_t(p.n));
