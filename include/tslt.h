@@ -506,7 +506,7 @@ int tslt_cache_evict(const tslt_cache* cache, const int32_t* pages, int64_t widt
  *   out         [B][n][N] of type dt, in rows of any alignment; may be base itself (the same place and strides)
  *   status      [B] int32; may be NULL
  * Sums are fp32; x A^T meets B in two terms of the rows' type (16 bits of it for bfloat16, 22 for binary16; fp32 rows: as it is), and the result is
- * rounded once.  A token whose x A^T is not finite gets NaN, or whatever fp32's rules give.
+ * rounded once.  A token whose x A^T is not finite (of bfloat16 rows: rounds to no finite number of theirs) gets NaN, or whatever fp32's rules give.
  * K a multiple of 16 bytes' elements, N any, 2^28 at most.  Workspace: tslt_adapt_workspace_bytes of the same arguments, 256-byte aligned; it need not be cleared. */
 #define TSLT_MAX_ADAPTER_RANK 256
 size_t tslt_adapt_workspace_bytes(int64_t B, int32_t n, int32_t K, int32_t N, int32_t R);

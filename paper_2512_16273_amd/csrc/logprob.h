@@ -512,7 +512,8 @@ __global__ __launch_bounds__(64 * W) void logprob_kernel(const LogprobParams p) 
 // dz = (1 / T) (p (c0 + c1 log2 p) + what the token and the likeliest ones were given), p = 2^(k z - k T lse): elementwise, bound by
 // reading a row and writing one (8 x 256 bfloat16 rows of 128256, all of which count, 203 us, 5.2 TB/s; 42 % of which count, the others filled with zeros, 147).  The few
 // numbers of the second part are put in place by one wave at the end.  Stores go past the caches (173 us with them, then without 178).
-// A row whose lse holds nothing of ln S any more (|lse| from 2^23 on) is added up again, p = 2^(k z - k c) / S with c the largest, by one workgroup, which reads it three times.
+// A row whose lse holds nothing of ln S any more (|lse| from 2^23 on) is added up again, p = 2^(k z - k c) / S with c the largest, by one workgroup, which reads it three times
+// (865 such bfloat16 rows of 128256 187 us, of others 70; 9 of them 43 and 5).
 
 struct LogprobBackwardParams {
   const void* logits;
